@@ -1,0 +1,560 @@
+"""Measured cases of the token log-probabilities, the mixture-of-experts layer of a few samples and
+the low-rank adapters.
+
+Each case is a dict of plain values; its "kind" names the operator:
+
+  logprob  log-probabilities of given tokens with their rows' entropies and most probable
+           alternatives; with "grad" the gradient of the logits too
+  few      routing, experts and combine of up to 64 samples
+  lora     a shared projection with each row's low-rank adapter: "few" rows in any order, or rows
+           in adapter order; with "grad" the gradients of the adapters and the input too
+
+run() computes a case with elementary torch operations in 32 bits, or, where `own` is set, through
+the public binding; exact() has the definitions in 64 bits.
+"""
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+DEV = "cuda"
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+BYTES = {"f32": 4, "bf16": 2}
+ANCHOR_COLS, ANCHOR_TILE = 64, 256
+
+
+# ------------------------------------------------------------------ the cases
+
+def listed():
+    return [
+        # Decoding: the next tag of one sample, of the skewed configuration's vocabulary, with 16
+        # alternatives at a temperature of 0.7.
+        dict(name="logprob_next", kind="logprob", n=1, V=100000, pad=0, dtype="bf16", m=16, scale=1 / 0.7,
+             masked=0.0, stored=False, grad=False),
+        # A small batch scored by fp32 logits of an odd vocabulary in padded rows, a third of the
+        # entries masked.
+        dict(name="logprob_odd", kind="logprob", n=37, V=50021, pad=6, dtype="f32", m=5, scale=1.0,
+             masked=0.33, stored=False, grad=False),
+        # Evaluating a batch by the logits that the balanced configuration's forward stored.
+        dict(name="logprob_stored", kind="logprob", n=4096, V=50000, pad=0, dtype="bf16", m=10, scale=1.0,
+             masked=0.0, stored=True, grad=False),
+        # A tuning step's loss on the balanced configuration's vocabulary: log-probabilities,
+        # entropies and the gradient of both.
+        dict(name="logprob_train", kind="logprob", n=8192, V=50000, pad=0, dtype="bf16", m=0, scale=1.0,
+             masked=0.0, stored=False, grad=True),
+        # The tiny configuration's experts for five samples, biases, fp32: launches are all of it.
+        dict(name="few_tiny", kind="few", n=5, K=8, d=64, h=128, o=64, top=1, act="relu", bias=True,
+             dtype="f32"),
+        # The balanced configuration's gater and experts for one sample.
+        dict(name="few_one", kind="few", n=1, K=16, d=2048, h=4096, o=1024, top=1, act="relu", bias=False,
+             dtype="bf16"),
+        # Eight samples in flight, two gated experts of the skewed configuration's 128 for each.
+        dict(name="few_batch", kind="few", n=8, K=128, d=2048, h=2048, o=1024, top=2, act="silu", bias=False,
+             dtype="bf16"),
+        # As many samples as the operator takes, four experts each: nearly every expert has work.
+        dict(name="few_most", kind="few", n=64, K=128, d=2048, h=2048, o=1024, top=4, act="silu", bias=True,
+             dtype="bf16"),
+        # One sample through a hidden layer of the balanced configuration with its cluster's adapter.
+        dict(name="lora_one", kind="lora", few=True, n=1, E=16, r=16, d=2048, o=4096, bias=True, none=0.0,
+             dtype="bf16", grad=False),
+        # The balanced configuration's decoder with an adapter for each cluster, 48 samples in any
+        # order, some of them without one.
+        dict(name="lora_decoder", kind="lora", few=True, n=48, E=16, r=32, d=1024, o=50000, bias=True, none=0.1,
+             dtype="bf16", grad=False),
+        # The tiny configuration's decoder tuned in fp32, an odd number of rows.
+        dict(name="lora_tiny", kind="lora", few=False, n=777, E=8, r=8, d=64, o=1000, bias=True, none=0.1,
+             dtype="f32", grad=True),
+        # A tuning step of 128 unevenly used adapters beside the balanced configuration's first layer.
+        dict(name="lora_train", kind="lora", few=False, n=16384, E=128, r=16, d=2048, o=4096, bias=False, none=0.05,
+             dtype="bf16", grad=True),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def _width(rng, lo, hi):
+    return max(8, _log(rng, lo, hi) // 8 * 8)
+
+
+def _draw_logprob(rng):
+    stored = rng.random() < 0.25
+    V = _log(rng, 1000, 100000)
+    V = V // 8 * 8 if stored else V
+    n = _log(rng, 1, max(1, min(8192, 400_000_000 // V)))
+    grad = rng.random() < 0.4
+    return dict(kind="logprob", n=n, V=V, pad=0 if stored else rng.choice([0, 0, 1, 8, 24]),
+                dtype=rng.choice(["bf16", "bf16", "f32"]) if n * V < 200_000_000 else "bf16",
+                m=0 if grad and rng.random() < 0.7 else rng.randint(1, 16),
+                scale=rng.choice([1.0, 1.0, rng.uniform(0.5, 2.0)]), masked=0.0 if stored else rng.choice([0.0, 0.0, 0.5]),
+                stored=stored, grad=grad)
+
+
+def _draw_few(rng):
+    K = _log(rng, 4, 128)
+    return dict(kind="few", n=_log(rng, 1, 64), K=K, d=_width(rng, 64, 2048), h=_width(rng, 64, 2048),
+                o=_width(rng, 64, 2048), top=rng.choice([1, 1, 2, 3, 4]), act=rng.choice(["relu", "silu"]),
+                bias=rng.random() < 0.5, dtype=rng.choice(["bf16", "bf16", "f32"]))
+
+
+def _draw_lora(rng):
+    few = rng.random() < 0.4
+    c = dict(kind="lora", few=few, n=_log(rng, 1, 64) if few else _log(rng, 65, 16384), E=_log(rng, 1, 128),
+             r=_width(rng, 8, 128), d=_width(rng, 64, 2048), o=_width(rng, 64, 50000 if few else 4096),
+             bias=rng.random() < 0.5, none=rng.choice([0.0, 0.0, 0.1, 0.4]))
+    c["dtype"] = rng.choice(["bf16", "bf16", "f32"]) if c["n"] * c["d"] * c["o"] < 1 << 34 else "bf16"
+    c["grad"] = not few and rng.random() < 0.6
+    return c
+
+
+def draw(rng):
+    kind = rng.choice(["logprob", "few", "lora"])
+    most = [work(c) for c in listed() if c["kind"] == kind]
+    most = {k: max(w[k] for w in most) for k in ("bytes", "flops")}
+    while True:
+        c = {"logprob": _draw_logprob, "few": _draw_few, "lora": _draw_lora}[kind](rng)
+        w = work(c)
+        if w["bytes"] <= most["bytes"] and w["flops"] <= most["flops"]:
+            return c
+
+
+def work(case):
+    c, b = case, BYTES[case["dtype"]]
+    n = c["n"]
+    if c["kind"] == "logprob":
+        size = n * c["V"]
+        anchors = -(-c["V"] // ANCHOR_TILE) * n * (ANCHOR_TILE // ANCHOR_COLS) * 4 if c["stored"] else 0
+        out = n * (4 + 12 + 8 * c["m"])
+        # max, exp, sum and the entropy's term for an entry; the gradient reads the logits a second
+        # time only because it needs the row's sum first: counted once
+        grad = size * b + 8 * n if c["grad"] else 0
+        return {"bytes": size * b + anchors + out + grad, "flops": size * (12 if c["grad"] else 6)}
+    if c["kind"] == "few":
+        K, d, h, o, top = c["K"], c["d"], c["h"], c["o"], min(c["top"], c["K"])
+        rows = 2 * h if c["act"] == "silu" else h
+        # experts that at least one of the samples chooses, for choices that favour none
+        distinct = K * (1.0 - (1.0 - top / K) ** n)
+        expert = rows * d + o * h + (rows + o if c["bias"] else 0)
+        return {"bytes": int(b * (distinct * expert + K * d + n * (d + o)) + 4 * K + 8 * n * top),
+                "flops": 2 * n * (K * d + top * (rows * d + h * o))}
+    E, r, d, o = c["E"], c["r"], c["d"], c["o"]
+    with_one = 1.0 - c["none"]
+    used = E * (1.0 - (1.0 - with_one / E) ** n)
+    base = 2 * n * d * o
+    ad = 2 * n * with_one * r * (d + o)
+    weights = d * o + (o if c["bias"] else 0) + used * r * (d + o)
+    if not c["grad"]:
+        return {"bytes": int(b * (n * (d + o) + weights) + 4 * n), "flops": int(base + ad)}
+    # forward, and dX, dA, dB: X, dY and the weights once, Y and dX in the data type, dA and dB in fp32
+    return {"bytes": int(b * (2 * n * (d + o) + weights) + 4 * E * r * (d + o) + 4 * n),
+            "flops": int(2 * base + 3 * ad)}
+
+
+# ------------------------------------------------------------------ inputs
+
+def _randn(shape, g, dtype, std=1.0):
+    return (torch.randn(*shape, generator=g, device=DEV, dtype=torch.float32) * std).to(dtype)
+
+
+def _weights(shape, g, dtype, fan_in):
+    """N(0, 1 / fan_in) in the data type, drawn one leading index at a time."""
+    out = torch.empty(*shape, device=DEV, dtype=dtype)
+    for part in out if len(shape) == 3 else (out,):
+        part.copy_(torch.randn(part.shape, generator=g, device=DEV, dtype=torch.float32).mul_(fan_in ** -0.5))
+    return out
+
+
+def _prepare_logprob(c, g):
+    n, V, dt = c["n"], c["V"], DT[c["dtype"]]
+    # a vocabulary in order of frequency: logits that fall with the logarithm of the rank, and noise
+    fall = -1.1 * torch.log(torch.arange(1, V + 1, device=DEV, dtype=torch.float32))
+    full = torch.empty(n, V + c["pad"], device=DEV, dtype=dt)
+    logits = full[:, :V]
+    step = max(1, (1 << 26) // V)
+    for s in range(0, n, step):
+        m = min(step, n - s)
+        logits[s:s + m] = torch.randn(m, V, generator=g, device=DEV).mul_(2.0).add_(fall).to(dt)
+    if c["pad"]:
+        full[:, V:] = float("nan")  # nothing of the padding may be used
+    # tokens as the softmax has them: of low rank mostly
+    token = torch.exp(torch.rand(n, generator=g, device=DEV) * math.log(V)).long().sub_(1).clamp_(0, V - 1)
+    if c["masked"]:
+        for s in range(0, n, step):
+            m = min(step, n - s)
+            off = torch.rand(m, V, generator=g, device=DEV) < c["masked"]
+            off[torch.arange(m, device=DEV), token[s:s + m]] = False
+            off[:, -32:] = False  # as many as there may be alternatives stay
+            logits[s:s + m].masked_fill_(off, float("-inf"))
+    st = {"case": c, "logits": logits, "token": token.to(torch.int32), "anchor": None}
+    if c["stored"]:
+        # the stored form: the largest of each 64 columns, and what every entry is below it
+        nb, slots = -(-V // ANCHOR_COLS), ANCHOR_TILE // ANCHOR_COLS
+        tiles = -(-V // ANCHOR_TILE)
+        anchor = torch.full((n, tiles * slots), -3.0e38, device=DEV)
+        for s in range(0, n, step):
+            m = min(step, n - s)
+            x = torch.full((m, nb * ANCHOR_COLS), float("-inf"), device=DEV)
+            x[:, :V] = logits[s:s + m].float()
+            x = x.view(m, nb, ANCHOR_COLS)
+            top = x.amax(2)
+            anchor[s:s + m, :nb] = top
+            logits[s:s + m] = (x - top[:, :, None]).view(m, -1)[:, :V].to(dt)
+        st["anchor"] = anchor.view(n, tiles, slots).transpose(0, 1).contiguous()
+    if c["grad"]:
+        st["g_logp"] = torch.randn(n, generator=g, device=DEV) / n
+        st["g_entropy"] = torch.randn(n, generator=g, device=DEV) / n
+    if own:
+        from paper_1704_06363_amd import hmoe
+        nbytes = hmoe.token_logprob_workspace(n, V, c["m"], dt)
+        st["ws"] = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=DEV)
+        f = lambda *s: torch.empty(*s, device=DEV)
+        st["out"] = {"logp": f(n), "entropy": f(n), "lse": f(n)}
+        if c["m"]:
+            st["out"]["top_idx"] = torch.empty(n, c["m"], device=DEV, dtype=torch.int32)
+            st["out"]["top_logp"] = f(n, c["m"])
+        if c["grad"]:
+            st["dlogits"] = torch.empty(n, V, device=DEV, dtype=dt)
+    return st
+
+
+def _prepare_few(c, g):
+    n, K, d, h, o, dt = c["n"], c["K"], c["d"], c["h"], c["o"], DT[c["dtype"]]
+    top = min(c["top"], K)
+    rows = 2 * h if c["act"] == "silu" else h
+    if top == 1:
+        # the gater's centres and features around them: the mixtures it is fitted on
+        R = _randn((K, d), g, dt, 2.0)
+        rb = -0.5 * R.float().pow(2).sum(1)
+        X = R.float()[torch.randint(0, K, (2 * n,), generator=g, device=DEV)]
+        X = (X + torch.randn(2 * n, d, generator=g, device=DEV)).to(dt)
+    else:
+        # a learned router's rows, and a small bias that evens out its choices
+        R = _weights((K, d), g, dt, d)
+        rb = torch.randn(K, generator=g, device=DEV) * 0.05
+        X = _randn((2 * n, d), g, dt)
+    # A sample whose choice hangs on the last bits of its scores has no answer to compare: such are
+    # passed over, of twice the samples wanted.
+    s = (X.double() @ R.double().t() + rb.double()).sort(1, descending=True)[0][:, :top + 1]
+    near = (s[:, :-1] - s[:, 1:] < 1e-4 * s.abs().amax()).any(1)
+    X = X[torch.sort(near.int(), stable=True)[1][:n]].contiguous()
+    st = {"case": c, "X": X, "top": top,
+          "p": {"R": R, "r_bias": rb, "W1": _weights((K, rows, d), g, dt, d), "W2": _weights((K, o, h), g, dt, h),
+                "b1": _randn((K, rows), g, dt, 0.1) if c["bias"] else None,
+                "b2": _randn((K, o), g, dt, 0.1) if c["bias"] else None}}
+    if own:
+        from paper_1704_06363_amd import hmoe
+        nbytes = hmoe.moe_few_workspace(st["p"], n, top, c["act"])
+        st["ws"] = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=DEV)
+        st["out"] = {"Y": torch.empty(n, o, device=DEV, dtype=dt),
+                     "expert": torch.empty(n, top, device=DEV, dtype=torch.int32),
+                     "weight": torch.empty(n, top, device=DEV)}
+    return st
+
+
+def _prepare_lora(c, g, seed):
+    n, E, r, d, o, dt = c["n"], c["E"], c["r"], c["d"], c["o"], DT[c["dtype"]]
+    rs = np.random.default_rng(seed)
+    # adapters are used unevenly: shares that fall with the rank, in a random order
+    share = np.arange(1, E + 1, dtype=np.float64) ** -0.8
+    ids = rs.permutation(E)[rs.choice(E, size=n, p=share / share.sum())].astype(np.int32)
+    ids[rs.random(n) < c["none"]] = -1
+    X = _randn((n, d), g, dt).clamp_min_(0.0)
+    p = {"W": _weights((o, d), g, dt, d), "b": _randn((o,), g, dt, 0.1) if c["bias"] else None,
+         "A": _weights((E, r, d), g, dt, d), "B": _weights((E, o, r), g, dt, r),
+         "scale": torch.rand(E, generator=g, device=DEV) + 0.5}
+    st = {"case": c, "X": X, "p": p, "adapter": torch.tensor(ids, device=DEV), "ids": ids}
+    if not c["few"]:
+        key = np.where(ids < 0, E, ids)
+        perm = np.argsort(key, kind="stable").astype(np.int32)
+        off = np.zeros(E + 1, np.int32)
+        off[1:] = np.cumsum(np.bincount(key, minlength=E + 1)[:E])
+        st.update(off=off.tolist(), offsets=torch.tensor(off, device=DEV), perm=torch.tensor(perm, device=DEV))
+        st["X"] = X[st["perm"].long()].contiguous()  # in adapter order, as the dispatch leaves them
+        if c["grad"]:
+            st["dY"] = _randn((n, o), g, dt)
+    if own:
+        from paper_1704_06363_amd import hmoe
+        f = lambda *s: torch.empty(*s, device=DEV)
+        Y = torch.empty(n, o, device=DEV, dtype=dt)
+        if c["few"]:
+            st["out"] = {"Y": Y}
+            nbytes = hmoe.lora_few_workspace(p, n)
+        else:
+            st["out"] = {"Y": Y, "U": torch.empty(hmoe.lora_saved_shape(p, n), device=DEV, dtype=dt)}
+            nbytes = hmoe.lora_workspace(p, n)
+            if c["grad"]:
+                st["gout"] = {"dX": torch.empty(n, d, device=DEV, dtype=dt), "dA": f(E, r, d), "dB": f(E, o, r)}
+        st["ws"] = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=DEV)
+    return st
+
+
+def prepare(case, seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(int(seed))
+    if case["kind"] == "logprob":
+        return _prepare_logprob(case, g)
+    if case["kind"] == "few":
+        return _prepare_few(case, g)
+    return _prepare_lora(case, g, seed)
+
+
+# ------------------------------------------------------------------ one pass
+
+def _key(x):
+    """int64 keys [.., V] in the order (value descending, index ascending) of fp32 values, largest first."""
+    V = x.shape[-1]
+    i = (x + 0.0).view(torch.int32)
+    i = torch.where(i < 0, i ^ 0x7FFFFFFF, i).long()
+    return (i << 32) + (V - 1 - torch.arange(V, device=x.device))
+
+
+def _top(x, m):
+    """The indexes of the m largest entries of each row, ties to the lowest index."""
+    return x.shape[-1] - 1 - (torch.topk(_key(x), m, dim=-1)[0] & 0xFFFFFFFF)
+
+
+def _whole(st):
+    """The logits in 32 bits, anchors added."""
+    x = st["logits"].float()
+    if st["anchor"] is not None:
+        n, V = x.shape
+        a = st["anchor"].transpose(0, 1).reshape(n, -1)
+        x = x + a.repeat_interleave(ANCHOR_COLS, 1)[:, :V]
+    return x
+
+
+def _plain_logprob(st):
+    c = st["case"]
+    x = _whole(st)
+    z = x * c["scale"]
+    tok = st["token"].long()[:, None]
+    mx = z.amax(1, keepdim=True)
+    d = z - mx
+    e = d.exp()
+    s = e.sum(1, keepdim=True)
+    ls = s.log()
+    out = {"logp": (d.gather(1, tok) - ls)[:, 0], "lse": (mx + ls)[:, 0]}
+    ent = ls - torch.where(e > 0, e * d, 0.0).sum(1, keepdim=True) / s
+    out["entropy"] = ent[:, 0]
+    if c["m"]:
+        idx = _top(x, c["m"])
+        out["top_idx"] = idx.to(torch.int32)
+        out["top_logp"] = d.gather(1, idx) - ls
+    if c["grad"]:
+        p = e / s
+        dz = p * (-st["g_logp"])[:, None]
+        dz -= torch.where(p > 0, p * (d - ls + ent), 0.0) * st["g_entropy"][:, None]
+        dz.scatter_add_(1, tok, st["g_logp"][:, None])
+        out["dlogits"] = (dz * c["scale"]).to(st["logits"].dtype)
+    return out
+
+
+def _plain_few(st):
+    c, p, X = st["case"], st["p"], st["X"].float()
+    s = X @ p["R"].float().t() + p["r_bias"]
+    idx = _top(s, st["top"])
+    top = s.gather(1, idx)
+    w = (top - top[:, :1]).exp()
+    w = w / w.sum(1, keepdim=True)
+    Y = torch.zeros(c["n"], c["o"], device=DEV)
+    for i in range(c["n"]):
+        for j in range(st["top"]):
+            e = idx[i, j:j + 1]
+            z = (p["W1"].index_select(0, e)[0].float() * X[i]).sum(1)
+            if c["bias"]:
+                z = z + p["b1"].index_select(0, e)[0].float()
+            if c["act"] == "silu":
+                z, up = z[:c["h"]], z[c["h"]:]
+                hid = z / (1.0 + (-z).exp()) * up
+            else:
+                hid = z.clamp_min(0.0)
+            y = (p["W2"].index_select(0, e)[0].float() * hid).sum(1)
+            if c["bias"]:
+                y = y + p["b2"].index_select(0, e)[0].float()
+            Y[i] += w[i, j] * y
+    return {"Y": Y.to(st["X"].dtype), "expert": idx.to(torch.int32), "weight": w}
+
+
+def _plain_lora(st):
+    c, p, dt = st["case"], st["p"], st["X"].dtype
+    X, W = st["X"].float(), p["W"].float()
+    Y = X @ W.t()
+    if c["bias"]:
+        Y = Y + p["b"].float()
+    if c["few"]:
+        on = (st["adapter"] >= 0).float()
+        a = st["adapter"].long().clamp_min(0)
+        for i in range(c["n"]):
+            A = p["A"].index_select(0, a[i:i + 1])[0].float()
+            B = p["B"].index_select(0, a[i:i + 1])[0].float()
+            u = (A * X[i]).sum(1) * (p["scale"].index_select(0, a[i:i + 1]) * on[i])
+            Y[i] += (B * u).sum(1)
+        return {"Y": Y.to(dt)}
+    off, perm = st["off"], st["perm"].long()
+    U = torch.zeros(c["n"], c["r"], device=DEV)
+    for e in range(c["E"]):
+        s = slice(off[e], off[e + 1])
+        if off[e] == off[e + 1]:
+            continue
+        U[s] = (X[s] @ p["A"][e].float().t()) * p["scale"][e]
+        Y[s] += U[s] @ p["B"][e].float().t()
+    out = {"Y": torch.empty_like(Y, dtype=dt)}
+    out["Y"][perm] = Y.to(dt)
+    if c["grad"]:
+        dY = st["dY"].float()[perm]
+        dX = dY @ W
+        dA, dB = torch.zeros_like(p["A"], dtype=torch.float32), torch.zeros_like(p["B"], dtype=torch.float32)
+        for e in range(c["E"]):
+            s = slice(off[e], off[e + 1])
+            if off[e] == off[e + 1]:
+                continue
+            V = (dY[s] @ p["B"][e].float()) * p["scale"][e]
+            dB[e] = dY[s].t() @ U[s]
+            dA[e] = V.t() @ X[s]
+            dX[s] += V @ p["A"][e].float()
+        out["dX"] = torch.empty_like(dX, dtype=dt)
+        out["dX"][perm] = dX.to(dt)
+        out.update(dA=dA, dB=dB)
+    return out
+
+
+def _own_logprob(st):
+    from paper_1704_06363_amd import hmoe
+    c = st["case"]
+    f = hmoe.token_logprob(st["logits"], st["token"], m=c["m"], scale=c["scale"], anchor=st["anchor"], out=st["out"],
+                           ws=st["ws"])
+    out = {"logp": f["logp"], "lse": f["lse"], "entropy": f["entropy"]}
+    if c["m"]:
+        out.update(top_idx=f["top_idx"], top_logp=f["top_logp"])
+    if c["grad"]:
+        out["dlogits"] = hmoe.token_logprob_backward(st["logits"], st["token"], f["lse"], f["entropy"], st["g_logp"],
+                                                     st["g_entropy"], scale=c["scale"], anchor=st["anchor"],
+                                                     out=st["dlogits"])
+    return out
+
+
+def _own_few(st):
+    from paper_1704_06363_amd import hmoe
+    return hmoe.moe_few(st["p"], st["X"], top_k=st["top"], act=st["case"]["act"], out=st["out"], ws=st["ws"])
+
+
+def _own_lora(st):
+    from paper_1704_06363_amd import hmoe
+    c, p = st["case"], st["p"]
+    if c["few"]:
+        return {"Y": hmoe.lora_few(p, st["X"], st["adapter"], out=st["out"]["Y"], ws=st["ws"])}
+    f = hmoe.lora_forward(p, st["X"], st["offsets"], st["perm"], out=st["out"], ws=st["ws"])
+    out = {"Y": f["Y"]}
+    if c["grad"]:
+        out.update(hmoe.lora_backward(p, st["X"], st["offsets"], st["dY"], f["U"], st["perm"], out=st["gout"],
+                                      ws=st["ws"]))
+    return out
+
+
+def run(state):
+    kind = state["case"]["kind"]
+    if own:
+        return {"logprob": _own_logprob, "few": _own_few, "lora": _own_lora}[kind](state)
+    return {"logprob": _plain_logprob, "few": _plain_few, "lora": _plain_lora}[kind](state)
+
+
+# ------------------------------------------------------------------ 64 bits
+
+def _first(values, m):
+    """Columns of the m largest per row by a stable sort: equal values keep their order."""
+    return torch.argsort(values, dim=1, descending=True, stable=True)[:, :m]
+
+
+def _exact_logprob(c, st):
+    n, V = c["n"], c["V"]
+    rows = max(1, (1 << 25) // V)
+    parts = []
+    for s in range(0, n, rows):
+        t = min(n, s + rows)
+        x = st["logits"][s:t]
+        if st["anchor"] is not None:  # anchor + stored value is an fp32 number by definition
+            col = torch.arange(V, device=DEV)
+            x = st["anchor"][col // ANCHOR_TILE, s:t, (col % ANCHOR_TILE) // ANCHOR_COLS].t() + x.float()
+        x = x.double()
+        lp = torch.log_softmax(x * c["scale"], 1)
+        p = lp.exp()
+        plogp = torch.where(p > 0, p * lp, torch.zeros_like(p))
+        ent = -plogp.sum(1)
+        tok = st["token"][s:t].long()
+        k = torch.arange(t - s, device=DEV)
+        q = {"logp": lp[k, tok], "lse": torch.logsumexp(x * c["scale"], 1), "entropy": ent}
+        if c["m"]:
+            idx = _first(x, c["m"])
+            q["top_idx"] = idx.to(torch.int32)
+            q["top_logp"] = lp.gather(1, idx)
+        if c["grad"]:
+            gl, ge = st["g_logp"][s:t].double()[:, None], st["g_entropy"][s:t].double()[:, None]
+            hot = torch.zeros_like(p)
+            hot[k, tok] = 1.0
+            q["dlogits"] = (gl * (hot - p) - ge * (plogp + p * ent[:, None])) * c["scale"]
+        parts.append(q)
+    return {k: torch.cat([q[k] for q in parts]) for k in parts[0]}
+
+
+def _exact_few(c, st):
+    p, X = st["p"], st["X"].double()
+    s = X @ p["R"].double().t() + p["r_bias"].double()
+    idx = _first(s, st["top"])
+    w = torch.softmax(s.gather(1, idx), 1)
+    Y = torch.zeros(c["n"], c["o"], device=DEV, dtype=torch.float64)
+    for e in torch.unique(idx).tolist():
+        i, j = torch.nonzero(idx == e, as_tuple=True)
+        z = X[i] @ p["W1"][e].double().t()
+        if c["bias"]:
+            z = z + p["b1"][e].double()
+        if c["act"] == "silu":
+            hid = torch.nn.functional.silu(z[:, :c["h"]]) * z[:, c["h"]:]
+        else:
+            hid = torch.relu(z)
+        y = hid @ p["W2"][e].double().t()
+        if c["bias"]:
+            y = y + p["b2"][e].double()
+        Y.index_add_(0, i, w[i, j][:, None] * y)
+    return {"Y": Y, "expert": idx.to(torch.int32), "weight": w}
+
+
+def _exact_lora(c, st):
+    p = st["p"]
+    n, E = c["n"], c["E"]
+    ids = torch.tensor(st["ids"], device=DEV)
+    X = st["X"].double()
+    if not c["few"]:
+        back = torch.empty_like(st["perm"].long())
+        back[st["perm"].long()] = torch.arange(n, device=DEV)
+        X = X[back]  # in sample order
+    W = p["W"].double()
+    Y = X @ W.t()
+    if c["bias"]:
+        Y = Y + p["b"].double()
+    out = {"Y": Y}
+    if c["grad"]:
+        dY = st["dY"].double()
+        out["dX"] = dY @ W
+        out["dA"] = torch.zeros(p["A"].shape, device=DEV, dtype=torch.float64)
+        out["dB"] = torch.zeros(p["B"].shape, device=DEV, dtype=torch.float64)
+    for e in range(E):
+        rows = torch.nonzero(ids == e)[:, 0]
+        if rows.numel() == 0:
+            continue
+        A, B, sc = p["A"][e].double(), p["B"][e].double(), p["scale"][e].double()
+        x = X[rows]
+        Y[rows] += sc * ((x @ A.t()) @ B.t())
+        if c["grad"]:
+            dy = dY[rows]
+            out["dX"][rows] += sc * ((dy @ B) @ A)
+            out["dB"][e] = sc * (dy.t() @ (x @ A.t()))
+            out["dA"][e] = sc * ((dy @ B).t() @ x)
+    return out
+
+
+def exact(case, seed):
+    st = prepare(case, seed)
+    return {"logprob": _exact_logprob, "few": _exact_few, "lora": _exact_lora}[case["kind"]](case, st)
