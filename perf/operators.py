@@ -211,7 +211,7 @@ def _prepare_logprob(c, g):
         nbytes = hmoe.token_logprob_workspace(n, V, c["m"], dt)
         st["ws"] = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=DEV)
         f = lambda *s: torch.empty(*s, device=DEV)
-        st["out"] = {"logp": f(n), "entropy": f(n), "lse": f(n)}
+        st["out"] = {"logp": f(n), "entropy": f(n), "lse": f(n), "stat": f(n, 2)}
         if c["m"]:
             st["out"]["top_idx"] = torch.empty(n, c["m"], device=DEV, dtype=torch.int32)
             st["out"]["top_logp"] = f(n, c["m"])
@@ -430,7 +430,7 @@ def _own_logprob(st):
     if c["m"]:
         out.update(top_idx=f["top_idx"], top_logp=f["top_logp"])
     if c["grad"]:
-        out["dlogits"] = hmoe.token_logprob_backward(st["logits"], st["token"], f["lse"], f["entropy"], st["g_logp"],
+        out["dlogits"] = hmoe.token_logprob_backward(st["logits"], st["token"], f["stat"], f["entropy"], st["g_logp"],
                                                      st["g_entropy"], scale=c["scale"], anchor=st["anchor"],
                                                      out=st["dlogits"])
     return out
