@@ -1,0 +1,70 @@
+// lm_api.hip -- the extern "C" entry points of include/hmoe_lm.h: argument validation, workspace
+// checks and dispatch to the launchers.  Host code only.
+#include <math.h>
+
+#include "checks.hpp"
+#include "lm_launch.hpp"
+
+using namespace hmoe;
+
+extern "C" {
+
+// ------------------------------------------------------------------ token log-probabilities
+
+static int check_logits(const void* logits, int64_t ld, const float* anchor, hmoe_dtype_t dt, int64_t n, int32_t vocab,
+                        float scale) {
+  HMOE_TRY(check_dtype(dt));
+  HMOE_TRY(check_n(n));
+  if (vocab < 1) return fail(HMOE_EINVAL, "vocab = %d is not positive", vocab);
+  if (ld < vocab) return fail(HMOE_EINVAL, "ld = %lld is less than vocab = %d", (long long)ld, vocab);
+  if (!(scale > 0.f) || isinf(scale)) return fail(HMOE_EINVAL, "scale = %g is not positive and finite", (double)scale);
+  if (n == 0) return HMOE_OK;
+  HMOE_TRY(check_ptr("logits", logits, anchor != nullptr));
+  if (reinterpret_cast<uintptr_t>(logits) % dtype_size(dt)) return fail(HMOE_ESHAPE, "logits are not aligned to their type");
+  if (anchor) {
+    HMOE_TRY(check_ptr("anchor", anchor));
+    HMOE_TRY(check_width("vocab (with anchors)", vocab));
+    if (ld != vocab) return fail(HMOE_ESHAPE, "anchored logits with rows %lld apart, vocab = %d", (long long)ld, vocab);
+  }
+  return HMOE_OK;
+}
+
+size_t hmoe_token_logprob_workspace(int64_t n, int32_t vocab, int32_t m, hmoe_dtype_t dt) {
+  if (n <= 0 || n >= (int64_t(1) << 31) || vocab < 1 || m < 0 || m > 16 || (dt != HMOE_F32 && dt != HMOE_BF16)) return 0;
+  return token_logprob_ws(n, vocab, m, dt);
+}
+
+int hmoe_token_logprob(const void* logits, int64_t ld, const float* anchor, hmoe_dtype_t dt, int64_t n, int32_t vocab,
+                       float scale, const int32_t* token, int32_t m, float* logp, float* entropy, float* lse,
+                       float* stat, int32_t* top_idx, float* top_logp, void* ws, size_t ws_bytes, void* stream) {
+  clear_error();
+  HMOE_TRY(check_logits(logits, ld, anchor, dt, n, vocab, scale));
+  if (m < 0 || m > 16 || m > vocab) return fail(HMOE_EINVAL, "m = %d outside [0, min(16, vocab)]", m);
+  if (n == 0) return HMOE_OK;
+  if (m > 0) HMOE_TRY(check_ptr("top_idx", top_idx, false));
+  HMOE_TRY(check_ws(token_logprob_ws(n, vocab, m, dt), ws_bytes, ws));
+  Workspace w(ws, ws_bytes);
+  return launch_token_logprob(logits, ld, anchor, dt, n, vocab, scale, token, m, logp, entropy, lse, stat, top_idx,
+                              top_logp, w, (hipStream_t)stream);
+}
+
+int hmoe_token_logprob_backward(const void* logits, int64_t ld, const float* anchor, hmoe_dtype_t dt, int64_t n,
+                                int32_t vocab, float scale, const int32_t* token, const float* stat,
+                                const float* entropy, const float* g_logp, const float* g_entropy, void* dlogits,
+                                int64_t ld_out, void* stream) {
+  clear_error();
+  HMOE_TRY(check_logits(logits, ld, anchor, dt, n, vocab, scale));
+  if (ld_out < vocab) return fail(HMOE_EINVAL, "ld_out = %lld is less than vocab = %d", (long long)ld_out, vocab);
+  if (n == 0) return HMOE_OK;
+  HMOE_TRY(check_ptr("stat", stat, false));
+  HMOE_TRY(check_ptr("dlogits", dlogits, false));
+  if (reinterpret_cast<uintptr_t>(dlogits) % dtype_size(dt)) return fail(HMOE_ESHAPE, "dlogits are not aligned to their type");
+  if (g_logp) HMOE_TRY(check_ptr("token", token, false));
+  if (g_entropy) HMOE_TRY(check_ptr("entropy", entropy, false));
+  if (dlogits == logits && (anchor || ld_out != ld))
+    return fail(HMOE_EINVAL, "dlogits in place of logits needs plain logits and the same stride");
+  return launch_token_logprob_backward(logits, ld, anchor, dt, n, vocab, scale, token, stat, entropy, g_logp,
+                                       g_entropy, dlogits, ld_out, (hipStream_t)stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,18 @@
+// lm_launch.hpp -- launchers behind include/hmoe_lm.h.  As in launch.hpp they only enqueue work on
+// `st`; sizes have been validated by the caller.
+#pragma once
+#include "hmoe_lm.h"
+#include "launch.hpp"
+
+namespace hmoe {
+
+// logprob.hip
+size_t token_logprob_ws(int64_t n, int V, int m, hmoe_dtype_t dt);
+int launch_token_logprob(const void* L, int64_t ld, const float* anc, hmoe_dtype_t dt, int64_t n, int V, float scale,
+                         const int32_t* token, int m, float* logp, float* entropy, float* lse, float* stat,
+                         int32_t* top_idx, float* top_logp, Workspace& ws, hipStream_t st);
+int launch_token_logprob_backward(const void* L, int64_t ld, const float* anc, hmoe_dtype_t dt, int64_t n, int V,
+                                  float scale, const int32_t* token, const float* stat, const float* entropy,
+                                  const float* g_logp, const float* g_entropy, void* dL, int64_t ldo, hipStream_t st);
+
+}  // namespace hmoe

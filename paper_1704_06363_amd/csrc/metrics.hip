@@ -19,6 +19,7 @@
 // k_topm_hits: one thread per row (p) and per draw (q); the rank of each matching tag in the
 // top-m list adds 1 to every m' above it.  Integer counts, summed through LDS and then with
 // one 64-bit atomic per block and m' -- integer sums, so the result does not depend on order.
+#include "lanes.hpp"
 #include "launch.hpp"
 #include "primitives.hpp"
 
@@ -113,17 +114,6 @@ __device__ __forceinline__ float mth_lane_value(float x, int m, int l) {
   xor2();
   xor1();
   return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), m - 1));
-}
-
-// Set bits of `mask` below this lane.
-__device__ __forceinline__ int lanes_below(uint64_t mask) {
-  return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
-}
-
-// Orders a wave's LDS writes before its later reads by other lanes of the same wave.
-__device__ __forceinline__ void wave_lds_fence() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
 }
 
 template <typename T, int M>

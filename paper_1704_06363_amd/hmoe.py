@@ -1,4 +1,4 @@
-"""Python binding of libhmoe.so (include/hmoe.h): argument marshalling only.
+"""Python binding of libhmoe.so (include/hmoe.h and include/hmoe_lm.h): argument marshalling only.
 
 Tensors are torch tensors on the GPU; every function hands their device pointers, the
 current HIP stream and a workspace to the C ABI and returns the output tensors.  No step of
@@ -29,6 +29,11 @@ SYMBOLS = (
     "hmoe_pca_workspace", "hmoe_pca_fit", "hmoe_pca_project",
     "hmoe_sgd_step", "hmoe_topm", "hmoe_topm_hits",
     "hmoe_timer_enable", "hmoe_timer_report",
+)
+
+# include/hmoe_lm.h
+LM_SYMBOLS = (
+    "hmoe_token_logprob_workspace", "hmoe_token_logprob", "hmoe_token_logprob_backward",
 )
 
 
@@ -97,6 +102,14 @@ def lib():
         L.hmoe_timer_enable.restype = _c.c_int
         L.hmoe_timer_report.argtypes = [_c.c_char_p, _SZ]
         L.hmoe_timer_report.restype = _I64
+        L.hmoe_token_logprob_workspace.restype = _SZ
+        L.hmoe_token_logprob_workspace.argtypes = [_I64, _I32, _I32, _c.c_int]
+        L.hmoe_token_logprob.argtypes = [_P, _I64, _P, _c.c_int, _I64, _I32, _c.c_float, _P, _I32, _P, _P, _P, _P,
+                                         _P, _P, _P, _SZ, _P]
+        L.hmoe_token_logprob_backward.argtypes = [_P, _I64, _P, _c.c_int, _I64, _I32, _c.c_float, _P, _P, _P, _P, _P,
+                                                  _P, _I64, _P]
+        for name in ("hmoe_token_logprob", "hmoe_token_logprob_backward"):
+            getattr(L, name).restype = _c.c_int
         for name in ("hmoe_kmeans_assign", "hmoe_kmeans_fit", "hmoe_kmeans_update",
                      "hmoe_moe_dispatch", "hmoe_moe_dispatch_noalloc", "hmoe_permute_rows", "hmoe_moe_forward",
                      "hmoe_moe_backward", "hmoe_pca_fit", "hmoe_pca_project", "hmoe_sgd_step",
@@ -511,6 +524,76 @@ def topm_hits(idx, row_ptr, tag, q_sample=None, q_tag=None, out=None):
     _chk(lib().hmoe_topm_hits(_ptr(idx), n, m, ctypes.byref(lab), _ptr(q_sample), _ptr(q_tag), S, _ptr(hits),
                               _stream()), "topm_hits")
     return hits
+
+
+# ------------------------------------------------------------------ token log-probabilities
+
+def _rows_ptr(t, what):
+    """(pointer, row stride in elements) of a matrix whose rows are contiguous."""
+    n, w = t.shape
+    if not t.is_cuda:
+        raise HmoeError("tensor is not on the GPU")
+    if w > 1 and t.stride(1) != 1:
+        raise HmoeError(f"{what}: the entries of a row are not contiguous")
+    return t.data_ptr(), (t.stride(0) if n > 1 else max(w, 1))
+
+
+def token_logprob_workspace(n, V, m, dtype) -> int:
+    return lib().hmoe_token_logprob_workspace(n, V, m, _DT[dtype])
+
+
+def token_logprob(logits, token=None, m: int = 0, scale: float = 1.0, anchor=None, out=None, ws=None):
+    """Log-probabilities of a given token per row of logits [n, V] (rows may be strided), entropies and the
+    m most probable alternatives, of softmax(scale * logits), in one pass.  token int32 [n]; one outside
+    [0, V) marks a row without a token (0).  anchor: as in topm.  Returns logp (None without token),
+    entropy, lse [n], stat [n, 2] (for token_logprob_backward) and, with m > 0, top_idx [n, m] int32 and
+    top_logp [n, m] fp32.  Of these, `out` (a dict) passes buffers; an entry of None is not computed."""
+    n, V = logits.shape
+    o = out or {}
+    dev = logits.device
+    f32, i32 = torch.float32, torch.int32
+    dt = _dt(logits)
+    _expect(token, (n,), i32, "token")
+    _expect(anchor, anchor_shape(n, V), f32, "anchor")
+    r = {}
+    for k, shape, dtype in (("logp", (n,), f32), ("entropy", (n,), f32), ("lse", (n,), f32), ("stat", (n, 2), f32),
+                            ("top_idx", (n, m), i32), ("top_logp", (n, m), f32)):
+        if (k == "logp" and token is None) or (m == 0 and k[0] == "t"):
+            r[k] = None
+        elif k in o:
+            r[k] = o[k]
+            _expect(r[k], shape, dtype, k)
+        else:
+            r[k] = torch.empty(shape, dtype=dtype, device=dev)
+    at, ld = _rows_ptr(logits, "logits")
+    w, wb = _workspace(lib().hmoe_token_logprob_workspace(n, V, m, dt), ws, dev)
+    _chk(lib().hmoe_token_logprob(at, ld, _ptr(anchor), dt, n, V, scale, _ptr(token), m, _ptr(r["logp"]),
+                                  _ptr(r["entropy"]), _ptr(r["lse"]), _ptr(r["stat"]), _ptr(r["top_idx"]),
+                                  _ptr(r["top_logp"]), _ptr(w), wb, _stream()), "token_logprob")
+    return r
+
+
+def token_logprob_backward(logits, token, stat, entropy=None, g_logp=None, g_entropy=None, scale: float = 1.0,
+                           anchor=None, out=None):
+    """The gradient with respect to the logits [n, V] of sum(g_logp * logp) + sum(g_entropy * entropy),
+    from the forward's stat and (with g_entropy) entropy.  out: a buffer, which may be logits itself."""
+    n, V = logits.shape
+    f32 = torch.float32
+    dt = _dt(logits)
+    _expect(token, (n,), torch.int32, "token")
+    _expect(stat, (n, 2), f32, "stat")
+    for t, k in ((entropy, "entropy"), (g_logp, "g_logp"), (g_entropy, "g_entropy")):
+        _expect(t, (n,), f32, k)
+    _expect(anchor, anchor_shape(n, V), f32, "anchor")
+    _expect(out, (n, V), logits.dtype, "out")
+    if out is None:
+        out = torch.empty((n, V), dtype=logits.dtype, device=logits.device)
+    at, ld = _rows_ptr(logits, "logits")
+    to, ldo = _rows_ptr(out, "out")
+    _chk(lib().hmoe_token_logprob_backward(at, ld, _ptr(anchor), dt, n, V, scale, _ptr(token), _ptr(stat),
+                                           _ptr(entropy), _ptr(g_logp), _ptr(g_entropy), to, ldo, _stream()),
+         "token_logprob_backward")
+    return out
 
 
 # ------------------------------------------------------------------ parameter update

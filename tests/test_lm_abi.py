@@ -1,0 +1,87 @@
+"""The entry points of include/hmoe_lm.h: exported, bound, and refusing bad arguments before anything is
+launched (no GPU needed)."""
+import ctypes
+import os
+import re
+
+import pytest
+import torch
+
+from paper_1704_06363_amd import hmoe
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+F = ctypes.c_float
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(hmoe.LIB_PATH):
+        from paper_1704_06363_amd import build
+        build.build()
+    return hmoe.lib()
+
+
+def refused(rc, code, word):
+    assert rc == code and word in hmoe.last_error(), (rc, hmoe.last_error())
+
+
+def test_exports_every_declared_symbol(lib):
+    src = open(os.path.join(ROOT, "include", "hmoe_lm.h")).read()
+    names = sorted(set(re.findall(r"\b(hmoe_[a-z_]+)\s*\(", re.sub(r"/\*.*?\*/", "", src, flags=re.S))))
+    assert set(names) == set(hmoe.LM_SYMBOLS)
+    for name in names:
+        assert hasattr(lib, name), name
+
+
+def test_token_logprob_refusals(lib):
+    def call(logits=16, ld=64, anchor=None, dt=1, n=10, vocab=64, scale=1.0, token=16, m=3, top=16, ws=None, wb=0):
+        return lib.hmoe_token_logprob(logits, ld, anchor, dt, n, vocab, F(scale), token, m, 16, 16, 16, 16, top, 16, ws,
+                                      wb, None)
+    refused(call(logits=None), -1, "logits")
+    refused(call(logits=17), -3, "aligned")
+    refused(call(dt=9), -2, "dtype")
+    refused(call(n=-1), -1, "n =")
+    refused(call(vocab=0), -1, "vocab")
+    refused(call(ld=63), -1, "ld")
+    for scale in (0.0, -1.0, float("nan"), float("inf")):
+        refused(call(scale=scale), -1, "scale")
+    refused(call(m=17), -1, "m = 17")
+    refused(call(m=-1), -1, "m = -1")
+    refused(call(vocab=8, m=9), -1, "m = 9")
+    refused(call(top=None), -1, "top_idx")
+    refused(call(anchor=20), -3, "anchor")
+    refused(call(anchor=16, ld=72), -3, "apart")
+    refused(call(anchor=16, vocab=60, ld=60), -3, "vocab")
+    refused(call(anchor=16, logits=18), -3, "aligned")
+    refused(call(vocab=100000, ld=100000, n=1), -4, "workspace")
+    assert call(n=0, logits=None) == 0
+    assert lib.hmoe_token_logprob_workspace(1, 100000, 16, 1) > 0
+    assert lib.hmoe_token_logprob_workspace(0, 100000, 16, 1) == 0
+
+    def grad(logits=16, ld=64, anchor=None, token=16, stat=16, entropy=16, gl=16, ge=16, out=32, ldo=64):
+        return lib.hmoe_token_logprob_backward(logits, ld, anchor, 1, 10, 64, F(1.0), token, stat, entropy, gl, ge, out,
+                                               ldo, None)
+    refused(grad(stat=None), -1, "stat")
+    refused(grad(token=None), -1, "token")
+    refused(grad(entropy=None), -1, "entropy")
+    refused(grad(out=None), -1, "dlogits")
+    refused(grad(out=33), -3, "aligned")
+    refused(grad(ldo=63), -1, "ld_out")
+    refused(grad(out=16, ldo=72), -1, "in place")
+    refused(grad(out=16, anchor=16), -1, "in place")
+
+
+def test_token_logprob_binding_refusals():
+    x, t = torch.zeros(4, 10), torch.zeros(4, dtype=torch.int32)
+    with pytest.raises(hmoe.HmoeError, match="GPU"):
+        hmoe.token_logprob(x, t)
+    with pytest.raises(hmoe.HmoeError, match="token: dtype"):
+        hmoe.token_logprob(x, t.long())
+    with pytest.raises(hmoe.HmoeError, match="token: shape"):
+        hmoe.token_logprob(x, t[:3])
+    with pytest.raises(hmoe.HmoeError, match="dtype"):
+        hmoe.token_logprob(x.half(), t)
+    with pytest.raises(hmoe.HmoeError, match="top_idx: shape"):
+        hmoe.token_logprob(x, t, m=3, out={"top_idx": torch.zeros(4, 2, dtype=torch.int32)})
+    with pytest.raises(hmoe.HmoeError, match="stat: shape"):
+        hmoe.token_logprob_backward(x, t, torch.zeros(4), None, torch.zeros(4))
