@@ -59,6 +59,46 @@ int hmoe_token_logprob_backward(const void* logits, int64_t ld, const float* anc
                                 const float* entropy, const float* g_logp, const float* g_entropy, void* dlogits,
                                 int64_t ld_out, void* stream);
 
+/* ------------------------------------------------------------------ mixture layer of a few samples */
+
+/* What an expert does between its layers. */
+enum {
+  HMOE_ACT_RELU = 0,      /* h = max(0, W1 x + b1), W1 [K][d_hid][d_in], b1 [K][d_hid]: hmoe_moe_params_t's */
+  HMOE_ACT_SILU_GATED = 1 /* h = silu(g) u, silu(g) = g / (1 + e^-g); W1 [K][2 d_hid][d_in], b1 [K][2 d_hid]: the
+                           * first d_hid rows give g, the others u */
+};
+
+#define HMOE_FEW_ROWS 64  /* most rows of the entry points for a few of them */
+#define HMOE_FEW_EXPERTS 8 /* most experts of a sample */
+
+/* A mixture layer that routes by itself.  R [K][d_in] the router's rows, r_bias float[K] or NULL; W2
+ * [K][d_out][d_hid], b2 [K][d_out]; biases may be NULL; matrices and biases in dtype dt.
+ * The gater of Eq. 2 over centres C is R = C, r_bias[e] = -|C_e|^2 / 2, top_k = 1: the nearest centre has the
+ * largest x . C_e - |C_e|^2 / 2. */
+typedef struct {
+  int32_t K, d_in, d_hid, d_out, top_k;
+  hmoe_dtype_t dt;
+  int32_t act; /* HMOE_ACT_* */
+  const void* R;
+  const float* r_bias;
+  const void *W1, *b1, *W2, *b2;
+} hmoe_few_params_t;
+
+/* The whole layer for 1 <= n <= HMOE_FEW_ROWS samples, for serving: no sort, no padding, each
+ * expert that is chosen read once.  For row i of X [n x d_in]:
+ *   s_e = R_e . x + r_bias[e];  expert[i][0 .. top_k) = the top_k largest, in decreasing order, equal ones in
+ *   increasing e (NaN ranks last);  weight[i][j] = softmax of those top_k scores;
+ *   Y[i] = sum_j weight[i][j] (W2_e h + b2_e), e = expert[i][j].
+ * A weight below 2^-126, the smallest normal float, is 0, and an expert of weight 0 is not evaluated: one
+ * with a score of -inf (r_bias[e] = -inf: it is off) never is.  A row of nothing else has Y = 0.  Scores, sums, h and weights are held in fp32; for the second product
+ * of bf16 data h is split into two bf16 numbers, so nothing but Y is rounded to bf16.
+ *   expert int32[n][top_k], weight float[n][top_k], Y [n x d_out] in dtype dt: out.
+ * 1 <= top_k <= min(HMOE_FEW_EXPERTS, K).  Errors: HMOE_EINVAL (n, K, top_k or act out of range, NULL pointer),
+ * HMOE_ESHAPE (width not a multiple of 8, misaligned pointer), HMOE_EDTYPE, HMOE_EWORKSPACE. */
+size_t hmoe_moe_few_workspace(const hmoe_few_params_t* p, int64_t n);
+int hmoe_moe_few(const hmoe_few_params_t* p, int64_t n, const void* X, int32_t* expert, float* weight, void* Y,
+                 void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -67,4 +67,49 @@ int hmoe_token_logprob_backward(const void* logits, int64_t ld, const float* anc
                                        g_entropy, dlogits, ld_out, (hipStream_t)stream);
 }
 
+// ------------------------------------------------------------------ mixture layer of a few samples
+
+static int check_few_rows(int64_t n) {
+  if (n < 0 || n > HMOE_FEW_ROWS) return fail(HMOE_EINVAL, "n = %lld outside [0, %d]", (long long)n, HMOE_FEW_ROWS);
+  return HMOE_OK;
+}
+
+static int check_few(const hmoe_few_params_t* p, int64_t n) {
+  if (!p) return fail(HMOE_EINVAL, "params are NULL");
+  HMOE_TRY(check_dtype(p->dt));
+  HMOE_TRY(check_k(p->K));
+  HMOE_TRY(check_width("d_in", p->d_in));
+  HMOE_TRY(check_width("d_hid", p->d_hid));
+  HMOE_TRY(check_width("d_out", p->d_out));
+  if (p->top_k < 1 || p->top_k > HMOE_FEW_EXPERTS || p->top_k > p->K)
+    return fail(HMOE_EINVAL, "top_k = %d outside [1, min(%d, K)]", p->top_k, HMOE_FEW_EXPERTS);
+  if (p->act != HMOE_ACT_RELU && p->act != HMOE_ACT_SILU_GATED) return fail(HMOE_EINVAL, "unknown act %d", p->act);
+  return check_few_rows(n);
+}
+
+size_t hmoe_moe_few_workspace(const hmoe_few_params_t* p, int64_t n) {
+  if (check_few(p, n) != HMOE_OK || n == 0) {
+    clear_error();
+    return 0;
+  }
+  return moe_few_ws(p, n);
+}
+
+int hmoe_moe_few(const hmoe_few_params_t* p, int64_t n, const void* X, int32_t* expert, float* weight, void* Y,
+                 void* ws, size_t ws_bytes, void* stream) {
+  clear_error();
+  HMOE_TRY(check_few(p, n));
+  if (n == 0) return HMOE_OK;
+  HMOE_TRY(check_ptr("R", p->R));
+  HMOE_TRY(check_ptr("W1", p->W1));
+  HMOE_TRY(check_ptr("W2", p->W2));
+  HMOE_TRY(check_ptr("X", X));
+  HMOE_TRY(check_ptr("expert", expert, false));
+  HMOE_TRY(check_ptr("weight", weight, false));
+  HMOE_TRY(check_ptr("Y", Y));
+  HMOE_TRY(check_ws(moe_few_ws(p, n), ws_bytes, ws));
+  Workspace w(ws, ws_bytes);
+  return launch_moe_few(p, n, X, expert, weight, Y, w, (hipStream_t)stream);
+}
+
 }  // extern "C"

@@ -15,4 +15,9 @@ int launch_token_logprob_backward(const void* L, int64_t ld, const float* anc, h
                                   float scale, const int32_t* token, const float* stat, const float* entropy,
                                   const float* g_logp, const float* g_entropy, void* dL, int64_t ldo, hipStream_t st);
 
+// moe_few.hip
+size_t moe_few_ws(const hmoe_few_params_t* p, int64_t n);
+int launch_moe_few(const hmoe_few_params_t* p, int64_t n, const void* X, int32_t* expert, float* weight, void* Y,
+                   Workspace& ws, hipStream_t st);
+
 }  // namespace hmoe

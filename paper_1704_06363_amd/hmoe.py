@@ -34,6 +34,7 @@ SYMBOLS = (
 # include/hmoe_lm.h
 LM_SYMBOLS = (
     "hmoe_token_logprob_workspace", "hmoe_token_logprob", "hmoe_token_logprob_backward",
+    "hmoe_moe_few_workspace", "hmoe_moe_few",
 )
 
 
@@ -47,6 +48,13 @@ class MoeParams(ctypes.Structure):
                 ("W1", ctypes.c_void_p), ("b1", ctypes.c_void_p), ("W2", ctypes.c_void_p),
                 ("b2", ctypes.c_void_p), ("D", ctypes.c_void_p), ("bD", ctypes.c_void_p),
                 ("decoders", ctypes.c_int32)]
+
+
+class FewParams(ctypes.Structure):
+    _fields_ = [("K", ctypes.c_int32), ("d_in", ctypes.c_int32), ("d_hid", ctypes.c_int32),
+                ("d_out", ctypes.c_int32), ("top_k", ctypes.c_int32), ("dt", ctypes.c_int), ("act", ctypes.c_int32),
+                ("R", ctypes.c_void_p), ("r_bias", ctypes.c_void_p), ("W1", ctypes.c_void_p),
+                ("b1", ctypes.c_void_p), ("W2", ctypes.c_void_p), ("b2", ctypes.c_void_p)]
 
 
 class Labels(ctypes.Structure):
@@ -108,7 +116,10 @@ def lib():
                                          _P, _P, _P, _SZ, _P]
         L.hmoe_token_logprob_backward.argtypes = [_P, _I64, _P, _c.c_int, _I64, _I32, _c.c_float, _P, _P, _P, _P, _P,
                                                   _P, _I64, _P]
-        for name in ("hmoe_token_logprob", "hmoe_token_logprob_backward"):
+        L.hmoe_moe_few_workspace.restype = _SZ
+        L.hmoe_moe_few_workspace.argtypes = [_c.POINTER(FewParams), _I64]
+        L.hmoe_moe_few.argtypes = [_c.POINTER(FewParams), _I64, _P, _P, _P, _P, _P, _SZ, _P]
+        for name in ("hmoe_token_logprob", "hmoe_token_logprob_backward", "hmoe_moe_few"):
             getattr(L, name).restype = _c.c_int
         for name in ("hmoe_kmeans_assign", "hmoe_kmeans_fit", "hmoe_kmeans_update",
                      "hmoe_moe_dispatch", "hmoe_moe_dispatch_noalloc", "hmoe_permute_rows", "hmoe_moe_forward",
@@ -594,6 +605,57 @@ def token_logprob_backward(logits, token, stat, entropy=None, g_logp=None, g_ent
                                            _ptr(entropy), _ptr(g_logp), _ptr(g_entropy), to, ldo, _stream()),
          "token_logprob_backward")
     return out
+
+
+# ------------------------------------------------------------------ mixture layer of a few samples
+
+FEW_ROWS, FEW_EXPERTS = 64, 8  # include/hmoe_lm.h: HMOE_FEW_ROWS, HMOE_FEW_EXPERTS
+_ACT = {"relu": 0, "silu": 1}
+
+
+def make_few_params(p: dict, top_k: int = 1, act: str = "relu") -> FewParams:
+    """p: the router R [K, d] with r_bias [K] (fp32) or None, W1 [K, h, d] ([K, 2h, d] for "silu", the gated
+    activation), b1 or None, W2 [K, o, h], b2 [K, o] or None."""
+    if act not in _ACT:
+        raise HmoeError(f"unknown activation {act!r}")
+    K, o, h = p["W2"].shape
+    dt = p["W1"].dtype
+    d = p["W1"].shape[2]
+    rows = 2 * h if act == "silu" else h
+    for k, shape, t in (("W1", (K, rows, d), dt), ("W2", (K, o, h), dt), ("R", (K, d), dt), ("b1", (K, rows), dt),
+                        ("b2", (K, o), dt), ("r_bias", (K,), torch.float32)):
+        _expect(p.get(k), shape, t, k)
+    return FewParams(K, d, h, o, top_k, _dt(p["W1"]), _ACT[act], _ptr(p["R"]), _ptr(p.get("r_bias")), _ptr(p["W1"]),
+                     _ptr(p.get("b1")), _ptr(p["W2"]), _ptr(p.get("b2")))
+
+
+def moe_few_workspace(p, n, top_k: int = 1, act: str = "relu") -> int:
+    prm = p if isinstance(p, FewParams) else make_few_params(p, top_k, act)
+    return lib().hmoe_moe_few_workspace(ctypes.byref(prm), n)
+
+
+def moe_few(p, X, top_k: int = 1, act: str = "relu", out=None, ws=None):
+    """The whole mixture layer for up to FEW_ROWS samples X [n, d]: routing by the top_k scores of R x + r_bias,
+    experts, combine (include/hmoe_lm.h).  p: a dict as in make_few_params, or the FewParams made from one.  With R
+    the gater's centres, r_bias = -|R|^2 / 2 and top_k = 1 it is Eq. 2's hard gate.  Returns Y [n, o], expert int32
+    [n, top_k] and weight fp32 [n, top_k]."""
+    prm = p if isinstance(p, FewParams) else make_few_params(p, top_k, act)
+    n = X.shape[0]
+    dev = X.device
+    o = out or {}
+    if _dt(X) != prm.dt:
+        raise HmoeError(f"X: dtype {X.dtype}, the parameters' expected")
+    k = prm.top_k
+    _expect(X, (n, prm.d_in), None, "X")
+    r = {}
+    for key, shape, dtype in (("Y", (n, prm.d_out), X.dtype), ("expert", (n, k), torch.int32),
+                              ("weight", (n, k), torch.float32)):
+        r[key] = o[key] if key in o else torch.empty(shape, dtype=dtype, device=dev)
+        _expect(r[key], shape, dtype, key)
+    w, wb = _workspace(lib().hmoe_moe_few_workspace(ctypes.byref(prm), n), ws, dev)
+    _chk(lib().hmoe_moe_few(ctypes.byref(prm), n, _ptr(X), _ptr(r["expert"]), _ptr(r["weight"]), _ptr(r["Y"]), _ptr(w),
+                            wb, _stream()), "moe_few")
+    return r
 
 
 # ------------------------------------------------------------------ parameter update

@@ -85,3 +85,49 @@ def test_token_logprob_binding_refusals():
         hmoe.token_logprob(x, t, m=3, out={"top_idx": torch.zeros(4, 2, dtype=torch.int32)})
     with pytest.raises(hmoe.HmoeError, match="stat: shape"):
         hmoe.token_logprob_backward(x, t, torch.zeros(4), None, torch.zeros(4))
+
+
+def test_moe_few_refusals(lib):
+    def call(n=4, X=16, expert=16, weight=16, Y=16, ws=None, wb=0, **kw):
+        a = dict(K=8, d_in=64, d_hid=128, d_out=64, top_k=2, dt=1, act=0, R=16, r_bias=16, W1=16, b1=None, W2=16,
+                 b2=None)
+        a.update(kw)
+        p = hmoe.FewParams(*a.values())
+        return lib.hmoe_moe_few(ctypes.byref(p), n, X, expert, weight, Y, ws, wb, None)
+    assert lib.hmoe_moe_few(None, 1, 16, 16, 16, 16, None, 0, None) == -1
+    refused(call(dt=5), -2, "dtype")
+    refused(call(K=0), -1, "K = 0")
+    refused(call(K=4097), -1, "K = 4097")
+    refused(call(d_in=60), -3, "d_in")
+    refused(call(d_hid=0), -3, "d_hid")
+    refused(call(d_out=12), -3, "d_out")
+    refused(call(top_k=0), -1, "top_k")
+    refused(call(top_k=9, K=16), -1, "top_k")
+    refused(call(top_k=3, K=2), -1, "top_k")
+    refused(call(act=2), -1, "act")
+    refused(call(n=65), -1, "n = 65")
+    refused(call(n=-1), -1, "n = -1")
+    refused(call(R=None), -1, "R")
+    refused(call(W1=20), -3, "W1")
+    refused(call(X=None), -1, "X")
+    refused(call(expert=None), -1, "expert")
+    refused(call(weight=None), -1, "weight")
+    refused(call(Y=24), -3, "Y")
+    refused(call(), -4, "workspace")
+    assert call(n=0, X=None) == 0
+
+
+def test_moe_few_binding_refusals():
+    b = torch.bfloat16
+    p = {"R": torch.zeros(3, 16, dtype=b), "r_bias": None, "W1": torch.zeros(3, 24, 16, dtype=b), "b1": None,
+         "W2": torch.zeros(3, 8, 24, dtype=b), "b2": None}
+    with pytest.raises(hmoe.HmoeError, match="activation"):
+        hmoe.make_few_params(p, 1, "tanh")
+    with pytest.raises(hmoe.HmoeError, match="W1: shape"):
+        hmoe.make_few_params(p, 1, "silu")
+    with pytest.raises(hmoe.HmoeError, match="r_bias: dtype"):
+        hmoe.make_few_params(dict(p, r_bias=torch.zeros(3, dtype=b)))
+    with pytest.raises(hmoe.HmoeError, match="R: shape"):
+        hmoe.make_few_params(dict(p, R=torch.zeros(4, 16, dtype=b)))
+    with pytest.raises(hmoe.HmoeError, match="GPU"):
+        hmoe.make_few_params(p)
