@@ -99,6 +99,52 @@ size_t hmoe_moe_few_workspace(const hmoe_few_params_t* p, int64_t n);
 int hmoe_moe_few(const hmoe_few_params_t* p, int64_t n, const void* X, int32_t* expert, float* weight, void* Y,
                  void* ws, size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------------------------ low-rank adapters */
+
+#define HMOE_LORA_RANK 128          /* largest rank */
+#define HMOE_LORA_WIDTH (1 << 21)   /* largest d_in and d_out */
+#define HMOE_LORA_ROWS (1 << 28)    /* most rows */
+
+/* A projection W [d_out][d_in] with bias b [d_out] (or NULL) that all rows share, and E adapters beside it:
+ * A [E][rank][d_in], B [E][d_out][rank], scale float[E] (NULL: ones); matrices and b in dtype dt.  With
+ * adapter a, or none:
+ *   y = W x + b + scale[a] B_a (A_a x).
+ * d_in, d_out and rank are multiples of 8 up to the limits above, 1 <= E <= 4096.  A hard mixture's experts can
+ * be such adapters (one per cluster), and so can its decoders, beside one D. */
+typedef struct {
+  int32_t E, d_in, d_out, rank;
+  hmoe_dtype_t dt;
+  const void *W, *b, *A, *B;
+  const float* scale;
+} hmoe_lora_t;
+
+/* For serving: n <= HMOE_FEW_ROWS rows X [n x d_in] of any mix of requests, adapter int32[n] (an id outside
+ * [0, E): none); Y [n x d_out] out.  W is read once, and so is each adapter that is used. */
+size_t hmoe_lora_few_workspace(const hmoe_lora_t* p, int64_t n);
+int hmoe_lora_few(const hmoe_lora_t* p, int64_t n, const void* X, const int32_t* adapter, void* Y, void* ws,
+                  size_t ws_bytes, void* stream);
+
+/* Many rows, in adapter order as hmoe_moe_dispatch leaves them: X_sorted [n x d_in], rows [offsets[a],
+ * offsets[a + 1]) with adapter a and rows from offsets[E] on without one; offsets int32[E + 1] starts at 0.
+ * perm int32[n] (slot -> sample, a permutation), or NULL: Y's rows are in slot order too.
+ *   Y [n x d_out] out, sample order.
+ *   U [n][hmoe_lora_saved_width] out, dtype dt: scale A x of every row with an adapter, for the
+ *     backward: fp32 values; with bf16 data blocks of 16 values and 16 remainders, so that U is good to 2^-16. */
+int32_t hmoe_lora_saved_width(int32_t rank, hmoe_dtype_t dt);
+size_t hmoe_lora_workspace(const hmoe_lora_t* p, int64_t n);
+int hmoe_lora_forward(const hmoe_lora_t* p, int64_t n, const void* X_sorted, const int32_t* offsets,
+                      const int32_t* perm, void* U, void* Y, void* ws, size_t ws_bytes, void* stream);
+
+/* Gradients with respect to the adapters and the input; W, b and scale are fixed.  With V = scale B_a^T dY:
+ *   dA[a] = sum over a's rows of V x^T, dB[a] = sum of dY U^T: float, A's and B's shapes, zeros for adapters
+ *   without rows, sums in a fixed order;  dX [n x d_in] (dtype dt, sample order) = W^T dY + A_a^T V.
+ *   dY [n x d_out] in sample order (slot order without perm).  dX, dA and dB may each be NULL.
+ * Errors of the four: HMOE_EINVAL (n, E or rank out of range, NULL pointer), HMOE_ESHAPE (width not a multiple
+ * of 8, misaligned pointer), HMOE_EDTYPE, HMOE_EWORKSPACE. */
+int hmoe_lora_backward(const hmoe_lora_t* p, int64_t n, const void* X_sorted, const int32_t* offsets,
+                       const int32_t* perm, const void* U, const void* dY, void* dX, float* dA, float* dB, void* ws,
+                       size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -16,8 +16,8 @@ ROOT = os.path.dirname(PKG)
 SRC = os.path.join(PKG, "csrc")
 OUT = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libhmoe.so")
-SOURCES = ["api.hip", "dispatch.hip", "kmeans.hip", "lm_api.hip", "logprob.hip", "metrics.hip", "moe.hip", "moe_few.hip",
-           "optim.hip", "pca.hip"]
+SOURCES = ["api.hip", "dispatch.hip", "kmeans.hip", "lm_api.hip", "logprob.hip", "lora.hip", "metrics.hip",
+           "moe.hip", "moe_few.hip", "optim.hip", "pca.hip"]
 ARCH = "gfx950"
 
 # Packed fp32 instructions are kept out of the generated code (hipcc's host pass warns that it

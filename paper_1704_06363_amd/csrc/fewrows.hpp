@@ -1,7 +1,7 @@
 // fewrows.hpp -- weights streamed past a few rows of activations: the products of 16 weight rows
 // with 16 activation rows, fragments loaded straight from HBM into registers.
 #pragma once
-#include "common.hpp"
+#include "lanes.hpp"
 
 namespace hmoe {
 
@@ -36,5 +36,54 @@ struct Halves {
     }
   }
 };
+
+// The slot-th of the groups 0 .. G - 1 that have rows, in ascending order, and its rows of the `total`
+// in ascending order, at most HMOE_FEW_ROWS.  A row whose group is outside [0, G) has none.  False if
+// there are not that many groups.  Entered by workgroups of THREADS >= 128; G <= 4096.
+template <int THREADS>
+__device__ __forceinline__ bool few_group(const int32_t* __restrict__ group, int total, int G, int slot, int* s_group,
+                                          int* s_rows, int* s_count) {
+  __shared__ uint32_t mask[128];
+  const int t = threadIdx.x;
+  if (t < 128) mask[t] = 0;
+  if (t == 0) *s_group = -1;
+  __syncthreads();
+  for (int q = t; q < total; q += THREADS) {
+    const int e = group[q];
+    if (e >= 0 && e < G) atomicOr(&mask[e >> 5], 1u << (e & 31));
+  }
+  __syncthreads();
+  if (t < 64) {
+    const uint32_t m0 = mask[2 * t], m1 = mask[2 * t + 1];
+    const int c = __popc(m0) + __popc(m1);
+    int inc = c;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(inc, o, 64);
+      if (t >= o) inc += v;
+    }
+    const int before = inc - c;
+    if (slot >= before && slot < inc) {
+      uint64_t both = ((uint64_t)m1 << 32) | m0;
+      for (int i = slot - before; i > 0; --i) both &= both - 1;
+      *s_group = 64 * t + __builtin_ctzll(both);
+    }
+  }
+  __syncthreads();
+  const int e = *s_group;
+  if (e < 0) return false;
+  if (t < 64) {
+    int count = 0;
+    for (int b = 0; b < total; b += 64) {
+      const bool mine = b + t < total && group[b + t] == e;
+      const uint64_t hit = __ballot(mine);
+      if (mine) s_rows[count + lanes_below(hit)] = b + t;
+      count += __popcll(hit);
+    }
+    if (t == 0) *s_count = count;
+  }
+  __syncthreads();
+  return true;
+}
 
 }  // namespace hmoe

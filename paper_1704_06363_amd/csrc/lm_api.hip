@@ -112,4 +112,107 @@ int hmoe_moe_few(const hmoe_few_params_t* p, int64_t n, const void* X, int32_t* 
   return launch_moe_few(p, n, X, expert, weight, Y, w, (hipStream_t)stream);
 }
 
+// ------------------------------------------------------------------ low-rank adapters
+
+static int check_lora(const hmoe_lora_t* p) {
+  if (!p) return fail(HMOE_EINVAL, "params are NULL");
+  HMOE_TRY(check_dtype(p->dt));
+  if (p->E < 1 || p->E > 4096) return fail(HMOE_EINVAL, "E = %d outside [1, 4096]", p->E);
+  HMOE_TRY(check_width("d_in", p->d_in));
+  HMOE_TRY(check_width("d_out", p->d_out));
+  HMOE_TRY(check_width("rank", p->rank));
+  if (p->rank > HMOE_LORA_RANK) return fail(HMOE_EINVAL, "rank = %d exceeds %d", p->rank, HMOE_LORA_RANK);
+  if (p->d_in > HMOE_LORA_WIDTH || p->d_out > HMOE_LORA_WIDTH)
+    return fail(HMOE_EINVAL, "d_in = %d or d_out = %d exceeds %d", p->d_in, p->d_out, HMOE_LORA_WIDTH);
+  return HMOE_OK;
+}
+
+static int check_lora_rows(int64_t n) {
+  if (n < 0 || n > HMOE_LORA_ROWS) return fail(HMOE_EINVAL, "n = %lld outside [0, %d]", (long long)n, HMOE_LORA_ROWS);
+  return HMOE_OK;
+}
+
+static int check_lora_params(const hmoe_lora_t* p) {
+  HMOE_TRY(check_ptr("W", p->W));
+  HMOE_TRY(check_ptr("A", p->A));
+  return check_ptr("B", p->B);
+}
+
+size_t hmoe_lora_few_workspace(const hmoe_lora_t* p, int64_t n) {
+  if (check_lora(p) != HMOE_OK || check_few_rows(n) != HMOE_OK || n == 0) {
+    clear_error();
+    return 0;
+  }
+  return lora_few_ws(p, n);
+}
+
+int hmoe_lora_few(const hmoe_lora_t* p, int64_t n, const void* X, const int32_t* adapter, void* Y, void* ws,
+                  size_t ws_bytes, void* stream) {
+  clear_error();
+  HMOE_TRY(check_lora(p));
+  HMOE_TRY(check_few_rows(n));
+  if (n == 0) return HMOE_OK;
+  HMOE_TRY(check_lora_params(p));
+  HMOE_TRY(check_ptr("X", X));
+  HMOE_TRY(check_ptr("adapter", adapter, false));
+  HMOE_TRY(check_ptr("Y", Y));
+  HMOE_TRY(check_ws(lora_few_ws(p, n), ws_bytes, ws));
+  Workspace w(ws, ws_bytes);
+  return launch_lora_few(p, n, X, adapter, Y, w, (hipStream_t)stream);
+}
+
+int32_t hmoe_lora_saved_width(int32_t rank, hmoe_dtype_t dt) {
+  if (rank < 1 || rank > HMOE_LORA_RANK || (dt != HMOE_F32 && dt != HMOE_BF16)) return 0;
+  return lora_saved_width(rank, dt);
+}
+
+size_t hmoe_lora_workspace(const hmoe_lora_t* p, int64_t n) {
+  if (check_lora(p) != HMOE_OK || check_lora_rows(n) != HMOE_OK || n == 0) {
+    clear_error();
+    return 0;
+  }
+  return lora_ws(p, n);
+}
+
+int hmoe_lora_forward(const hmoe_lora_t* p, int64_t n, const void* X_sorted, const int32_t* offsets,
+                      const int32_t* perm, void* U, void* Y, void* ws, size_t ws_bytes, void* stream) {
+  clear_error();
+  HMOE_TRY(check_lora(p));
+  HMOE_TRY(check_lora_rows(n));
+  if (n == 0) return HMOE_OK;
+  HMOE_TRY(check_lora_params(p));
+  HMOE_TRY(check_ptr("X_sorted", X_sorted));
+  HMOE_TRY(check_ptr("offsets", offsets, false));
+  HMOE_TRY(check_ptr("U", U));
+  HMOE_TRY(check_ptr("Y", Y));
+  HMOE_TRY(check_ws(lora_ws(p, n), ws_bytes, ws));
+  Workspace w(ws, ws_bytes);
+  return launch_lora_forward(p, n, X_sorted, offsets, perm, U, Y, w, (hipStream_t)stream);
+}
+
+int hmoe_lora_backward(const hmoe_lora_t* p, int64_t n, const void* X_sorted, const int32_t* offsets,
+                       const int32_t* perm, const void* U, const void* dY, void* dX, float* dA, float* dB, void* ws,
+                       size_t ws_bytes, void* stream) {
+  clear_error();
+  HMOE_TRY(check_lora(p));
+  HMOE_TRY(check_lora_rows(n));
+  if (dA) HMOE_TRY(check_ptr("dA", dA));
+  if (dB) HMOE_TRY(check_ptr("dB", dB));
+  if (n > 0) {
+    HMOE_TRY(check_lora_params(p));
+    HMOE_TRY(check_ptr("X_sorted", X_sorted));
+    HMOE_TRY(check_ptr("offsets", offsets, false));
+    HMOE_TRY(check_ptr("U", U));
+    HMOE_TRY(check_ptr("dY", dY));
+    if (dX) HMOE_TRY(check_ptr("dX", dX));
+    HMOE_TRY(check_ws(lora_ws(p, n), ws_bytes, ws));
+    Workspace w(ws, ws_bytes);
+    return launch_lora_backward(p, n, X_sorted, offsets, perm, U, dY, dX, dA, dB, w, (hipStream_t)stream);
+  }
+  // no rows: the adapters' gradients are zeros
+  if (dA) HMOE_TRY(launch_zero_f32(dA, (int64_t)p->E * p->rank * p->d_in, (hipStream_t)stream));
+  if (dB) HMOE_TRY(launch_zero_f32(dB, (int64_t)p->E * p->rank * p->d_out, (hipStream_t)stream));
+  return HMOE_OK;
+}
+
 }  // extern "C"

@@ -20,4 +20,15 @@ size_t moe_few_ws(const hmoe_few_params_t* p, int64_t n);
 int launch_moe_few(const hmoe_few_params_t* p, int64_t n, const void* X, int32_t* expert, float* weight, void* Y,
                    Workspace& ws, hipStream_t st);
 
+// lora.hip
+int lora_saved_width(int rank, hmoe_dtype_t dt);
+size_t lora_few_ws(const hmoe_lora_t* p, int64_t n);
+size_t lora_ws(const hmoe_lora_t* p, int64_t n);
+int launch_lora_few(const hmoe_lora_t* p, int64_t n, const void* X, const int32_t* adapter, void* Y, Workspace& ws,
+                    hipStream_t st);
+int launch_lora_forward(const hmoe_lora_t* p, int64_t n, const void* X, const int32_t* offsets, const int32_t* perm,
+                        void* U, void* Y, Workspace& ws, hipStream_t st);
+int launch_lora_backward(const hmoe_lora_t* p, int64_t n, const void* X, const int32_t* offsets, const int32_t* perm,
+                         const void* U, const void* dY, void* dX, float* dA, float* dB, Workspace& ws, hipStream_t st);
+
 }  // namespace hmoe

@@ -1,0 +1,613 @@
+// lora.hip -- a shared projection with a low-rank adapter for each group of rows:
+//   Y_i = W x_i + b + s_a B_a (A_a x_i),  a the adapter of row i (or none),
+// and its gradients with W fixed:  with V_i = s_a B_a^T dY_i,
+//   dX_i = W^T dY_i + A_a^T V_i,   dB_a = sum_i dY_i (s_a A_a x_i)^T,   dA_a = sum_i V_i x_i^T.
+//
+// The narrow products U = s A x and V stay in fp32 accuracy: for bf16 data each value is kept as two
+// bf16 numbers, and since the fragments of one MFMA step hold 32 values of K, 16 values of U with their
+// remainders fill exactly one step against 16 values of B taken twice (row layout of U below).  The
+// second number costs no instruction and makes the fp32 gradients good to 2^-16 instead of 2^-9.
+#include "fewrows.hpp"
+#include "gemm.hpp"
+#include "lm_launch.hpp"
+#include "primitives.hpp"
+
+namespace hmoe {
+
+namespace {
+
+// A row of U or V: bf16: blocks of 32, 16 values of the rank (zeros past it) and then their
+// remainders; fp32: the values.
+__host__ __device__ inline int u_blocks(int rank) { return (rank + 15) / 16; }
+template <typename T>
+__host__ __device__ inline int u_width(int rank) {
+  return sizeof(T) == 2 ? 32 * u_blocks(rank) : rank;
+}
+
+// This lane's 16 bytes of step kb of row `row` of U.
+template <typename T>
+__device__ __forceinline__ i32x4 u_frag(const T* __restrict__ U, int64_t row, int ldu, int kb, int lg, int rank) {
+  if constexpr (sizeof(T) == 2) return *reinterpret_cast<const i32x4*>(U + row * ldu + 32 * kb + 8 * lg);
+  return 16 * kb + 4 * lg < rank ? *reinterpret_cast<const i32x4*>(U + row * ldu + 16 * kb + 4 * lg) : i32x4{0, 0, 0, 0};
+}
+// And of the row of `rank` values that multiplies it (bf16: the same for the value and its remainder).
+template <typename T>
+__device__ __forceinline__ i32x4 r_frag(const T* __restrict__ row, int kb, int lg, int rank) {
+  const int c = sizeof(T) == 2 ? 16 * kb + 8 * (lg & 1) : 16 * kb + 4 * lg;
+  return c < rank ? *reinterpret_cast<const i32x4*>(row + c) : i32x4{0, 0, 0, 0};
+}
+// Stores four values 16 kb + 4 lg .. of a row of U (those past the rank as zeros).
+template <typename T>
+__device__ __forceinline__ void u_store(T* __restrict__ U, int64_t row, int ldu, int kb, int lg, int rank, floatx4 v) {
+  const bool in = 16 * kb + 4 * lg < rank;  // the rank is a multiple of 8
+  if constexpr (sizeof(T) == 2) {
+    vec4<T> hi, lo;
+#pragma unroll
+    for (int z = 0; z < 4; ++z) {
+      const Halves<T> p(in ? v[z] : 0.f);
+      hi[z] = p.part[0];
+      lo[z] = p.part[1];
+    }
+    *reinterpret_cast<vec4<T>*>(U + row * ldu + 32 * kb + 4 * lg) = hi;
+    *reinterpret_cast<vec4<T>*>(U + row * ldu + 32 * kb + 16 + 4 * lg) = lo;
+  } else if (in) {
+    *reinterpret_cast<floatx4*>(U + row * ldu + 16 * kb + 4 * lg) = v;
+  }
+}
+
+// ------------------------------------------------------------------ few rows
+
+struct LoraFew {
+  const void *X, *W, *b, *A, *B;
+  const float* scale;
+  const int32_t* adapter;
+  int n, E, d, o, rank;
+  void* U;
+  void* Y;
+};
+
+// U of 16 values of the rank for the rows of one adapter; the waves split d.
+constexpr int kFewShrinkWaves = 8;
+template <typename T>
+__global__ void __launch_bounds__(64 * kFewShrinkWaves) k_lora_few_shrink(LoraFew a) {
+  constexpr int N = 16 / sizeof(T), STEP = 4 * N, NW = kFewShrinkWaves;
+  __shared__ int s_group, s_count, s_rows[HMOE_FEW_ROWS];
+  __shared__ floatx4 s_acc[NW][64];
+  const int blocks = u_blocks(a.rank), kb = blockIdx.x % blocks;
+  if (!few_group<64 * NW>(a.adapter, a.n, a.E, blockIdx.x / blocks, &s_group, s_rows, &s_count)) return;
+  const int e = s_group, count = s_count, ldu = u_width<T>(a.rank);
+  const int l = threadIdx.x & 63, w = threadIdx.x >> 6, lr = l & 15, lg = l >> 4;
+  const int r = 16 * kb + lr < a.rank ? 16 * kb + lr : a.rank - 1;
+  const T* A = static_cast<const T*>(a.A) + ((int64_t)e * a.rank + r) * a.d;
+  const int steps = (a.d + STEP - 1) / STEP, s0 = steps * w / NW, s1 = steps * (w + 1) / NW;
+  const float scale = a.scale ? a.scale[e] : 1.f;
+  for (int t0 = 0; t0 < count; t0 += 16) {
+    const int row = s_rows[t0 + lr < count ? t0 + lr : count - 1];
+    const T* x = static_cast<const T*>(a.X) + (int64_t)row * a.d;
+    floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int s = s0; s < s1; ++s) {
+      const int at = s * STEP + lg * N;
+      const i32x4 av = at < a.d ? *reinterpret_cast<const i32x4*>(A + at) : i32x4{0, 0, 0, 0};
+      const i32x4 xv = at < a.d ? *reinterpret_cast<const i32x4*>(x + at) : i32x4{0, 0, 0, 0};
+      step_mfma<T>(av, xv, acc);
+    }
+    s_acc[w][l] = acc;
+    __syncthreads();
+    if (w == 0 && t0 + lr < count) {
+      acc = s_acc[0][l];
+#pragma unroll
+      for (int q = 1; q < NW; ++q) acc += s_acc[q][l];
+      u_store(static_cast<T*>(a.U), row, ldu, kb, lg, a.rank, acc * scale);
+    }
+    __syncthreads();
+  }
+}
+
+// 16 MI columns of Y for all rows (16 NT at most); the waves split d, and the adapters of the rows.
+template <typename T, int MI, int NT>
+__global__ void __launch_bounds__(256) k_lora_few(LoraFew a) {
+  constexpr int N = 16 / sizeof(T), STEP = 4 * N;
+  __shared__ floatx4 s_acc[4][MI][NT][64];
+  const int l = threadIdx.x & 63, w = threadIdx.x >> 6, lr = l & 15, lg = l >> 4;
+  const int c0 = blockIdx.x * 16 * MI;
+  const T* W[MI];
+  int col[MI];
+#pragma unroll
+  for (int i = 0; i < MI; ++i) {
+    col[i] = c0 + 16 * i + lr < a.o ? c0 + 16 * i + lr : a.o - 1;
+    W[i] = static_cast<const T*>(a.W) + (int64_t)col[i] * a.d;
+  }
+  const T* x[NT];
+  int row[NT], mine[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    row[t] = 16 * t + lr < a.n ? 16 * t + lr : a.n - 1;
+    x[t] = static_cast<const T*>(a.X) + (int64_t)row[t] * a.d;
+    mine[t] = a.adapter[row[t]];
+  }
+  const int all = a.adapter[l < a.n ? l : a.n - 1];  // a lane to a row
+  floatx4 acc[MI][NT];
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) acc[i][t] = floatx4{0.f, 0.f, 0.f, 0.f};
+  const int steps = (a.d + STEP - 1) / STEP, s0 = steps * w / 4, s1 = steps * (w + 1) / 4;
+#pragma unroll 4
+  for (int s = s0; s < s1; ++s) {
+    const int at = s * STEP + lg * N;
+    i32x4 wv[MI], xv[NT];
+#pragma unroll
+    for (int i = 0; i < MI; ++i) wv[i] = at < a.d ? *reinterpret_cast<const i32x4*>(W[i] + at) : i32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int t = 0; t < NT; ++t) xv[t] = at < a.d ? *reinterpret_cast<const i32x4*>(x[t] + at) : i32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) step_mfma<T>(wv[i], xv[t], acc[i][t]);
+  }
+  // the adapters in the order of their first rows, one to a wave in turn
+  uint64_t left = __ballot(l < a.n && all >= 0 && all < a.E);
+  const int ldu = u_width<T>(a.rank), blocks = u_blocks(a.rank);
+  for (int turn = 0; left != 0; ++turn) {
+    const int e = __builtin_amdgcn_readlane(all, __builtin_ctzll(left));
+    const uint64_t with = __ballot(all == e) & left;
+    left &= ~with;
+    if (turn % 4 != w) continue;
+    const T* B = static_cast<const T*>(a.B) + (int64_t)e * a.o * a.rank;
+    // sums of their own, which only the adapter's rows take: another row's zeros times an infinite B would
+    // not be zeros
+    floatx4 own[MI][NT];
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) own[i][t] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int kb = 0; kb < blocks; ++kb) {
+      i32x4 bv[MI];
+#pragma unroll
+      for (int i = 0; i < MI; ++i) bv[i] = r_frag(B + (int64_t)col[i] * a.rank, kb, lg, a.rank);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        if (((with >> (16 * t)) & 0xffff) == 0) continue;
+        i32x4 uv = {0, 0, 0, 0};
+        if (mine[t] == e) uv = u_frag(static_cast<const T*>(a.U), row[t], ldu, kb, lg, a.rank);
+#pragma unroll
+        for (int i = 0; i < MI; ++i) step_mfma<T>(bv[i], uv, own[i][t]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+        if (mine[t] == e) acc[i][t] += own[i][t];
+  }
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) s_acc[w][i][t][l] = acc[i][t];
+  __syncthreads();
+  for (int q = w; q < MI * NT; q += 4) {
+    const int i = q / NT, t = q % NT, c = c0 + 16 * i + 4 * lg;
+    floatx4 v = (s_acc[0][i][t][l] + s_acc[1][i][t][l]) + (s_acc[2][i][t][l] + s_acc[3][i][t][l]);
+    if (16 * t + lr >= a.n || c >= a.o) continue;
+    vec4<T> y;
+#pragma unroll
+    for (int z = 0; z < 4; ++z) y[z] = from_f32<T>(v[z] + (a.b ? to_f32(static_cast<const T*>(a.b)[c + z]) : 0.f));
+    *reinterpret_cast<vec4<T>*>(static_cast<T*>(a.Y) + (int64_t)(16 * t + lr) * a.o + c) = y;
+  }
+}
+
+template <typename T, int MI>
+int lora_few_mi(const LoraFew& a, hipStream_t st) {
+  const dim3 grid((unsigned)cdiv(a.o, 16 * MI)), block(256);
+  switch ((a.n + 15) / 16) {
+    case 1: HMOE_LAUNCH("lora few", (k_lora_few<T, MI, 1>), grid, block, 0, st, a); break;
+    case 2: HMOE_LAUNCH("lora few", (k_lora_few<T, MI, 2>), grid, block, 0, st, a); break;
+    case 3: HMOE_LAUNCH("lora few", (k_lora_few<T, MI, 3>), grid, block, 0, st, a); break;
+    default: HMOE_LAUNCH("lora few", (k_lora_few<T, MI, 4>), grid, block, 0, st, a); break;
+  }
+  return HMOE_OK;
+}
+
+template <typename T>
+int lora_few_t(const LoraFew& a, hipStream_t st) {
+  const int slots = a.n < a.E ? a.n : a.E;
+  HMOE_LAUNCH("lora few shrink", k_lora_few_shrink<T>, dim3((unsigned)(slots * u_blocks(a.rank))),
+              dim3(64 * kFewShrinkWaves), 0, st, a);
+  // wide outputs: two blocks of columns to a workgroup, which halves the reads of X
+  if (a.o >= 16 * 1024) return lora_few_mi<T, 2>(a, st);
+  return lora_few_mi<T, 1>(a, st);
+}
+
+// ------------------------------------------------------------------ rows in adapter order
+
+// U = s_e rows A_e^T for 32 rows of one adapter and 16 RT values of the rank: rows [n][K], A [E][rank][K].
+// The four waves split K.
+template <typename T, int RT>
+__global__ void __launch_bounds__(256) k_lora_shrink(const T* __restrict__ X, int K, const T* __restrict__ A, int rank,
+                                                     const float* __restrict__ scale, const int32_t* __restrict__ seg,
+                                                     const int32_t* __restrict__ tile_start, int E, T* __restrict__ U) {
+  constexpr int N = 16 / sizeof(T), STEP = 4 * N, MT = 2;
+  __shared__ floatx4 s_acc[4][RT][MT][64];
+  const int64_t tile = blockIdx.x;
+  if (tile >= tile_start[E]) return;
+  const int e = find_segment(tile_start, E, tile);
+  const int64_t r0 = seg[e] + (tile - tile_start[e]) * (16 * MT);
+  const int rows = seg[e + 1] - r0 < 16 * MT ? (int)(seg[e + 1] - r0) : 16 * MT;
+  const int l = threadIdx.x & 63, w = threadIdx.x >> 6, lr = l & 15, lg = l >> 4;
+  const int kb0 = blockIdx.y * RT;
+  const T *x[MT], *ar[RT];
+#pragma unroll
+  for (int t = 0; t < MT; ++t) x[t] = X + (r0 + (16 * t + lr < rows ? 16 * t + lr : rows - 1)) * K;
+#pragma unroll
+  for (int i = 0; i < RT; ++i) {
+    const int r = 16 * (kb0 + i) + lr;
+    ar[i] = A + ((int64_t)e * rank + (r < rank ? r : rank - 1)) * K;
+  }
+  floatx4 acc[RT][MT];
+#pragma unroll
+  for (int i = 0; i < RT; ++i)
+#pragma unroll
+    for (int t = 0; t < MT; ++t) acc[i][t] = floatx4{0.f, 0.f, 0.f, 0.f};
+  const int steps = (K + STEP - 1) / STEP, s0 = (int)((int64_t)steps * w / 4), s1 = (int)((int64_t)steps * (w + 1) / 4);
+#pragma unroll 4
+  for (int s = s0; s < s1; ++s) {
+    const int at = s * STEP + lg * N;
+    i32x4 xv[MT], av[RT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) xv[t] = at < K ? *reinterpret_cast<const i32x4*>(x[t] + at) : i32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < RT; ++i) av[i] = at < K ? *reinterpret_cast<const i32x4*>(ar[i] + at) : i32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+      for (int t = 0; t < MT; ++t) step_mfma<T>(av[i], xv[t], acc[i][t]);
+  }
+#pragma unroll
+  for (int i = 0; i < RT; ++i)
+#pragma unroll
+    for (int t = 0; t < MT; ++t) s_acc[w][i][t][l] = acc[i][t];
+  __syncthreads();
+  const float sc = scale ? scale[e] : 1.f;
+  for (int q = w; q < RT * MT; q += 4) {
+    const int i = q / MT, t = q % MT;
+    if (kb0 + i >= u_blocks(rank) || 16 * t + lr >= rows) continue;
+    const floatx4 v = (s_acc[0][i][t][l] + s_acc[1][i][t][l]) + (s_acc[2][i][t][l] + s_acc[3][i][t][l]);
+    u_store(U, r0 + 16 * t + lr, u_width<T>(rank), kb0 + i, lg, rank, v * sc);
+  }
+}
+
+// acc += U B_e^T over the adapters of this wave's rows, fragments straight from memory.
+template <class C>
+__device__ __forceinline__ void lora_extend(const TileCoord& tc, floatx4 (&acc)[C::MI][C::NJ],
+                                            const typename C::type* __restrict__ U, const typename C::type* __restrict__ B,
+                                            int rank, int cols, const int32_t* __restrict__ seg, int E) {
+  using T = typename C::type;
+  const Frag<C> f;
+  const int l = threadIdx.x & 63;
+  const int64_t lo = tc.m0 + f.wm * C::WM;
+  const int64_t hi = lo + C::WM < tc.m0 + tc.m_rows ? lo + C::WM : tc.m0 + tc.m_rows;
+  int e = -1;  // the last adapter whose rows start at or before lo
+  for (int b = 0; b < E; b += 64) e += __popcll(__ballot(b + l < E && seg[b + l < E ? b + l : 0] <= lo));
+  if (e < 0 || lo >= hi) return;
+  const int ldu = u_width<T>(rank), blocks = u_blocks(rank);
+  for (; e < E; ++e) {
+    const int64_t s = seg[e] > lo ? seg[e] : lo, t = seg[e + 1] < hi ? seg[e + 1] : hi;
+    if (seg[e] >= hi) break;
+    if (s >= t) continue;
+    const int i0 = (int)(s - lo) / 16, i1 = (int)(t - 1 - lo) / 16;
+    for (int kb = 0; kb < blocks; ++kb) {
+      i32x4 bv[C::NJ];
+#pragma unroll
+      for (int j = 0; j < C::NJ; ++j) {
+        const int col = f.block(j) + f.lr;
+        bv[j] = col < tc.n_cols ? r_frag(B + ((int64_t)e * cols + tc.n0 + col) * rank, kb, f.lg, rank) : i32x4{0, 0, 0, 0};
+      }
+#pragma unroll
+      for (int i = 0; i < C::MI; ++i) {
+        if (i < i0 || i > i1) continue;
+        const int64_t first = lo + 16 * i, row = first + f.lr;
+        i32x4 uv = {0, 0, 0, 0};
+        if (row >= s && row < t) uv = u_frag(U, row, ldu, kb, f.lg, rank);
+        const bool whole = first >= s && first + 16 <= t;
+#pragma unroll
+        for (int j = 0; j < C::NJ; ++j) {
+          // where rows of others share the fragment only the adapter's take the product: their zeros
+          // times an infinite B would not be zeros
+          floatx4 own = whole ? acc[i][j] : floatx4{0.f, 0.f, 0.f, 0.f};
+          if constexpr (C::TRANS) step_mfma<T>(bv[j], uv, own);
+          else step_mfma<T>(uv, bv[j], own);
+          if (whole) {
+            acc[i][j] = own;
+          } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int64_t at = C::TRANS ? row : first + 4 * f.lg + r;
+              acc[i][j][r] += at >= s && at < t ? own[r] : 0.f;
+            }
+          }
+        }
+      }
+    }
+  }
+}
+
+struct LoraRow {  // destination row
+  const int32_t* __restrict__ map;
+  int64_t m0;
+  __device__ __forceinline__ int64_t operator()(int r) const { return map ? map[m0 + r] : m0 + r; }
+};
+
+// out[map[m]] = A[m] W^T + bias + U[m] B_e^T.   W_KC: W [cols][Kd], otherwise [Kd][cols].
+template <class C, bool W_KC>
+__global__ void __launch_bounds__(C::THREADS)
+    k_lora_gemm(const typename C::type* __restrict__ A, const typename C::type* __restrict__ W,
+                const typename C::type* __restrict__ bias, const typename C::type* __restrict__ U,
+                const typename C::type* __restrict__ B, int rank, const int32_t* __restrict__ seg, int E, int64_t n,
+                int cols, int Kd, const int32_t* __restrict__ map, typename C::type* __restrict__ out) {
+  using T = typename C::type;
+  extern __shared__ __attribute__((aligned(16))) char smem_raw[];
+  lds<char>* smem = (lds<char>*)smem_raw;
+  const TileCoord tc = tile_plain<C>(n, cols, Kd);
+  if (!tc.valid) return;
+  floatx4 acc[C::MI][C::NJ];
+  gemm_tile<C, true, W_KC>(A + tc.m0 * Kd, Kd, tc.m_rows, W_KC ? W + (int64_t)tc.n0 * Kd : W + tc.n0, W_KC ? Kd : cols,
+                           tc.n_cols, Kd, smem, acc);
+  lora_extend<C>(tc, acc, U, B, rank, cols, seg, E);
+  using F = Frag<C>;
+  const F f;
+  float bv[F::NCOL];
+#pragma unroll
+  for (int q = 0; q < F::NCOL; ++q) {
+    const int col = f.colq(q);
+    bv[q] = (bias && col < tc.n_cols) ? to_f32(bias[tc.n0 + col]) : 0.f;
+  }
+  store_out<C, T>(tc, acc, smem, out, cols, [&](int, int j, int r, float v) { return v + bv[F::qidx(j, r)]; },
+                  LoraRow{map, tc.m0}, NoVec{});
+}
+
+// out [E][cols][rows] = in [E][rows][cols], 32 x 32 pieces through LDS; an adapter to a blockIdx.y.
+template <typename T>
+__global__ void __launch_bounds__(256) k_lora_transpose(const T* __restrict__ in, T* __restrict__ out, int rows, int cols) {
+  __shared__ T s[32][33];
+  const int64_t base = (int64_t)blockIdx.y * rows * cols;
+  const int across = (cols + 31) / 32;
+  const int c0 = blockIdx.x % across * 32, r0 = blockIdx.x / across * 32, x = threadIdx.x & 31, y = threadIdx.x >> 5;
+  for (int i = y; i < 32; i += 8)
+    if (r0 + i < rows && c0 + x < cols) s[i][x] = in[base + (int64_t)(r0 + i) * cols + c0 + x];
+  __syncthreads();
+  for (int i = y; i < 32; i += 8)
+    if (c0 + i < cols && r0 + x < rows) out[base + (int64_t)(c0 + i) * rows + r0 + x] = s[x][i];
+}
+
+// ------------------------------------------------------------------ gradients of the adapters
+
+// Rows of one adapter that a workgroup sums over; adapters with more have several pieces, joined
+// in order by k_lora_grad_join.
+constexpr int kLoraPiece = 1024;
+// Where such a piece's sums are kept: every adapter of more than kLoraPiece rows advances seg / kLoraPiece by
+// at least half of its pieces.
+__device__ __forceinline__ int64_t lora_piece_slot(int64_t seg_e, int64_t local) {
+  return 2 * (seg_e / kLoraPiece) + local;
+}
+
+// For one piece of adapter e's rows:  U_LEFT: out[c][m] = sum_rows U[c] D[m] (dA: [rank][width]),
+// otherwise out[m][c] = sum_rows D[m] U[c] (dB: [width][rank]).  D [n][width] with U or V as u_width says.
+template <typename T, bool U_LEFT>
+__global__ void __launch_bounds__(256) k_lora_grad(const T* __restrict__ D, int width, const T* __restrict__ U, int rank,
+                                                   const int32_t* __restrict__ seg,
+                                                   const int32_t* __restrict__ tile_start, int E,
+                                                   float* __restrict__ out, float* __restrict__ part) {
+  using C = CfgQuarter<T>;
+  extern __shared__ __attribute__((aligned(16))) char smem_raw[];
+  lds<char>* smem = (lds<char>*)smem_raw;
+  const int64_t piece = blockIdx.x;
+  if (piece >= tile_start[E]) return;
+  const int e = find_segment(tile_start, E, piece);
+  const int64_t local = piece - tile_start[e], p0 = seg[e] + local * kLoraPiece;
+  const int64_t len = seg[e + 1] - p0;
+  const int rows = (int)(len < kLoraPiece ? len : kLoraPiece);
+  const int ldu = u_width<T>(rank);
+  const int d0 = blockIdx.y * 64, u0 = blockIdx.z * 64;
+  const int dv = width - d0 < 64 ? width - d0 : 64, uv = ldu - u0 < 64 ? ldu - u0 : 64;
+  const T *pd = D + p0 * width + d0, *pu = U + p0 * ldu + u0;
+  floatx4 acc[C::MI][C::NJ];
+  if constexpr (U_LEFT) gemm_tile<C, false, false>(pu, ldu, uv, pd, width, dv, rows, smem, acc);
+  else gemm_tile<C, false, false>(pd, width, dv, pu, ldu, uv, rows, smem, acc);
+  const int64_t size = (int64_t)width * rank;
+  float* to = tile_start[e + 1] - tile_start[e] > 1 ? part + lora_piece_slot(seg[e], local) * size : out + e * size;
+  const Frag<C> f;
+  const auto put = [&](int c, int m, float v) {  // value c of the rank, column m of D
+    if (c < rank && m < width) to[U_LEFT ? (int64_t)c * width + m : (int64_t)m * rank + c] = v;
+  };
+#pragma unroll
+  for (int i = 0; i < C::MI; ++i)
+#pragma unroll
+    for (int j = 0; j < C::NJ; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        if constexpr (sizeof(T) == 2) {  // the sums with the values and with their remainders are one
+          if constexpr (U_LEFT) {
+            if (i == 0) put((u0 + 32 * f.wm) / 2 + 4 * f.lg + r, d0 + f.col(j, r), acc[0][j][r] + acc[1][j][r]);
+          } else {
+            if (j == 0) put((u0 + 32 * f.wn) / 2 + f.lr, d0 + f.row(i, r), acc[i][0][r] + acc[i][1][r]);
+          }
+        } else {
+          if constexpr (U_LEFT) put(u0 + f.row(i, r), d0 + f.col(j, r), acc[i][j][r]);
+          else put(u0 + f.col(j, r), d0 + f.row(i, r), acc[i][j][r]);
+        }
+      }
+}
+
+// The pieces of an adapter added in their order; adapters without rows get zeros.
+__global__ void __launch_bounds__(256) k_lora_grad_join(const float* __restrict__ part, const int32_t* __restrict__ seg,
+                                                        const int32_t* __restrict__ tile_start, int64_t size,
+                                                        float* __restrict__ out) {
+  const int e = blockIdx.y;
+  const int64_t pieces = tile_start[e + 1] - tile_start[e];
+  if (pieces == 1) return;
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (i >= size) return;
+  floatx4 s = {0.f, 0.f, 0.f, 0.f};
+  const float* p = part + lora_piece_slot(seg[e], 0) * size + i;
+  for (int64_t q = 0; q < pieces; ++q) s += *reinterpret_cast<const floatx4*>(p + q * size);
+  *reinterpret_cast<floatx4*>(out + e * size + i) = s;
+}
+
+struct LoraTables {
+  int32_t *shrink, *piece;  // E + 1: tiles of 32 rows, pieces of kLoraPiece
+};
+
+int lora_tables(const int32_t* offsets, int E, const LoraTables& t, hipStream_t st) {
+  return launch_seg_plan(offsets, E, SegPlan{{32, kLoraPiece, 0}, {t.shrink, t.piece, nullptr}, nullptr}, st);
+}
+
+template <typename T>
+int lora_shrink(const T* X, int K, const T* A, int rank, const float* scale, const int32_t* seg, const int32_t* tiles,
+                int E, int64_t n, T* U, hipStream_t st) {
+  const int blocks = u_blocks(rank);
+  const unsigned bound = (unsigned)(n / 32 + (E < n ? E : n));
+  if (blocks == 1)
+    HMOE_LAUNCH("lora shrink", (k_lora_shrink<T, 1>), dim3(bound), dim3(256), 0, st, X, K, A, rank, scale, seg, tiles, E, U);
+  else if (blocks == 2)
+    HMOE_LAUNCH("lora shrink", (k_lora_shrink<T, 2>), dim3(bound), dim3(256), 0, st, X, K, A, rank, scale, seg, tiles, E, U);
+  else
+    HMOE_LAUNCH("lora shrink", (k_lora_shrink<T, 4>), dim3(bound, (unsigned)cdiv(blocks, 4)), dim3(256), 0, st, X, K, A,
+                rank, scale, seg, tiles, E, U);
+  return HMOE_OK;
+}
+
+// Fewer of the type's tiles (gemm.hpp) than CUs: quarter tiles.
+template <typename T, bool W_KC>
+int lora_gemm(const T* A, const T* W, const T* bias, const T* U, const T* B, int rank, const int32_t* seg, int E,
+              int64_t n, int cols, int Kd, const int32_t* map, T* out, hipStream_t st) {
+  using C = typename std::conditional<W_KC, typename Pick<T>::C, typename Pick<T>::CK>::type;
+  using Q = CfgQuarter<T>;
+  const char* label = W_KC ? "lora forward" : "lora input gradient";
+  const int64_t tiles = cdiv(n, C::BM) * cdiv(cols, C::BN);
+  if (tiles < device_cus())
+    HMOE_LAUNCH(label, (k_lora_gemm<Q, W_KC>), dim3((unsigned)(cdiv(n, Q::BM) * cdiv(cols, Q::BN))), dim3(Q::THREADS),
+                Q::LDS, st, A, W, bias, U, B, rank, seg, E, n, cols, Kd, map, out);
+  else
+    HMOE_LAUNCH(label, (k_lora_gemm<C, W_KC>), dim3((unsigned)tiles), dim3(C::THREADS), C::LDS, st, A, W, bias, U, B, rank,
+                seg, E, n, cols, Kd, map, out);
+  return HMOE_OK;
+}
+
+template <typename T, bool U_LEFT>
+int lora_grad(const T* D, int width, const T* U, int rank, const int32_t* seg, const int32_t* pieces, int E, int64_t n,
+              float* out, float* part, hipStream_t st) {
+  using C = CfgQuarter<T>;
+  const char* label = U_LEFT ? "lora dA" : "lora dB";
+  const unsigned bound = (unsigned)(n / kLoraPiece + (E < n ? E : n));
+  HMOE_LAUNCH(label, (k_lora_grad<T, U_LEFT>),
+              dim3(bound, (unsigned)cdiv(width, 64), (unsigned)cdiv(u_width<T>(rank), 64)), dim3(256), C::LDS, st, D, width,
+              U, rank, seg, pieces, E, out, part);
+  const int64_t size = (int64_t)width * rank;
+  HMOE_LAUNCH("lora gradient join", k_lora_grad_join, dim3((unsigned)cdiv(size, 1024), (unsigned)E), dim3(256), 0, st,
+              part, seg, pieces, size, out);
+  return HMOE_OK;
+}
+
+struct LoraSpace {
+  LoraTables tables;
+  void *dYs, *Bt, *At, *V;
+  float* part;
+};
+
+LoraSpace lora_carve(const hmoe_lora_t* p, int64_t n, Workspace& ws) {
+  const size_t s = dtype_size(p->dt), ldu = p->dt == HMOE_BF16 ? u_width<bf16>(p->rank) : u_width<float>(p->rank);
+  LoraSpace x;
+  x.tables.shrink = ws.take<int32_t>(p->E + 1);
+  x.tables.piece = ws.take<int32_t>(p->E + 1);
+  x.dYs = ws.take<char>((size_t)n * p->d_out * s);
+  x.Bt = ws.take<char>((size_t)p->E * p->rank * p->d_out * s);
+  x.At = ws.take<char>((size_t)p->E * p->rank * p->d_in * s);
+  x.V = ws.take<char>((size_t)n * ldu * s);
+  const size_t wide = p->d_out > p->d_in ? p->d_out : p->d_in;
+  x.part = ws.take<float>(n > kLoraPiece ? (2 * (n / kLoraPiece) + 2) * wide * p->rank : 0);
+  return x;
+}
+
+template <typename T>
+int lora_forward_t(const hmoe_lora_t* p, int64_t n, const T* X, const int32_t* offsets, const int32_t* perm, T* U, T* Y,
+                   const LoraSpace& w, hipStream_t st) {
+  HMOE_TRY(lora_tables(offsets, p->E, w.tables, st));
+  HMOE_TRY(lora_shrink<T>(X, p->d_in, (const T*)p->A, p->rank, p->scale, offsets, w.tables.shrink, p->E, n, U, st));
+  return lora_gemm<T, true>(X, (const T*)p->W, (const T*)p->b, U, (const T*)p->B, p->rank, offsets, p->E, n, p->d_out,
+                               p->d_in, perm, Y, st);
+}
+
+template <typename T>
+int lora_transpose(const void* in, void* out, int E, int rows, int cols, hipStream_t st) {
+  HMOE_LAUNCH("lora transpose", k_lora_transpose<T>, dim3((unsigned)(cdiv(cols, 32) * cdiv(rows, 32)), (unsigned)E),
+              dim3(256), 0, st, (const T*)in, (T*)out, rows, cols);
+  return HMOE_OK;
+}
+
+template <typename T>
+int lora_backward_t(const hmoe_lora_t* p, int64_t n, const T* X, const int32_t* offsets, const int32_t* perm, const T* U,
+                    const T* dY, T* dX, float* dA, float* dB, const LoraSpace& w, hipStream_t st) {
+  HMOE_TRY(lora_tables(offsets, p->E, w.tables, st));
+  if (perm) {
+    HMOE_TRY(launch_permute(dY, w.dYs, perm, n, p->d_out, p->dt, st));
+    dY = (const T*)w.dYs;
+  }
+  if (dX || dA) {
+    HMOE_TRY(lora_transpose<T>(p->B, w.Bt, p->E, p->d_out, p->rank, st));
+    HMOE_TRY(lora_shrink<T>(dY, p->d_out, (const T*)w.Bt, p->rank, p->scale, offsets, w.tables.shrink, p->E, n, (T*)w.V, st));
+  }
+  if (dX) {
+    HMOE_TRY(lora_transpose<T>(p->A, w.At, p->E, p->rank, p->d_in, st));
+    HMOE_TRY(lora_gemm<T, false>(dY, (const T*)p->W, nullptr, (const T*)w.V, (const T*)w.At, p->rank, offsets, p->E, n,
+                                    p->d_in, p->d_out, perm, dX, st));
+  }
+  if (dB)
+    HMOE_TRY(lora_grad<T, false>(dY, p->d_out, U, p->rank, offsets, w.tables.piece, p->E, n, dB, w.part, st));
+  if (dA)
+    HMOE_TRY(lora_grad<T, true>(X, p->d_in, (const T*)w.V, p->rank, offsets, w.tables.piece, p->E, n, dA, w.part, st));
+  return HMOE_OK;
+}
+
+}  // namespace
+
+int lora_saved_width(int rank, hmoe_dtype_t dt) { return dt == HMOE_BF16 ? u_width<bf16>(rank) : u_width<float>(rank); }
+
+size_t lora_few_ws(const hmoe_lora_t* p, int64_t n) {
+  Workspace w(nullptr, 0);
+  w.take<char>((size_t)n * lora_saved_width(p->rank, p->dt) * dtype_size(p->dt));
+  return w.off;
+}
+
+size_t lora_ws(const hmoe_lora_t* p, int64_t n) {
+  Workspace w(nullptr, 0);
+  lora_carve(p, n, w);
+  return w.off;
+}
+
+int launch_lora_few(const hmoe_lora_t* p, int64_t n, const void* X, const int32_t* adapter, void* Y, Workspace& ws,
+                    hipStream_t st) {
+  LoraFew a = {X, p->W, p->b, p->A, p->B, p->scale, adapter, (int)n, p->E, p->d_in, p->d_out, p->rank, nullptr, Y};
+  a.U = ws.take<char>((size_t)n * lora_saved_width(p->rank, p->dt) * dtype_size(p->dt));
+  return p->dt == HMOE_BF16 ? lora_few_t<bf16>(a, st) : lora_few_t<float>(a, st);
+}
+
+int launch_lora_forward(const hmoe_lora_t* p, int64_t n, const void* X, const int32_t* offsets, const int32_t* perm,
+                        void* U, void* Y, Workspace& ws, hipStream_t st) {
+  const LoraSpace w = lora_carve(p, n, ws);
+  if (p->dt == HMOE_BF16)
+    return lora_forward_t<bf16>(p, n, (const bf16*)X, offsets, perm, (bf16*)U, (bf16*)Y, w, st);
+  return lora_forward_t<float>(p, n, (const float*)X, offsets, perm, (float*)U, (float*)Y, w, st);
+}
+
+int launch_lora_backward(const hmoe_lora_t* p, int64_t n, const void* X, const int32_t* offsets, const int32_t* perm,
+                         const void* U, const void* dY, void* dX, float* dA, float* dB, Workspace& ws, hipStream_t st) {
+  const LoraSpace w = lora_carve(p, n, ws);
+  if (p->dt == HMOE_BF16)
+    return lora_backward_t<bf16>(p, n, (const bf16*)X, offsets, perm, (const bf16*)U, (const bf16*)dY, (bf16*)dX, dA, dB,
+                                 w, st);
+  return lora_backward_t<float>(p, n, (const float*)X, offsets, perm, (const float*)U, (const float*)dY, (float*)dX, dA,
+                                dB, w, st);
+}
+
+}  // namespace hmoe

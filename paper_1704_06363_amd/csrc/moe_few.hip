@@ -2,7 +2,6 @@
 #include <float.h>
 
 #include "fewrows.hpp"
-#include "lanes.hpp"
 #include "lm_launch.hpp"
 
 namespace hmoe {
@@ -63,55 +62,6 @@ __global__ void __launch_bounds__(256) k_few_route(FewArgs a) {
 
 // ------------------------------------------------------------------ experts
 
-constexpr int kFewMost = 64;  // samples
-
-// The slot-th of the experts that have samples, in ascending order, and its rows (q = sample k + choice) in
-// ascending order.  False if there are not that many.
-__device__ __forceinline__ bool few_group(const int32_t* __restrict__ chosen, int total, int slot, int* s_expert,
-                                          int* s_rows, int* s_count) {
-  __shared__ uint32_t mask[128];
-  const int t = threadIdx.x;
-  if (t < 128) mask[t] = 0;
-  if (t == 0) *s_expert = -1;
-  __syncthreads();
-  for (int q = t; q < total; q += 256) {
-    const int e = chosen[q];
-    if (e >= 0) atomicOr(&mask[e >> 5], 1u << (e & 31));
-  }
-  __syncthreads();
-  if (t < 64) {
-    const uint32_t m0 = mask[2 * t], m1 = mask[2 * t + 1];
-    const int c = __popc(m0) + __popc(m1);
-    int inc = c;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int v = __shfl_up(inc, o, 64);
-      if (t >= o) inc += v;
-    }
-    const int before = inc - c;
-    if (slot >= before && slot < inc) {
-      uint64_t both = ((uint64_t)m1 << 32) | m0;
-      for (int i = slot - before; i > 0; --i) both &= both - 1;
-      *s_expert = 64 * t + __builtin_ctzll(both);
-    }
-  }
-  __syncthreads();
-  const int e = *s_expert;
-  if (e < 0) return false;
-  if (t < 64) {
-    int count = 0;
-    for (int b = 0; b < total; b += 64) {
-      const bool mine = b + t < total && chosen[b + t] == e;
-      const uint64_t hit = __ballot(mine);
-      if (mine) s_rows[count + lanes_below(hit)] = b + t;
-      count += __popcll(hit);
-    }
-    if (t == 0) *s_count = count;
-  }
-  __syncthreads();
-  return true;
-}
-
 // LAYER 1: hid[q] = act(W1_e x + b1_e).   LAYER 2: part[split][q] = W2_e hid[q] over a split of the reduction.
 // A workgroup has 16 outputs (GATED: and the 16 they are gated with) of one expert; its four waves split
 // the reduction and join in LDS.
@@ -120,12 +70,12 @@ __global__ void __launch_bounds__(256) k_few_layer(FewArgs a, int tiles) {
   constexpr int N = 16 / sizeof(T), STEP = 4 * N;
   constexpr int MI = LAYER == 1 && GATED ? 2 : 1;
   constexpr int NX = LAYER == 2 ? Halves<T>::N : 1;  // operands of an activation
-  __shared__ int s_expert, s_count, s_rows[kFewMost];
+  __shared__ int s_expert, s_count, s_rows[HMOE_FEW_ROWS];
   __shared__ floatx4 s_acc[4][MI][64];
   const int splits = LAYER == 1 ? 1 : a.splits;
   const int slot = blockIdx.x / (tiles * splits);
   const int tile = blockIdx.x % tiles, split = blockIdx.x / tiles % splits;
-  if (!few_group(a.chosen, a.n * a.k, slot, &s_expert, s_rows, &s_count)) return;
+  if (!few_group<256>(a.chosen, a.n * a.k, a.K, slot, &s_expert, s_rows, &s_count)) return;
   const int e = s_expert, count = s_count;
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6, lr = l & 15, lg = l >> 4;
   const int kd = LAYER == 1 ? a.d : a.h, rows = LAYER == 1 ? a.h : a.o;

@@ -35,6 +35,8 @@ SYMBOLS = (
 LM_SYMBOLS = (
     "hmoe_token_logprob_workspace", "hmoe_token_logprob", "hmoe_token_logprob_backward",
     "hmoe_moe_few_workspace", "hmoe_moe_few",
+    "hmoe_lora_few_workspace", "hmoe_lora_few", "hmoe_lora_saved_width", "hmoe_lora_workspace", "hmoe_lora_forward",
+    "hmoe_lora_backward",
 )
 
 
@@ -55,6 +57,12 @@ class FewParams(ctypes.Structure):
                 ("d_out", ctypes.c_int32), ("top_k", ctypes.c_int32), ("dt", ctypes.c_int), ("act", ctypes.c_int32),
                 ("R", ctypes.c_void_p), ("r_bias", ctypes.c_void_p), ("W1", ctypes.c_void_p),
                 ("b1", ctypes.c_void_p), ("W2", ctypes.c_void_p), ("b2", ctypes.c_void_p)]
+
+
+class Lora(ctypes.Structure):
+    _fields_ = [("E", ctypes.c_int32), ("d_in", ctypes.c_int32), ("d_out", ctypes.c_int32), ("rank", ctypes.c_int32),
+                ("dt", ctypes.c_int), ("W", ctypes.c_void_p), ("b", ctypes.c_void_p), ("A", ctypes.c_void_p),
+                ("B", ctypes.c_void_p), ("scale", ctypes.c_void_p)]
 
 
 class Labels(ctypes.Structure):
@@ -119,7 +127,16 @@ def lib():
         L.hmoe_moe_few_workspace.restype = _SZ
         L.hmoe_moe_few_workspace.argtypes = [_c.POINTER(FewParams), _I64]
         L.hmoe_moe_few.argtypes = [_c.POINTER(FewParams), _I64, _P, _P, _P, _P, _P, _SZ, _P]
-        for name in ("hmoe_token_logprob", "hmoe_token_logprob_backward", "hmoe_moe_few"):
+        for name in ("hmoe_lora_few_workspace", "hmoe_lora_workspace"):
+            getattr(L, name).restype = _SZ
+            getattr(L, name).argtypes = [_c.POINTER(Lora), _I64]
+        L.hmoe_lora_saved_width.restype = _I32
+        L.hmoe_lora_saved_width.argtypes = [_I32, _c.c_int]
+        L.hmoe_lora_few.argtypes = [_c.POINTER(Lora), _I64, _P, _P, _P, _P, _SZ, _P]
+        L.hmoe_lora_forward.argtypes = [_c.POINTER(Lora), _I64, _P, _P, _P, _P, _P, _P, _SZ, _P]
+        L.hmoe_lora_backward.argtypes = [_c.POINTER(Lora), _I64, _P, _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P]
+        for name in ("hmoe_token_logprob", "hmoe_token_logprob_backward", "hmoe_moe_few", "hmoe_lora_few",
+                     "hmoe_lora_forward", "hmoe_lora_backward"):
             getattr(L, name).restype = _c.c_int
         for name in ("hmoe_kmeans_assign", "hmoe_kmeans_fit", "hmoe_kmeans_update",
                      "hmoe_moe_dispatch", "hmoe_moe_dispatch_noalloc", "hmoe_permute_rows", "hmoe_moe_forward",
@@ -655,6 +672,101 @@ def moe_few(p, X, top_k: int = 1, act: str = "relu", out=None, ws=None):
     w, wb = _workspace(lib().hmoe_moe_few_workspace(ctypes.byref(prm), n), ws, dev)
     _chk(lib().hmoe_moe_few(ctypes.byref(prm), n, _ptr(X), _ptr(r["expert"]), _ptr(r["weight"]), _ptr(r["Y"]), _ptr(w),
                             wb, _stream()), "moe_few")
+    return r
+
+
+# ------------------------------------------------------------------ low-rank adapters
+
+def make_lora(p: dict) -> Lora:
+    """p: the shared W [o, d] with b [o] or None, the adapters A [E, r, d], B [E, o, r], and scale [E] (fp32) or
+    None."""
+    E, r, d = p["A"].shape
+    o = p["W"].shape[0]
+    dt = p["W"].dtype
+    for k, shape, t in (("W", (o, d), dt), ("b", (o,), dt), ("A", (E, r, d), dt), ("B", (E, o, r), dt),
+                        ("scale", (E,), torch.float32)):
+        _expect(p.get(k), shape, t, k)
+    return Lora(E, d, o, r, _dt(p["W"]), _ptr(p["W"]), _ptr(p.get("b")), _ptr(p["A"]), _ptr(p["B"]), _ptr(p.get("scale")))
+
+
+def _lora(p, X):
+    prm = p if isinstance(p, Lora) else make_lora(p)
+    if _dt(X) != prm.dt:
+        raise HmoeError(f"X: dtype {X.dtype}, the parameters' expected")
+    _expect(X, (None, prm.d_in), None, "X")
+    return prm
+
+
+def lora_few_workspace(p, n) -> int:
+    return lib().hmoe_lora_few_workspace(ctypes.byref(p if isinstance(p, Lora) else make_lora(p)), n)
+
+
+def lora_workspace(p, n) -> int:
+    """Of lora_forward and lora_backward."""
+    return lib().hmoe_lora_workspace(ctypes.byref(p if isinstance(p, Lora) else make_lora(p)), n)
+
+
+def lora_saved_shape(p, n):
+    """Shape of lora_forward's U, in the data type."""
+    prm = p if isinstance(p, Lora) else make_lora(p)
+    return (n, lib().hmoe_lora_saved_width(prm.rank, prm.dt))
+
+
+def lora_few(p, X, adapter, out=None, ws=None):
+    """W x + b + scale B_a (A_a x) for up to FEW_ROWS rows X [n, d] of any mix of adapters: adapter int32 [n], an
+    id outside [0, E) for none.  p: a dict as in make_lora, or the Lora made from one.  Returns Y [n, o]."""
+    prm = _lora(p, X)
+    n = X.shape[0]
+    _expect(adapter, (n,), torch.int32, "adapter")
+    if out is None:
+        out = torch.empty((n, prm.d_out), dtype=X.dtype, device=X.device)
+    _expect(out, (n, prm.d_out), X.dtype, "out")
+    w, wb = _workspace(lib().hmoe_lora_few_workspace(ctypes.byref(prm), n), ws, X.device)
+    _chk(lib().hmoe_lora_few(ctypes.byref(prm), n, _ptr(X), _ptr(adapter), _ptr(out), _ptr(w), wb, _stream()), "lora_few")
+    return out
+
+
+def lora_forward(p, X_sorted, offsets, perm=None, out=None, ws=None):
+    """The same for many rows in adapter order (moe_dispatch of their adapters, whose ids outside [0, E) come
+    last, without one): offsets int32 [E + 1], perm int32 [n] (slot -> sample) or None (Y in slot order too).
+    Returns Y [n, o] in sample order and U, which lora_backward needs."""
+    prm = _lora(p, X_sorted)
+    n = X_sorted.shape[0]
+    o = out or {}
+    dt = X_sorted.dtype
+    _expect(offsets, (prm.E + 1,), torch.int32, "offsets")
+    _expect(perm, (n,), torch.int32, "perm")
+    r = {}
+    for k, shape in (("Y", (n, prm.d_out)), ("U", (n, lib().hmoe_lora_saved_width(prm.rank, prm.dt)))):
+        r[k] = o[k] if k in o else torch.empty(shape, dtype=dt, device=X_sorted.device)
+        _expect(r[k], shape, dt, k)
+    w, wb = _workspace(lib().hmoe_lora_workspace(ctypes.byref(prm), n), ws, X_sorted.device)
+    _chk(lib().hmoe_lora_forward(ctypes.byref(prm), n, _ptr(X_sorted), _ptr(offsets), _ptr(perm), _ptr(r["U"]),
+                                 _ptr(r["Y"]), _ptr(w), wb, _stream()), "lora_forward")
+    return r
+
+
+def lora_backward(p, X_sorted, offsets, dY, U, perm=None, want_dX=True, want_adapters=True, out=None, ws=None):
+    """Gradients of the adapters, dA [E, r, d] and dB [E, o, r] (fp32), and of the input, dX [n, d] in sample
+    order, from dY [n, o] in sample order and the forward's U.  W, b and scale are fixed."""
+    prm = _lora(p, X_sorted)
+    n = X_sorted.shape[0]
+    o = out or {}
+    dt, dev, f32 = X_sorted.dtype, X_sorted.device, torch.float32
+    _expect(offsets, (prm.E + 1,), torch.int32, "offsets")
+    _expect(perm, (n,), torch.int32, "perm")
+    _expect(dY, (n, prm.d_out), dt, "dY")
+    _expect(U, (n, lib().hmoe_lora_saved_width(prm.rank, prm.dt)), dt, "U")
+    r = {}
+    for k, want, shape, t in (("dX", want_dX, (n, prm.d_in), dt), ("dA", want_adapters, (prm.E, prm.rank, prm.d_in), f32),
+                              ("dB", want_adapters, (prm.E, prm.d_out, prm.rank), f32)):
+        r[k] = None
+        if want:
+            r[k] = o[k] if k in o else torch.empty(shape, dtype=t, device=dev)
+            _expect(r[k], shape, t, k)
+    w, wb = _workspace(lib().hmoe_lora_workspace(ctypes.byref(prm), n), ws, dev)
+    _chk(lib().hmoe_lora_backward(ctypes.byref(prm), n, _ptr(X_sorted), _ptr(offsets), _ptr(perm), _ptr(U), _ptr(dY),
+                                  _ptr(r["dX"]), _ptr(r["dA"]), _ptr(r["dB"]), _ptr(w), wb, _stream()), "lora_backward")
     return r
 
 

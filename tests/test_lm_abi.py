@@ -131,3 +131,61 @@ def test_moe_few_binding_refusals():
         hmoe.make_few_params(dict(p, R=torch.zeros(4, 16, dtype=b)))
     with pytest.raises(hmoe.HmoeError, match="GPU"):
         hmoe.make_few_params(p)
+
+
+def test_lora_refusals(lib):
+    ok = dict(E=8, d_in=64, d_out=128, rank=16, dt=1, W=16, b=None, A=16, B=16, scale=None)
+
+    def prm(**kw):
+        return hmoe.Lora(*dict(ok, **kw).values())
+
+    def few(n=4, X=16, adapter=16, Y=16, **kw):
+        return lib.hmoe_lora_few(ctypes.byref(prm(**kw)), n, X, adapter, Y, None, 0, None)
+
+    def fwd(n=400, X=16, offsets=16, U=16, Y=16, **kw):
+        return lib.hmoe_lora_forward(ctypes.byref(prm(**kw)), n, X, offsets, None, U, Y, None, 0, None)
+
+    def bwd(n=400, X=16, offsets=16, U=16, dY=16, dX=16, dA=16, dB=16, **kw):
+        return lib.hmoe_lora_backward(ctypes.byref(prm(**kw)), n, X, offsets, None, U, dY, dX, dA, dB, None, 0, None)
+    for call in (few, fwd, bwd):
+        refused(call(dt=3), -2, "dtype")
+        refused(call(E=0), -1, "E = 0")
+        refused(call(E=4097), -1, "E = 4097")
+        refused(call(d_in=4), -3, "d_in")
+        refused(call(d_out=0), -3, "d_out")
+        refused(call(rank=12), -3, "rank")
+        refused(call(rank=136), -1, "rank")
+        refused(call(d_in=(1 << 21) + 8), -1, "exceeds")
+        refused(call(n=-1), -1, "n =")
+        refused(call(W=None), -1, "W")
+        refused(call(A=24), -3, "A")
+        refused(call(B=None), -1, "B")
+        refused(call(X=None), -1, "X")
+        refused(call(), -4, "workspace")
+    assert lib.hmoe_lora_few(None, 1, 16, 16, 16, None, 0, None) == -1
+    refused(few(n=65), -1, "n = 65")
+    refused(few(adapter=None), -1, "adapter")
+    refused(few(Y=8), -3, "Y")
+    refused(fwd(n=(1 << 28) + 1), -1, "n =")
+    refused(fwd(offsets=None), -1, "offsets")
+    refused(fwd(U=None), -1, "U")
+    refused(bwd(U=None), -1, "U")
+    refused(bwd(dY=None), -1, "dY")
+    refused(bwd(dX=8), -3, "dX")
+    refused(bwd(dA=8), -3, "dA")
+    assert few(n=0, X=None) == 0 and fwd(n=0, X=None) == 0
+    assert lib.hmoe_lora_saved_width(24, 1) == 64 and lib.hmoe_lora_saved_width(24, 0) == 24
+
+
+def test_lora_binding_refusals():
+    b = torch.bfloat16
+    p = {"W": torch.zeros(24, 16, dtype=b), "b": None, "A": torch.zeros(3, 8, 16, dtype=b),
+         "B": torch.zeros(3, 24, 8, dtype=b), "scale": None}
+    with pytest.raises(hmoe.HmoeError, match="B: shape"):
+        hmoe.make_lora(dict(p, B=torch.zeros(3, 24, 16, dtype=b)))
+    with pytest.raises(hmoe.HmoeError, match="A: dtype"):
+        hmoe.make_lora(dict(p, A=torch.zeros(3, 8, 16)))
+    with pytest.raises(hmoe.HmoeError, match="scale: dtype"):
+        hmoe.make_lora(dict(p, scale=torch.zeros(3, dtype=b)))
+    with pytest.raises(hmoe.HmoeError, match="GPU"):
+        hmoe.make_lora(p)
