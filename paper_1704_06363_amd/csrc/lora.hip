@@ -55,6 +55,35 @@ __device__ __forceinline__ void u_store(T* __restrict__ U, int64_t row, int ldu,
   }
 }
 
+// The index-th of the runs of at most `height` rows that segments 0 .. G - 1 are cut into: its segment and its
+// number in it, false past the last.  Found by each wave for itself: a lane counts the runs of an equal
+// share of the segments, a scan over the lanes names the share and a second one the segment -- two trips to
+// memory for up to 64 segments a lane (a binary search in a table takes one for each halving, 3 us of
+// them for 128 segments, and a launch before it for the table).  Entered by whole waves.
+struct Run {
+  int segment;
+  int64_t local;
+};
+__device__ __forceinline__ bool find_run(const int32_t* __restrict__ seg, int G, int height, int64_t index, Run& run) {
+  const int l = threadIdx.x & 63, per = (G + 63) / 64;
+  const auto runs = [&](int e) { return e < G ? (int64_t)((seg[e + 1] - seg[e] + height - 1) / height) : (int64_t)0; };
+  int64_t mine = 0;
+#pragma unroll 8
+  for (int i = 0; i < per; ++i) mine += runs(l * per + i);
+  int64_t end = wave_incl_scan(mine);
+  uint64_t past = __ballot(end > index);
+  if (past == 0) return false;
+  int at = __builtin_ctzll(past);
+  const int first = at * per;
+  const int64_t before = lane_value((uint64_t)(end - mine), at);
+  mine = l < per ? runs(first + l) : 0;
+  end = before + wave_incl_scan(mine);
+  at = __builtin_ctzll(__ballot(end > index));
+  run.segment = first + at;
+  run.local = index - (int64_t)lane_value((uint64_t)(end - mine), at);
+  return true;
+}
+
 // ------------------------------------------------------------------ few rows
 
 struct LoraFew {
@@ -226,13 +255,13 @@ int lora_few_t(const LoraFew& a, hipStream_t st) {
 template <typename T, int RT>
 __global__ void __launch_bounds__(256) k_lora_shrink(const T* __restrict__ X, int K, const T* __restrict__ A, int rank,
                                                      const float* __restrict__ scale, const int32_t* __restrict__ seg,
-                                                     const int32_t* __restrict__ tile_start, int E, T* __restrict__ U) {
+                                                     int E, T* __restrict__ U) {
   constexpr int N = 16 / sizeof(T), STEP = 4 * N, MT = 2;
   __shared__ floatx4 s_acc[4][RT][MT][64];
-  const int64_t tile = blockIdx.x;
-  if (tile >= tile_start[E]) return;
-  const int e = find_segment(tile_start, E, tile);
-  const int64_t r0 = seg[e] + (tile - tile_start[e]) * (16 * MT);
+  Run run;
+  if (!find_run(seg, E, 16 * MT, blockIdx.x, run)) return;
+  const int e = run.segment;
+  const int64_t r0 = seg[e] + run.local * (16 * MT);
   const int rows = seg[e + 1] - r0 < 16 * MT ? (int)(seg[e + 1] - r0) : 16 * MT;
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6, lr = l & 15, lg = l >> 4;
   const int kb0 = blockIdx.y * RT;
@@ -366,18 +395,42 @@ __global__ void __launch_bounds__(C::THREADS)
                   LoraRow{map, tc.m0}, NoVec{});
 }
 
-// out [E][cols][rows] = in [E][rows][cols], 32 x 32 pieces through LDS; an adapter to a blockIdx.y.
-template <typename T>
-__global__ void __launch_bounds__(256) k_lora_transpose(const T* __restrict__ in, T* __restrict__ out, int rows, int cols) {
-  __shared__ T s[32][33];
-  const int64_t base = (int64_t)blockIdx.y * rows * cols;
-  const int across = (cols + 31) / 32;
-  const int c0 = blockIdx.x % across * 32, r0 = blockIdx.x / across * 32, x = threadIdx.x & 31, y = threadIdx.x >> 5;
-  for (int i = y; i < 32; i += 8)
-    if (r0 + i < rows && c0 + x < cols) s[i][x] = in[base + (int64_t)(r0 + i) * cols + c0 + x];
+// out [E][cols][rows] = in [E][rows][cols] for the adapters that have rows, one to a blockIdx.y.  The short
+// side is the rank: a workgroup takes all of it (16-byte vectors, 128 at most) and 64 of the long side.
+// TALL: rows is the long side.
+template <typename T, bool TALL>
+__global__ void __launch_bounds__(256) k_lora_transpose(const T* __restrict__ in, T* __restrict__ out, int rows, int cols,
+                                                        const int32_t* __restrict__ seg) {
+  constexpr int N = 16 / sizeof(T);
+  __shared__ T s[64 * (HMOE_LORA_RANK + 1)];  // [long][short], odd rows of it
+  const int e = blockIdx.y;
+  if (seg[e] == seg[e + 1]) return;
+  const int rank = TALL ? cols : rows, size = TALL ? rows : cols;
+  const int p0 = blockIdx.x * 64, valid = size - p0 < 64 ? size - p0 : 64, ld = rank + 1;
+  const int64_t base = (int64_t)e * rows * cols;
+  const auto walk = [&](const bool tall, auto body) {  // vectors along the rank, or along the long side
+    const int vecs = tall ? rank / N : valid / N, lines = tall ? valid : rank;
+    for (int q = threadIdx.x; q < vecs * lines; q += 256) {
+      const int line = q / vecs, v = (q - line * vecs) * N;
+      const int64_t at = tall ? (int64_t)(p0 + line) * rank + v : (int64_t)line * size + p0 + v;
+      const int first = tall ? line * ld + v : v * ld + line, step = tall ? 1 : ld;
+      body(base + at, first, step);
+    }
+  };
+  walk(TALL, [&](int64_t at, int first, int step) {
+    const i32x4 v = *reinterpret_cast<const i32x4*>(in + at);
+    const T* x = reinterpret_cast<const T*>(&v);
+#pragma unroll
+    for (int z = 0; z < N; ++z) s[first + z * step] = x[z];
+  });
   __syncthreads();
-  for (int i = y; i < 32; i += 8)
-    if (c0 + i < cols && r0 + x < rows) out[base + (int64_t)(c0 + i) * rows + r0 + x] = s[x][i];
+  walk(!TALL, [&](int64_t at, int first, int step) {
+    i32x4 v;
+    T* x = reinterpret_cast<T*>(&v);
+#pragma unroll
+    for (int z = 0; z < N; ++z) x[z] = s[first + z * step];
+    *reinterpret_cast<i32x4*>(out + at) = v;
+  });
 }
 
 // ------------------------------------------------------------------ gradients of the adapters
@@ -395,16 +448,15 @@ __device__ __forceinline__ int64_t lora_piece_slot(int64_t seg_e, int64_t local)
 // otherwise out[m][c] = sum_rows D[m] U[c] (dB: [width][rank]).  D [n][width] with U or V as u_width says.
 template <typename T, bool U_LEFT>
 __global__ void __launch_bounds__(256) k_lora_grad(const T* __restrict__ D, int width, const T* __restrict__ U, int rank,
-                                                   const int32_t* __restrict__ seg,
-                                                   const int32_t* __restrict__ tile_start, int E,
+                                                   const int32_t* __restrict__ seg, int E,
                                                    float* __restrict__ out, float* __restrict__ part) {
   using C = CfgQuarter<T>;
   extern __shared__ __attribute__((aligned(16))) char smem_raw[];
   lds<char>* smem = (lds<char>*)smem_raw;
-  const int64_t piece = blockIdx.x;
-  if (piece >= tile_start[E]) return;
-  const int e = find_segment(tile_start, E, piece);
-  const int64_t local = piece - tile_start[e], p0 = seg[e] + local * kLoraPiece;
+  Run run;
+  if (!find_run(seg, E, kLoraPiece, blockIdx.x, run)) return;
+  const int e = run.segment;
+  const int64_t local = run.local, p0 = seg[e] + local * kLoraPiece;
   const int64_t len = seg[e + 1] - p0;
   const int rows = (int)(len < kLoraPiece ? len : kLoraPiece);
   const int ldu = u_width<T>(rank);
@@ -415,7 +467,7 @@ __global__ void __launch_bounds__(256) k_lora_grad(const T* __restrict__ D, int 
   if constexpr (U_LEFT) gemm_tile<C, false, false>(pu, ldu, uv, pd, width, dv, rows, smem, acc);
   else gemm_tile<C, false, false>(pd, width, dv, pu, ldu, uv, rows, smem, acc);
   const int64_t size = (int64_t)width * rank;
-  float* to = tile_start[e + 1] - tile_start[e] > 1 ? part + lora_piece_slot(seg[e], local) * size : out + e * size;
+  float* to = seg[e + 1] - seg[e] > kLoraPiece ? part + lora_piece_slot(seg[e], local) * size : out + e * size;
   const Frag<C> f;
   const auto put = [&](int c, int m, float v) {  // value c of the rank, column m of D
     if (c < rank && m < width) to[U_LEFT ? (int64_t)c * width + m : (int64_t)m * rank + c] = v;
@@ -441,10 +493,9 @@ __global__ void __launch_bounds__(256) k_lora_grad(const T* __restrict__ D, int 
 
 // The pieces of an adapter added in their order; adapters without rows get zeros.
 __global__ void __launch_bounds__(256) k_lora_grad_join(const float* __restrict__ part, const int32_t* __restrict__ seg,
-                                                        const int32_t* __restrict__ tile_start, int64_t size,
-                                                        float* __restrict__ out) {
+                                                        int64_t size, float* __restrict__ out) {
   const int e = blockIdx.y;
-  const int64_t pieces = tile_start[e + 1] - tile_start[e];
+  const int64_t pieces = cdiv(seg[e + 1] - seg[e], kLoraPiece);
   if (pieces == 1) return;
   const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
   if (i >= size) return;
@@ -454,26 +505,18 @@ __global__ void __launch_bounds__(256) k_lora_grad_join(const float* __restrict_
   *reinterpret_cast<floatx4*>(out + e * size + i) = s;
 }
 
-struct LoraTables {
-  int32_t *shrink, *piece;  // E + 1: tiles of 32 rows, pieces of kLoraPiece
-};
-
-int lora_tables(const int32_t* offsets, int E, const LoraTables& t, hipStream_t st) {
-  return launch_seg_plan(offsets, E, SegPlan{{32, kLoraPiece, 0}, {t.shrink, t.piece, nullptr}, nullptr}, st);
-}
-
 template <typename T>
-int lora_shrink(const T* X, int K, const T* A, int rank, const float* scale, const int32_t* seg, const int32_t* tiles,
-                int E, int64_t n, T* U, hipStream_t st) {
+int lora_shrink(const T* X, int K, const T* A, int rank, const float* scale, const int32_t* seg, int E,
+                int64_t n, T* U, hipStream_t st) {
   const int blocks = u_blocks(rank);
   const unsigned bound = (unsigned)(n / 32 + (E < n ? E : n));
   if (blocks == 1)
-    HMOE_LAUNCH("lora shrink", (k_lora_shrink<T, 1>), dim3(bound), dim3(256), 0, st, X, K, A, rank, scale, seg, tiles, E, U);
+    HMOE_LAUNCH("lora shrink", (k_lora_shrink<T, 1>), dim3(bound), dim3(256), 0, st, X, K, A, rank, scale, seg, E, U);
   else if (blocks == 2)
-    HMOE_LAUNCH("lora shrink", (k_lora_shrink<T, 2>), dim3(bound), dim3(256), 0, st, X, K, A, rank, scale, seg, tiles, E, U);
+    HMOE_LAUNCH("lora shrink", (k_lora_shrink<T, 2>), dim3(bound), dim3(256), 0, st, X, K, A, rank, scale, seg, E, U);
   else
     HMOE_LAUNCH("lora shrink", (k_lora_shrink<T, 4>), dim3(bound, (unsigned)cdiv(blocks, 4)), dim3(256), 0, st, X, K, A,
-                rank, scale, seg, tiles, E, U);
+                rank, scale, seg, E, U);
   return HMOE_OK;
 }
 
@@ -495,22 +538,21 @@ int lora_gemm(const T* A, const T* W, const T* bias, const T* U, const T* B, int
 }
 
 template <typename T, bool U_LEFT>
-int lora_grad(const T* D, int width, const T* U, int rank, const int32_t* seg, const int32_t* pieces, int E, int64_t n,
+int lora_grad(const T* D, int width, const T* U, int rank, const int32_t* seg, int E, int64_t n,
               float* out, float* part, hipStream_t st) {
   using C = CfgQuarter<T>;
   const char* label = U_LEFT ? "lora dA" : "lora dB";
   const unsigned bound = (unsigned)(n / kLoraPiece + (E < n ? E : n));
   HMOE_LAUNCH(label, (k_lora_grad<T, U_LEFT>),
               dim3(bound, (unsigned)cdiv(width, 64), (unsigned)cdiv(u_width<T>(rank), 64)), dim3(256), C::LDS, st, D, width,
-              U, rank, seg, pieces, E, out, part);
+              U, rank, seg, E, out, part);
   const int64_t size = (int64_t)width * rank;
   HMOE_LAUNCH("lora gradient join", k_lora_grad_join, dim3((unsigned)cdiv(size, 1024), (unsigned)E), dim3(256), 0, st,
-              part, seg, pieces, size, out);
+              part, seg, size, out);
   return HMOE_OK;
 }
 
 struct LoraSpace {
-  LoraTables tables;
   void *dYs, *Bt, *At, *V;
   float* part;
 };
@@ -518,8 +560,6 @@ struct LoraSpace {
 LoraSpace lora_carve(const hmoe_lora_t* p, int64_t n, Workspace& ws) {
   const size_t s = dtype_size(p->dt), ldu = p->dt == HMOE_BF16 ? u_width<bf16>(p->rank) : u_width<float>(p->rank);
   LoraSpace x;
-  x.tables.shrink = ws.take<int32_t>(p->E + 1);
-  x.tables.piece = ws.take<int32_t>(p->E + 1);
   x.dYs = ws.take<char>((size_t)n * p->d_out * s);
   x.Bt = ws.take<char>((size_t)p->E * p->rank * p->d_out * s);
   x.At = ws.take<char>((size_t)p->E * p->rank * p->d_in * s);
@@ -532,40 +572,38 @@ LoraSpace lora_carve(const hmoe_lora_t* p, int64_t n, Workspace& ws) {
 template <typename T>
 int lora_forward_t(const hmoe_lora_t* p, int64_t n, const T* X, const int32_t* offsets, const int32_t* perm, T* U, T* Y,
                    const LoraSpace& w, hipStream_t st) {
-  HMOE_TRY(lora_tables(offsets, p->E, w.tables, st));
-  HMOE_TRY(lora_shrink<T>(X, p->d_in, (const T*)p->A, p->rank, p->scale, offsets, w.tables.shrink, p->E, n, U, st));
+  HMOE_TRY(lora_shrink<T>(X, p->d_in, (const T*)p->A, p->rank, p->scale, offsets, p->E, n, U, st));
   return lora_gemm<T, true>(X, (const T*)p->W, (const T*)p->b, U, (const T*)p->B, p->rank, offsets, p->E, n, p->d_out,
                                p->d_in, perm, Y, st);
 }
 
-template <typename T>
-int lora_transpose(const void* in, void* out, int E, int rows, int cols, hipStream_t st) {
-  HMOE_LAUNCH("lora transpose", k_lora_transpose<T>, dim3((unsigned)(cdiv(cols, 32) * cdiv(rows, 32)), (unsigned)E),
-              dim3(256), 0, st, (const T*)in, (T*)out, rows, cols);
+template <typename T, bool TALL>
+int lora_transpose(const void* in, void* out, int E, int rows, int cols, const int32_t* seg, hipStream_t st) {
+  HMOE_LAUNCH("lora transpose", (k_lora_transpose<T, TALL>), dim3((unsigned)cdiv(TALL ? rows : cols, 64), (unsigned)E),
+              dim3(256), 0, st, (const T*)in, (T*)out, rows, cols, seg);
   return HMOE_OK;
 }
 
 template <typename T>
 int lora_backward_t(const hmoe_lora_t* p, int64_t n, const T* X, const int32_t* offsets, const int32_t* perm, const T* U,
                     const T* dY, T* dX, float* dA, float* dB, const LoraSpace& w, hipStream_t st) {
-  HMOE_TRY(lora_tables(offsets, p->E, w.tables, st));
   if (perm) {
     HMOE_TRY(launch_permute(dY, w.dYs, perm, n, p->d_out, p->dt, st));
     dY = (const T*)w.dYs;
   }
   if (dX || dA) {
-    HMOE_TRY(lora_transpose<T>(p->B, w.Bt, p->E, p->d_out, p->rank, st));
-    HMOE_TRY(lora_shrink<T>(dY, p->d_out, (const T*)w.Bt, p->rank, p->scale, offsets, w.tables.shrink, p->E, n, (T*)w.V, st));
+    HMOE_TRY(lora_transpose<T, true>(p->B, w.Bt, p->E, p->d_out, p->rank, offsets, st));
+    HMOE_TRY(lora_shrink<T>(dY, p->d_out, (const T*)w.Bt, p->rank, p->scale, offsets, p->E, n, (T*)w.V, st));
   }
   if (dX) {
-    HMOE_TRY(lora_transpose<T>(p->A, w.At, p->E, p->rank, p->d_in, st));
+    HMOE_TRY(lora_transpose<T, false>(p->A, w.At, p->E, p->rank, p->d_in, offsets, st));
     HMOE_TRY(lora_gemm<T, false>(dY, (const T*)p->W, nullptr, (const T*)w.V, (const T*)w.At, p->rank, offsets, p->E, n,
                                     p->d_in, p->d_out, perm, dX, st));
   }
   if (dB)
-    HMOE_TRY(lora_grad<T, false>(dY, p->d_out, U, p->rank, offsets, w.tables.piece, p->E, n, dB, w.part, st));
+    HMOE_TRY(lora_grad<T, false>(dY, p->d_out, U, p->rank, offsets, p->E, n, dB, w.part, st));
   if (dA)
-    HMOE_TRY(lora_grad<T, true>(X, p->d_in, (const T*)w.V, p->rank, offsets, w.tables.piece, p->E, n, dA, w.part, st));
+    HMOE_TRY(lora_grad<T, true>(X, p->d_in, (const T*)w.V, p->rank, offsets, p->E, n, dA, w.part, st));
   return HMOE_OK;
 }
 

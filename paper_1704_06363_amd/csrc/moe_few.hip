@@ -23,29 +23,11 @@ struct FewArgs {
 
 // ------------------------------------------------------------------ routing
 
-// A workgroup to a sample: the scores of all experts, a wave to each in turn, and the k best.
-template <typename T>
-__global__ void __launch_bounds__(256) k_few_route(FewArgs a) {
-  constexpr int N = 16 / sizeof(T);
-  __shared__ uint64_t s_key[4096];
-  const int l = threadIdx.x & 63, w = threadIdx.x >> 6, t = blockIdx.x;
-  const T* x = static_cast<const T*>(a.X) + (int64_t)t * a.d;
-  for (int e = w; e < a.K; e += 4) {
-    const T* r = static_cast<const T*>(a.R) + (int64_t)e * a.d;
-    float s = 0.f;
-    for (int v = l; v < a.d / N; v += 64) {
-      const i32x4 xv = *reinterpret_cast<const i32x4*>(x + v * N), rv = *reinterpret_cast<const i32x4*>(r + v * N);
-      const T *xe = reinterpret_cast<const T*>(&xv), *re = reinterpret_cast<const T*>(&rv);
-#pragma unroll
-      for (int z = 0; z < N; ++z) s = fmaf(to_f32(xe[z]), to_f32(re[z]), s);
-    }
-    s = wave_sum(s);
-    if (l == 0) s_key[e] = rank_key(s + (a.r_bias ? a.r_bias[e] : 0.f), (uint32_t)e);
-  }
-  __syncthreads();
-  if (w != 0) return;
+// The k best of K keys, by one wave: weights, and which experts are evaluated.
+__device__ __forceinline__ void few_choose(const FewArgs& a, int t, const lds<uint64_t>* key) {
+  const int l = threadIdx.x & 63;
   uint64_t best = 0;
-  for (int b = 0; b < a.K; b += 64) wave_merge(best, b + l < a.K ? s_key[b + l] : 0);
+  for (int b = 0; b < a.K; b += 64) wave_merge(best, b + l < a.K ? key[b + l] : 0);
   const float s = (uint32_t)(best >> 32) == 0 ? NAN : key_value(best);
   const float top = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(s)));
   float p = l < a.k ? (s == -INFINITY ? 0.f : __expf(s - top)) : 0.f;
@@ -58,6 +40,48 @@ __global__ void __launch_bounds__(256) k_few_route(FewArgs a) {
     a.weight[q] = p;
     a.chosen[q] = p == 0.f ? -1 : (int32_t)key_index(best);
   }
+}
+
+// A workgroup to a sample: the scores of all experts, four at a time to a wave, and the k best.
+constexpr int kRouteWaves = 16, kRouteEach = 4;
+template <typename T>
+__global__ void __launch_bounds__(64 * kRouteWaves) k_few_route(FewArgs a) {
+  constexpr int N = 16 / sizeof(T), G = kRouteEach;
+  __shared__ uint64_t s_key[4096];
+  const int l = threadIdx.x & 63, w = threadIdx.x >> 6, t = blockIdx.x;
+  const T* x = static_cast<const T*>(a.X) + (int64_t)t * a.d;
+  for (int e0 = w * G; e0 < a.K; e0 += kRouteWaves * G) {
+    const T* r[G];
+    float s[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      r[g] = static_cast<const T*>(a.R) + (int64_t)(e0 + g < a.K ? e0 + g : a.K - 1) * a.d;
+      s[g] = 0.f;
+    }
+#pragma unroll 4
+    for (int v = l; v < a.d / N; v += 64) {
+      const i32x4 xv = *reinterpret_cast<const i32x4*>(x + v * N);
+      i32x4 rv[G];
+#pragma unroll
+      for (int g = 0; g < G; ++g) rv[g] = *reinterpret_cast<const i32x4*>(r[g] + v * N);
+      const T* xe = reinterpret_cast<const T*>(&xv);
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        const T* re = reinterpret_cast<const T*>(&rv[g]);
+#pragma unroll
+        for (int z = 0; z < N; ++z) s[g] = fmaf(to_f32(xe[z]), to_f32(re[z]), s[g]);
+      }
+    }
+#pragma unroll
+    for (int g = 0; g < G; ++g) s[g] = wave_sum(s[g]);
+    if (l == 0) {
+#pragma unroll
+      for (int g = 0; g < G; ++g)
+        if (e0 + g < a.K) s_key[e0 + g] = rank_key(s[g] + (a.r_bias ? a.r_bias[e0 + g] : 0.f), (uint32_t)(e0 + g));
+    }
+  }
+  __syncthreads();
+  if (w == 0) few_choose(a, t, (const lds<uint64_t>*)s_key);
 }
 
 // ------------------------------------------------------------------ experts
@@ -166,7 +190,7 @@ template <typename T>
 int moe_few_t(const FewArgs& a, bool gated, hipStream_t st) {
   const int64_t slots = (int64_t)a.n * a.k < a.K ? (int64_t)a.n * a.k : a.K;
   const int t1 = (int)cdiv(a.h, 16), t2 = (int)cdiv(a.o, 16);
-  HMOE_LAUNCH("few route", k_few_route<T>, dim3(a.n), dim3(256), 0, st, a);
+  HMOE_LAUNCH("few route", k_few_route<T>, dim3(a.n), dim3(64 * kRouteWaves), 0, st, a);
   if (gated)
     HMOE_LAUNCH("few layer 1", (k_few_layer<T, 1, true>), dim3((unsigned)(slots * t1)), dim3(256), 0, st, a, t1);
   else
