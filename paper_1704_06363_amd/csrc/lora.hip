@@ -250,13 +250,13 @@ int lora_few_t(const LoraFew& a, hipStream_t st) {
 
 // ------------------------------------------------------------------ rows in adapter order
 
-// U = s_e rows A_e^T for 32 rows of one adapter and 16 RT values of the rank: rows [n][K], A [E][rank][K].
+// U = s_e rows A_e^T for 16 MT rows of one adapter and 16 RT values of the rank: rows [n][K], A [E][rank][K].
 // The four waves split K.
-template <typename T, int RT>
+template <typename T, int RT, int MT>
 __global__ void __launch_bounds__(256) k_lora_shrink(const T* __restrict__ X, int K, const T* __restrict__ A, int rank,
                                                      const float* __restrict__ scale, const int32_t* __restrict__ seg,
                                                      int E, T* __restrict__ U) {
-  constexpr int N = 16 / sizeof(T), STEP = 4 * N, MT = 2;
+  constexpr int N = 16 / sizeof(T), STEP = 4 * N;
   __shared__ floatx4 s_acc[4][RT][MT][64];
   Run run;
   if (!find_run(seg, E, 16 * MT, blockIdx.x, run)) return;
@@ -436,54 +436,69 @@ __global__ void __launch_bounds__(256) k_lora_transpose(const T* __restrict__ in
 // ------------------------------------------------------------------ gradients of the adapters
 
 // Rows of one adapter that a workgroup sums over; adapters with more have several pieces, joined
-// in order by k_lora_grad_join.
-constexpr int kLoraPiece = 1024;
-// Where such a piece's sums are kept: every adapter of more than kLoraPiece rows advances seg / kLoraPiece by
-// at least half of its pieces.
-__device__ __forceinline__ int64_t lora_piece_slot(int64_t seg_e, int64_t local) {
-  return 2 * (seg_e / kLoraPiece) + local;
+// in order by k_lora_grad_join.  A 64th of all rows, so that no workgroup has much more than the others (with
+// 1024 for 16384 rows the few long ones took 69 us for dB and 57 for dA) and 130 pieces at most are kept.
+inline int lora_piece(int64_t n) {
+  int rows = 256;
+  while (rows < (1 << 20) && (int64_t)rows * 64 < n) rows *= 2;
+  return rows;
 }
+// Where a piece's sums are kept: every adapter of more than `piece` rows advances seg / piece by at least
+// half of its pieces.
+__device__ __forceinline__ int64_t lora_piece_slot(int64_t seg_e, int64_t local, int piece) {
+  return 2 * (seg_e / piece) + local;
+}
+
+// Tiles of the gradients: BW columns of D by UW of U, four waves.  The reduction over an adapter's rows is
+// often short, a stage or two, and then a workgroup is all latency: 256 columns rather than 64 (111 us for
+// dB and 74 for dA at 16384 rows of 128 adapters, 4096 and 2048 columns) keep 36 KB of loads in flight in
+// each.  64 where 256 leave CUs idle.
+template <typename T, int UW, int BW, bool U_LEFT>
+struct GradTile {
+  static constexpr int W = BW / (BW == 256 ? 4 : 2), V = BW == 256 ? UW : UW / 2;
+  using type = typename std::conditional<U_LEFT, Cfg<T, UW, BW, V, W>, Cfg<T, BW, UW, W, V>>::type;
+};
 
 // For one piece of adapter e's rows:  U_LEFT: out[c][m] = sum_rows U[c] D[m] (dA: [rank][width]),
 // otherwise out[m][c] = sum_rows D[m] U[c] (dB: [width][rank]).  D [n][width] with U or V as u_width says.
-template <typename T, bool U_LEFT>
+template <typename T, int UW, int BW, bool U_LEFT>
 __global__ void __launch_bounds__(256) k_lora_grad(const T* __restrict__ D, int width, const T* __restrict__ U, int rank,
-                                                   const int32_t* __restrict__ seg, int E,
+                                                   const int32_t* __restrict__ seg, int E, int piece,
                                                    float* __restrict__ out, float* __restrict__ part) {
-  using C = CfgQuarter<T>;
+  using C = typename GradTile<T, UW, BW, U_LEFT>::type;
+  static_assert(C::THREADS == 256, "four waves");
   extern __shared__ __attribute__((aligned(16))) char smem_raw[];
   lds<char>* smem = (lds<char>*)smem_raw;
   Run run;
-  if (!find_run(seg, E, kLoraPiece, blockIdx.x, run)) return;
+  if (!find_run(seg, E, piece, blockIdx.x, run)) return;
   const int e = run.segment;
-  const int64_t local = run.local, p0 = seg[e] + local * kLoraPiece;
+  const int64_t local = run.local, p0 = seg[e] + local * piece;
   const int64_t len = seg[e + 1] - p0;
-  const int rows = (int)(len < kLoraPiece ? len : kLoraPiece);
+  const int rows = (int)(len < piece ? len : piece);
   const int ldu = u_width<T>(rank);
-  const int d0 = blockIdx.y * 64, u0 = blockIdx.z * 64;
-  const int dv = width - d0 < 64 ? width - d0 : 64, uv = ldu - u0 < 64 ? ldu - u0 : 64;
+  const int d0 = blockIdx.y * BW, u0 = blockIdx.z * UW;
+  const int dv = width - d0 < BW ? width - d0 : BW, uv = ldu - u0 < UW ? ldu - u0 : UW;
   const T *pd = D + p0 * width + d0, *pu = U + p0 * ldu + u0;
   floatx4 acc[C::MI][C::NJ];
   if constexpr (U_LEFT) gemm_tile<C, false, false>(pu, ldu, uv, pd, width, dv, rows, smem, acc);
   else gemm_tile<C, false, false>(pd, width, dv, pu, ldu, uv, rows, smem, acc);
   const int64_t size = (int64_t)width * rank;
-  float* to = seg[e + 1] - seg[e] > kLoraPiece ? part + lora_piece_slot(seg[e], local) * size : out + e * size;
+  float* to = seg[e + 1] - seg[e] > piece ? part + lora_piece_slot(seg[e], local, piece) * size : out + e * size;
   const Frag<C> f;
   const auto put = [&](int c, int m, float v) {  // value c of the rank, column m of D
     if (c < rank && m < width) to[U_LEFT ? (int64_t)c * width + m : (int64_t)m * rank + c] = v;
   };
+  constexpr bool BF = sizeof(T) == 2;  // the sums with 16 values and with their remainders are one
 #pragma unroll
   for (int i = 0; i < C::MI; ++i)
 #pragma unroll
     for (int j = 0; j < C::NJ; ++j)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        if constexpr (sizeof(T) == 2) {  // the sums with the values and with their remainders are one
-          if constexpr (U_LEFT) {
-            if (i == 0) put((u0 + 32 * f.wm) / 2 + 4 * f.lg + r, d0 + f.col(j, r), acc[0][j][r] + acc[1][j][r]);
-          } else {
-            if (j == 0) put((u0 + 32 * f.wn) / 2 + f.lr, d0 + f.row(i, r), acc[i][0][r] + acc[i][1][r]);
-          }
+        if constexpr (BF && U_LEFT) {
+          if (i % 2 == 0) put((u0 + f.wm * C::WM) / 2 + 8 * i + 4 * f.lg + r, d0 + f.col(j, r), acc[i][j][r] + acc[i + 1][j][r]);
+        } else if constexpr (BF) {
+          if (j % 2 == 0) put((u0 + f.wn * C::WN) / 2 + 8 * j + f.lr, d0 + f.row(i, r), acc[i][j][r] + acc[i][j + 1][r]);
         } else {
           if constexpr (U_LEFT) put(u0 + f.row(i, r), d0 + f.col(j, r), acc[i][j][r]);
           else put(u0 + f.col(j, r), d0 + f.row(i, r), acc[i][j][r]);
@@ -493,14 +508,14 @@ __global__ void __launch_bounds__(256) k_lora_grad(const T* __restrict__ D, int 
 
 // The pieces of an adapter added in their order; adapters without rows get zeros.
 __global__ void __launch_bounds__(256) k_lora_grad_join(const float* __restrict__ part, const int32_t* __restrict__ seg,
-                                                        int64_t size, float* __restrict__ out) {
+                                                        int piece, int64_t size, float* __restrict__ out) {
   const int e = blockIdx.y;
-  const int64_t pieces = cdiv(seg[e + 1] - seg[e], kLoraPiece);
+  const int64_t pieces = cdiv(seg[e + 1] - seg[e], piece);
   if (pieces == 1) return;
   const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
   if (i >= size) return;
   floatx4 s = {0.f, 0.f, 0.f, 0.f};
-  const float* p = part + lora_piece_slot(seg[e], 0) * size + i;
+  const float* p = part + lora_piece_slot(seg[e], 0, piece) * size + i;
   for (int64_t q = 0; q < pieces; ++q) s += *reinterpret_cast<const floatx4*>(p + q * size);
   *reinterpret_cast<floatx4*>(out + e * size + i) = s;
 }
@@ -509,14 +524,14 @@ template <typename T>
 int lora_shrink(const T* X, int K, const T* A, int rank, const float* scale, const int32_t* seg, int E,
                 int64_t n, T* U, hipStream_t st) {
   const int blocks = u_blocks(rank);
-  const unsigned bound = (unsigned)(n / 32 + (E < n ? E : n));
+  const auto bound = [&](int rows) { return (unsigned)(n / rows + (E < n ? E : n)); };
   if (blocks == 1)
-    HMOE_LAUNCH("lora shrink", (k_lora_shrink<T, 1>), dim3(bound), dim3(256), 0, st, X, K, A, rank, scale, seg, E, U);
+    HMOE_LAUNCH("lora shrink", (k_lora_shrink<T, 1, 1>), dim3(bound(16)), dim3(256), 0, st, X, K, A, rank, scale, seg, E, U);
   else if (blocks == 2)
-    HMOE_LAUNCH("lora shrink", (k_lora_shrink<T, 2>), dim3(bound), dim3(256), 0, st, X, K, A, rank, scale, seg, E, U);
+    HMOE_LAUNCH("lora shrink", (k_lora_shrink<T, 2, 2>), dim3(bound(32)), dim3(256), 0, st, X, K, A, rank, scale, seg, E, U);
   else
-    HMOE_LAUNCH("lora shrink", (k_lora_shrink<T, 4>), dim3(bound, (unsigned)cdiv(blocks, 4)), dim3(256), 0, st, X, K, A,
-                rank, scale, seg, E, U);
+    HMOE_LAUNCH("lora shrink", (k_lora_shrink<T, 4, 2>), dim3(bound(32), (unsigned)cdiv(blocks, 4)), dim3(256), 0, st, X, K,
+                A, rank, scale, seg, E, U);
   return HMOE_OK;
 }
 
@@ -537,19 +552,29 @@ int lora_gemm(const T* A, const T* W, const T* bias, const T* U, const T* B, int
   return HMOE_OK;
 }
 
-template <typename T, bool U_LEFT>
-int lora_grad(const T* D, int width, const T* U, int rank, const int32_t* seg, int E, int64_t n,
-              float* out, float* part, hipStream_t st) {
-  using C = CfgQuarter<T>;
-  const char* label = U_LEFT ? "lora dA" : "lora dB";
-  const unsigned bound = (unsigned)(n / kLoraPiece + (E < n ? E : n));
-  HMOE_LAUNCH(label, (k_lora_grad<T, U_LEFT>),
-              dim3(bound, (unsigned)cdiv(width, 64), (unsigned)cdiv(u_width<T>(rank), 64)), dim3(256), C::LDS, st, D, width,
-              U, rank, seg, E, out, part);
+template <typename T, int UW, int BW, bool U_LEFT>
+int lora_grad_tiles(const T* D, int width, const T* U, int rank, const int32_t* seg, int E, int64_t n, float* out,
+                    float* part, hipStream_t st) {
+  using C = typename GradTile<T, UW, BW, U_LEFT>::type;
+  const int piece = lora_piece(n);
+  HMOE_LAUNCH(U_LEFT ? "lora dA" : "lora dB", (k_lora_grad<T, UW, BW, U_LEFT>),
+              dim3((unsigned)(n / piece + (E < n ? E : n)), (unsigned)cdiv(width, BW),
+                   (unsigned)cdiv(u_width<T>(rank), UW)),
+              dim3(256), C::LDS, st, D, width, U, rank, seg, E, piece, out, part);
   const int64_t size = (int64_t)width * rank;
   HMOE_LAUNCH("lora gradient join", k_lora_grad_join, dim3((unsigned)cdiv(size, 1024), (unsigned)E), dim3(256), 0, st,
-              part, seg, size, out);
+              part, seg, piece, size, out);
   return HMOE_OK;
+}
+template <typename T, bool U_LEFT>
+int lora_grad(const T* D, int width, const T* U, int rank, const int32_t* seg, int E, int64_t n, float* out, float* part,
+              hipStream_t st) {
+  const int ldu = u_width<T>(rank);
+  if ((n / lora_piece(n) + (E < n ? E : n)) * cdiv(width, 256) < device_cus())
+    return lora_grad_tiles<T, 64, 64, U_LEFT>(D, width, U, rank, seg, E, n, out, part, st);
+  if (ldu <= 32) return lora_grad_tiles<T, 32, 256, U_LEFT>(D, width, U, rank, seg, E, n, out, part, st);
+  if (ldu <= 64) return lora_grad_tiles<T, 64, 256, U_LEFT>(D, width, U, rank, seg, E, n, out, part, st);
+  return lora_grad_tiles<T, 128, 256, U_LEFT>(D, width, U, rank, seg, E, n, out, part, st);
 }
 
 struct LoraSpace {
@@ -565,7 +590,8 @@ LoraSpace lora_carve(const hmoe_lora_t* p, int64_t n, Workspace& ws) {
   x.At = ws.take<char>((size_t)p->E * p->rank * p->d_in * s);
   x.V = ws.take<char>((size_t)n * ldu * s);
   const size_t wide = p->d_out > p->d_in ? p->d_out : p->d_in;
-  x.part = ws.take<float>(n > kLoraPiece ? (2 * (n / kLoraPiece) + 2) * wide * p->rank : 0);
+  const int64_t piece = lora_piece(n);
+  x.part = ws.take<float>(n > piece ? (2 * (n / piece) + 2) * wide * p->rank : 0);
   return x;
 }
 
