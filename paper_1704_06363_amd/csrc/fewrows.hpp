@@ -19,6 +19,44 @@ __device__ __forceinline__ void step_mfma(i32x4 a, i32x4 b, floatx4& acc) {
   }
 }
 
+// body(wv, xv) for the steps s0 <= s < s1 of a reduction over kd elements, with this lane's 16 bytes of the
+// rows at w and x.  The loads of U steps go out together: under a bound on K of their own (which the
+// compiler does not move loads across) they ran one step at a time.  kd is a multiple of 8: past it, in
+// the last step, both operands are zeros.
+template <typename T, int U, int MI, int NX, class Body>
+__device__ __forceinline__ void stream_steps(const T* const (&w)[MI], const T* const (&x)[NX], int kd, int s0, int s1,
+                                             Body body) {
+  constexpr int N = 16 / sizeof(T), STEP = 4 * N;
+  const int lg = (threadIdx.x & 63) >> 4;
+  const int ragged = kd % STEP ? kd / STEP : -1;  // the step with less than STEP elements
+  for (int s = s0; s < s1; s += U) {
+    i32x4 wv[U][MI], xv[U][NX];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int at = (s + u < s1 ? s + u : s1 - 1) * STEP + lg * N;
+      const int in = at < kd ? at : kd - N;
+#pragma unroll
+      for (int i = 0; i < MI; ++i) wv[u][i] = *reinterpret_cast<const i32x4*>(w[i] + in);
+#pragma unroll
+      for (int j = 0; j < NX; ++j) xv[u][j] = *reinterpret_cast<const i32x4*>(x[j] + in);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (s + u >= s1) break;
+      if (s + u == ragged) {
+        const bool out = ragged * STEP + lg * N >= kd;
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+          if (out) wv[u][i] = i32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < NX; ++j)
+          if (out) xv[u][j] = i32x4{0, 0, 0, 0};
+      }
+      body(wv[u], xv[u]);
+    }
+  }
+}
+
 // A value that feeds a bf16 product without losing its low bits: v = hi + lo up to 2^-16 of it, each a
 // bf16 operand of its own MFMA.  hi is cut off rather than rounded, so that no finite v becomes
 // infinite.  (fp32 data: the value itself.)

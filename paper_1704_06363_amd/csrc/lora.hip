@@ -99,7 +99,7 @@ struct LoraFew {
 constexpr int kFewShrinkWaves = 8;
 template <typename T>
 __global__ void __launch_bounds__(64 * kFewShrinkWaves) k_lora_few_shrink(LoraFew a) {
-  constexpr int N = 16 / sizeof(T), STEP = 4 * N, NW = kFewShrinkWaves;
+  constexpr int STEP = 64 / sizeof(T), NW = kFewShrinkWaves;
   __shared__ int s_group, s_count, s_rows[HMOE_FEW_ROWS];
   __shared__ floatx4 s_acc[NW][64];
   const int blocks = u_blocks(a.rank), kb = blockIdx.x % blocks;
@@ -114,13 +114,8 @@ __global__ void __launch_bounds__(64 * kFewShrinkWaves) k_lora_few_shrink(LoraFe
     const int row = s_rows[t0 + lr < count ? t0 + lr : count - 1];
     const T* x = static_cast<const T*>(a.X) + (int64_t)row * a.d;
     floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-    for (int s = s0; s < s1; ++s) {
-      const int at = s * STEP + lg * N;
-      const i32x4 av = at < a.d ? *reinterpret_cast<const i32x4*>(A + at) : i32x4{0, 0, 0, 0};
-      const i32x4 xv = at < a.d ? *reinterpret_cast<const i32x4*>(x + at) : i32x4{0, 0, 0, 0};
-      step_mfma<T>(av, xv, acc);
-    }
+    stream_steps<T, 8>({A}, {x}, a.d, s0, s1,
+                       [&](const i32x4(&av)[1], const i32x4(&xv)[1]) { step_mfma<T>(av[0], xv[0], acc); });
     s_acc[w][l] = acc;
     __syncthreads();
     if (w == 0 && t0 + lr < count) {
@@ -136,7 +131,7 @@ __global__ void __launch_bounds__(64 * kFewShrinkWaves) k_lora_few_shrink(LoraFe
 // 16 MI columns of Y for all rows (16 NT at most); the waves split d, and the adapters of the rows.
 template <typename T, int MI, int NT>
 __global__ void __launch_bounds__(256) k_lora_few(LoraFew a) {
-  constexpr int N = 16 / sizeof(T), STEP = 4 * N;
+  constexpr int STEP = 64 / sizeof(T);
   __shared__ floatx4 s_acc[4][MI][NT][64];
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6, lr = l & 15, lg = l >> 4;
   const int c0 = blockIdx.x * 16 * MI;
@@ -162,19 +157,12 @@ __global__ void __launch_bounds__(256) k_lora_few(LoraFew a) {
 #pragma unroll
     for (int t = 0; t < NT; ++t) acc[i][t] = floatx4{0.f, 0.f, 0.f, 0.f};
   const int steps = (a.d + STEP - 1) / STEP, s0 = steps * w / 4, s1 = steps * (w + 1) / 4;
-#pragma unroll 4
-  for (int s = s0; s < s1; ++s) {
-    const int at = s * STEP + lg * N;
-    i32x4 wv[MI], xv[NT];
-#pragma unroll
-    for (int i = 0; i < MI; ++i) wv[i] = at < a.d ? *reinterpret_cast<const i32x4*>(W[i] + at) : i32x4{0, 0, 0, 0};
-#pragma unroll
-    for (int t = 0; t < NT; ++t) xv[t] = at < a.d ? *reinterpret_cast<const i32x4*>(x[t] + at) : i32x4{0, 0, 0, 0};
+  stream_steps<T, 4>(W, x, a.d, s0, s1, [&](const i32x4(&wv)[MI], const i32x4(&xv)[NT]) {
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
       for (int t = 0; t < NT; ++t) step_mfma<T>(wv[i], xv[t], acc[i][t]);
-  }
+  });
   // the adapters in the order of their first rows, one to a wave in turn
   uint64_t left = __ballot(l < a.n && all >= 0 && all < a.E);
   const int ldu = u_width<T>(a.rank), blocks = u_blocks(a.rank);
@@ -256,7 +244,7 @@ template <typename T, int RT, int MT>
 __global__ void __launch_bounds__(256) k_lora_shrink(const T* __restrict__ X, int K, const T* __restrict__ A, int rank,
                                                      const float* __restrict__ scale, const int32_t* __restrict__ seg,
                                                      int E, T* __restrict__ U) {
-  constexpr int N = 16 / sizeof(T), STEP = 4 * N;
+  constexpr int STEP = 64 / sizeof(T);
   __shared__ floatx4 s_acc[4][RT][MT][64];
   Run run;
   if (!find_run(seg, E, 16 * MT, blockIdx.x, run)) return;
@@ -279,19 +267,12 @@ __global__ void __launch_bounds__(256) k_lora_shrink(const T* __restrict__ X, in
 #pragma unroll
     for (int t = 0; t < MT; ++t) acc[i][t] = floatx4{0.f, 0.f, 0.f, 0.f};
   const int steps = (K + STEP - 1) / STEP, s0 = (int)((int64_t)steps * w / 4), s1 = (int)((int64_t)steps * (w + 1) / 4);
-#pragma unroll 4
-  for (int s = s0; s < s1; ++s) {
-    const int at = s * STEP + lg * N;
-    i32x4 xv[MT], av[RT];
-#pragma unroll
-    for (int t = 0; t < MT; ++t) xv[t] = at < K ? *reinterpret_cast<const i32x4*>(x[t] + at) : i32x4{0, 0, 0, 0};
-#pragma unroll
-    for (int i = 0; i < RT; ++i) av[i] = at < K ? *reinterpret_cast<const i32x4*>(ar[i] + at) : i32x4{0, 0, 0, 0};
+  stream_steps<T, RT == 1 ? 8 : 4>(ar, x, K, s0, s1, [&](const i32x4(&av)[RT], const i32x4(&xv)[MT]) {
 #pragma unroll
     for (int i = 0; i < RT; ++i)
 #pragma unroll
       for (int t = 0; t < MT; ++t) step_mfma<T>(av[i], xv[t], acc[i][t]);
-  }
+  });
 #pragma unroll
   for (int i = 0; i < RT; ++i)
 #pragma unroll

@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(64 * kRouteWaves) k_few_route(FewArgs a) {
 // the reduction and join in LDS.
 template <typename T, int LAYER, bool GATED>
 __global__ void __launch_bounds__(256) k_few_layer(FewArgs a, int tiles) {
-  constexpr int N = 16 / sizeof(T), STEP = 4 * N;
+  constexpr int STEP = 64 / sizeof(T);
   constexpr int MI = LAYER == 1 && GATED ? 2 : 1;
   constexpr int NX = LAYER == 2 ? Halves<T>::N : 1;  // operands of an activation
   __shared__ int s_expert, s_count, s_rows[HMOE_FEW_ROWS];
@@ -115,21 +115,17 @@ __global__ void __launch_bounds__(256) k_few_layer(FewArgs a, int tiles) {
     floatx4 acc[MI];
 #pragma unroll
     for (int i = 0; i < MI; ++i) acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-    for (int s = s0; s < s1; ++s) {
-      const int at = s * STEP + lg * N;
-      i32x4 wv[MI], xv[NX];
+    const T *wp[MI], *xp[NX];
 #pragma unroll
-      for (int i = 0; i < MI; ++i)
-        wv[i] = at < kd ? *reinterpret_cast<const i32x4*>(W + (int64_t)i * a.h * kd + at) : i32x4{0, 0, 0, 0};
+    for (int i = 0; i < MI; ++i) wp[i] = W + (int64_t)i * a.h * kd;
 #pragma unroll
-      for (int j = 0; j < NX; ++j)
-        xv[j] = at < kd ? *reinterpret_cast<const i32x4*>(x + j * kd + at) : i32x4{0, 0, 0, 0};
+    for (int j = 0; j < NX; ++j) xp[j] = x + j * kd;
+    stream_steps<T, 8 / (MI + NX - 1)>(wp, xp, kd, s0, s1, [&](const i32x4(&wv)[MI], const i32x4(&xv)[NX]) {
 #pragma unroll
       for (int i = 0; i < MI; ++i)
 #pragma unroll
         for (int j = 0; j < NX; ++j) step_mfma<T>(wv[i], xv[j], acc[i]);
-    }
+    });
 #pragma unroll
     for (int i = 0; i < MI; ++i) s_acc[w][i][l] = acc[i];
     __syncthreads();
