@@ -5,6 +5,9 @@
 
 namespace hmoe {
 
+template <typename T>
+using quad = T __attribute__((ext_vector_type(4)));
+
 // acc += A B^T over one step of 64 bytes of K: lane l holds 16 bytes (bf16: 8, fp32: 4 elements) of
 // row l % 16 at byte 16 (l / 16) of the step.  Lane l of acc has rows 4 (l / 16) .. + 3 of A against row l % 16 of B.
 template <typename T>

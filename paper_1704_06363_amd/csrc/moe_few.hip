@@ -14,20 +14,33 @@ struct FewArgs {
   int n, K, d, h, o, k;  // k experts to a sample
   int32_t* expert;       // [n k]
   float* weight;
-  int32_t* chosen;  // [n k]: expert, or -1 where its weight is 0
-  void* hid;        // [n k][Halves][h]
-  float* part;      // [splits][n k][o]
-  int splits;       // of the second layer's reduction
+  int32_t* chosen;   // [n k]: expert, or -1 where its weight is 0
+  float* score;      // [n][K], where one workgroup does not hold them all
+  void* hid;         // [n k][Halves][h]
+  int splits;        // of the second layer's reduction
+  float* part;       // [splits][n k][o], where Y has several
+  uint32_t* count;   // per 16 columns of Y: workgroups that have written their part
+  int counts;
   void* Y;
 };
 
 // ------------------------------------------------------------------ routing
 
-// The k best of K keys, by one wave: weights, and which experts are evaluated.
-__device__ __forceinline__ void few_choose(const FewArgs& a, int t, const lds<uint64_t>* key) {
+// By the call's first kernel, for its last one.
+__device__ __forceinline__ void clear_counts(const FewArgs& a) {
+  if (blockIdx.x == 0 && blockIdx.y == 0)
+    for (int i = threadIdx.x; i < a.counts; i += blockDim.x) a.count[i] = 0;
+}
+
+// The k best of a sample's K scores, by one wave: weights, and which experts are evaluated.
+template <typename T, class Score>
+__device__ __forceinline__ void few_choose(const FewArgs& a, int t, Score score) {
   const int l = threadIdx.x & 63;
   uint64_t best = 0;
-  for (int b = 0; b < a.K; b += 64) wave_merge(best, b + l < a.K ? key[b + l] : 0);
+  for (int b = 0; b < a.K; b += 64) {
+    const int e = b + l;
+    wave_merge(best, e < a.K ? rank_key(score(e) + (a.r_bias ? a.r_bias[e] : 0.f), (uint32_t)e) : 0);
+  }
   const float s = (uint32_t)(best >> 32) == 0 ? NAN : key_value(best);
   const float top = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(s)));
   float p = l < a.k ? (s == -INFINITY ? 0.f : __expf(s - top)) : 0.f;
@@ -40,15 +53,19 @@ __device__ __forceinline__ void few_choose(const FewArgs& a, int t, const lds<ui
     a.weight[q] = p;
     a.chosen[q] = p == 0.f ? -1 : (int32_t)key_index(best);
   }
+  if (a.counts == 0 && sum == 0.f)  // nobody else writes the row
+    for (int c = l; c < a.o; c += 64) static_cast<T*>(a.Y)[(int64_t)t * a.o + c] = from_f32<T>(0.f);
 }
 
-// A workgroup to a sample: the scores of all experts, four at a time to a wave, and the k best.
-constexpr int kRouteWaves = 16, kRouteEach = 4;
+// A workgroup to a sample: the scores of all experts, four at a time to a wave, and the k best.  One CU
+// draws some 40 GB/s from its L2 here, so this is for small routers.
+constexpr int kRouteWaves = 16, kRouteEach = 4, kRouteMost = 512;
 template <typename T>
 __global__ void __launch_bounds__(64 * kRouteWaves) k_few_route(FewArgs a) {
   constexpr int N = 16 / sizeof(T), G = kRouteEach;
-  __shared__ uint64_t s_key[4096];
+  __shared__ float s_score[kRouteMost];
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6, t = blockIdx.x;
+  clear_counts(a);
   const T* x = static_cast<const T*>(a.X) + (int64_t)t * a.d;
   for (int e0 = w * G; e0 < a.K; e0 += kRouteWaves * G) {
     const T* r[G];
@@ -77,66 +94,126 @@ __global__ void __launch_bounds__(64 * kRouteWaves) k_few_route(FewArgs a) {
     if (l == 0) {
 #pragma unroll
       for (int g = 0; g < G; ++g)
-        if (e0 + g < a.K) s_key[e0 + g] = rank_key(s[g] + (a.r_bias ? a.r_bias[e0 + g] : 0.f), (uint32_t)(e0 + g));
+        if (e0 + g < a.K) s_score[e0 + g] = s[g];
     }
   }
   __syncthreads();
-  if (w == 0) few_choose(a, t, (const lds<uint64_t>*)s_key);
+  if (w == 0) few_choose<T>(a, t, [&](int e) { return s_score[e]; });
+}
+
+// Scores of 16 samples against 16 experts; eight waves split the reduction.
+constexpr int kScoreWaves = 8;
+template <typename T>
+__global__ void __launch_bounds__(64 * kScoreWaves) k_few_score(FewArgs a) {
+  constexpr int STEP = 64 / sizeof(T), NW = kScoreWaves;
+  __shared__ floatx4 s_acc[NW][64];
+  const int l = threadIdx.x & 63, w = threadIdx.x >> 6, lr = l & 15, lg = l >> 4;
+  const int e0 = blockIdx.x * 16, t = blockIdx.y * 16 + lr;
+  clear_counts(a);
+  const T* const x[1] = {static_cast<const T*>(a.X) + (int64_t)(t < a.n ? t : a.n - 1) * a.d};
+  const T* const r[1] = {static_cast<const T*>(a.R) + (int64_t)(e0 + lr < a.K ? e0 + lr : a.K - 1) * a.d};
+  const int steps = (a.d + STEP - 1) / STEP;
+  floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+  stream_steps<T, 8>(r, x, a.d, (int)((int64_t)steps * w / NW), (int)((int64_t)steps * (w + 1) / NW),
+                     [&](const i32x4(&rv)[1], const i32x4(&xv)[1]) { step_mfma<T>(rv[0], xv[0], acc); });
+  s_acc[w][l] = acc;
+  __syncthreads();
+  if (w != 0 || t >= a.n) return;
+#pragma unroll
+  for (int q = 1; q < NW; ++q) acc += s_acc[q][l];
+#pragma unroll
+  for (int z = 0; z < 4; ++z)
+    if (e0 + 4 * lg + z < a.K) a.score[(int64_t)t * a.K + e0 + 4 * lg + z] = acc[z];
+}
+
+template <typename T>
+__global__ void __launch_bounds__(64) k_few_choose(FewArgs a) {
+  const int t = blockIdx.x;
+  few_choose<T>(a, t, [&](int e) { return a.score[(int64_t)t * a.K + e]; });
 }
 
 // ------------------------------------------------------------------ experts
 
-// LAYER 1: hid[q] = act(W1_e x + b1_e).   LAYER 2: part[split][q] = W2_e hid[q] over a split of the reduction.
-// A workgroup has 16 outputs (GATED: and the 16 they are gated with) of one expert; its four waves split
-// the reduction and join in LDS.
-template <typename T, int LAYER, bool GATED>
-__global__ void __launch_bounds__(256) k_few_layer(FewArgs a, int tiles) {
+// Four floats that workgroups of other XCDs read later in the same launch: stored and loaded past the
+// L2s (which are not coherent with each other), so that neither side has to write back or drop what its
+// L2 holds -- as the fences of a release and an acquire do: 93 us instead of 17 for the second layer of 8
+// samples with two of 128 experts each.
+__device__ __forceinline__ void store_through(float* p, floatx4 v) {
+  uint64_t* q = reinterpret_cast<uint64_t*>(p);
+  const uint64_t lo = ((uint64_t)__float_as_uint(v[1]) << 32) | __float_as_uint(v[0]);
+  const uint64_t hi = ((uint64_t)__float_as_uint(v[3]) << 32) | __float_as_uint(v[2]);
+  __hip_atomic_store(q, lo, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __hip_atomic_store(q + 1, hi, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ floatx4 load_through(const float* p) {
+  const uint64_t* q = reinterpret_cast<const uint64_t*>(p);
+  const uint64_t lo = __hip_atomic_load(q, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  const uint64_t hi = __hip_atomic_load(q + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return floatx4{__uint_as_float((uint32_t)lo), __uint_as_float((uint32_t)(lo >> 32)), __uint_as_float((uint32_t)hi),
+                 __uint_as_float((uint32_t)(hi >> 32))};
+}
+
+// LAYER 1: hid[q] = act(W1_e x + b1_e).   LAYER 2: Y, the combine included.
+// A workgroup has 16 outputs (GATED: and the 16 they are gated with) of one expert, or of a split of
+// its reduction; its four waves split that further and join in LDS.  In layer 2 with several parts to an
+// output the workgroup that is the last to store its part of 16 columns adds them up, in the order of the
+// choices and splits: the result does not depend on which one that is.
+// U steps of loads go out together: more of them keep fewer waves on a CU.  64 samples with four of 128
+// experts each, U = 4 / 8: 334 / 343 us for the first layer (2048 -> 2 x 2048), 114 / 132 for the second
+// (2048 -> 1024); one sample with one of 16, U = 4 / 8 / 16: 6.9 / 6.5 / 5.3 us for the first
+// (2048 -> 4096), whose waves have 16 steps each.
+template <typename T, int LAYER, bool GATED, int U>
+__global__ void __launch_bounds__(256) k_few_layer(FewArgs a, int tiles, int slots) {
   constexpr int STEP = 64 / sizeof(T);
   constexpr int MI = LAYER == 1 && GATED ? 2 : 1;
   constexpr int NX = LAYER == 2 ? Halves<T>::N : 1;  // operands of an activation
   __shared__ int s_expert, s_count, s_rows[HMOE_FEW_ROWS];
   __shared__ floatx4 s_acc[4][MI][64];
   const int splits = LAYER == 1 ? 1 : a.splits;
-  const int slot = blockIdx.x / (tiles * splits);
-  const int tile = blockIdx.x % tiles, split = blockIdx.x / tiles % splits;
-  if (!few_group<256>(a.chosen, a.n * a.k, a.K, slot, &s_expert, s_rows, &s_count)) return;
-  const int e = s_expert, count = s_count;
+  const int slot = blockIdx.x / (tiles * splits), tile = blockIdx.x % tiles, split = blockIdx.x / tiles % splits;
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6, lr = l & 15, lg = l >> 4;
-  const int kd = LAYER == 1 ? a.d : a.h, rows = LAYER == 1 ? a.h : a.o;
-  const int r = tile * 16 + lr < rows ? tile * 16 + lr : rows - 1;
-  const T* W = LAYER == 1 ? static_cast<const T*>(a.W1) + ((int64_t)e * MI * a.h + r) * kd
-                          : static_cast<const T*>(a.W2) + ((int64_t)e * a.o + r) * kd;
-  const int steps = (kd + STEP - 1) / STEP, parts = 4 * splits, part = split * 4 + w;
-  const int s0 = (int)((int64_t)steps * part / parts), s1 = (int)((int64_t)steps * (part + 1) / parts);
-  for (int t0 = 0; t0 < count; t0 += 16) {
-    const int q = s_rows[t0 + lr < count ? t0 + lr : count - 1];
-    const T* x = LAYER == 1 ? static_cast<const T*>(a.X) + (int64_t)(q / a.k) * kd
-                            : static_cast<const T*>(a.hid) + (int64_t)q * NX * kd;
-    floatx4 acc[MI];
+  const int c0 = tile * 16 + 4 * lg;
+  // the choices of one sample are groups of their own
+  const bool any = a.n == 1 ? a.chosen[slot] >= 0
+                            : few_group<256>(a.chosen, a.n * a.k, a.K, slot, &s_expert, s_rows, &s_count);
+  if (LAYER == 1 && !any) return;
+  if (any) {
+    const int e = a.n == 1 ? a.chosen[slot] : s_expert, count = a.n == 1 ? 1 : s_count;
+    const int kd = LAYER == 1 ? a.d : a.h, rows = LAYER == 1 ? a.h : a.o;
+    const int r = tile * 16 + lr < rows ? tile * 16 + lr : rows - 1;
+    const T* W[MI];
 #pragma unroll
-    for (int i = 0; i < MI; ++i) acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
-    const T *wp[MI], *xp[NX];
+    for (int i = 0; i < MI; ++i)
+      W[i] = LAYER == 1 ? static_cast<const T*>(a.W1) + ((int64_t)e * MI * a.h + (int64_t)i * a.h + r) * kd
+                        : static_cast<const T*>(a.W2) + ((int64_t)e * a.o + r) * kd;
+    const int steps = (kd + STEP - 1) / STEP, shares = 4 * splits, share = split * 4 + w;
+    const int s0 = (int)((int64_t)steps * share / shares), s1 = (int)((int64_t)steps * (share + 1) / shares);
+    for (int t0 = 0; t0 < count; t0 += 16) {
+      const int q = a.n == 1 ? slot : s_rows[t0 + lr < count ? t0 + lr : count - 1];
+      const T* x[NX];
 #pragma unroll
-    for (int i = 0; i < MI; ++i) wp[i] = W + (int64_t)i * a.h * kd;
+      for (int j = 0; j < NX; ++j)
+        x[j] = LAYER == 1 ? static_cast<const T*>(a.X) + (int64_t)(q / a.k) * kd
+                          : static_cast<const T*>(a.hid) + ((int64_t)q * NX + j) * kd;
+      floatx4 acc[MI];
 #pragma unroll
-    for (int j = 0; j < NX; ++j) xp[j] = x + j * kd;
-    stream_steps<T, 8 / (MI + NX - 1)>(wp, xp, kd, s0, s1, [&](const i32x4(&wv)[MI], const i32x4(&xv)[NX]) {
+      for (int i = 0; i < MI; ++i) acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+      stream_steps<T, U>(W, x, kd, s0, s1, [&](const i32x4(&wv)[MI], const i32x4(&xv)[NX]) {
 #pragma unroll
-      for (int i = 0; i < MI; ++i)
+        for (int i = 0; i < MI; ++i)
 #pragma unroll
-        for (int j = 0; j < NX; ++j) step_mfma<T>(wv[i], xv[j], acc[i]);
-    });
+          for (int j = 0; j < NX; ++j) step_mfma<T>(wv[i], xv[j], acc[i]);
+      });
 #pragma unroll
-    for (int i = 0; i < MI; ++i) s_acc[w][i][l] = acc[i];
-    __syncthreads();
-    if (w == 0 && t0 + lr < count) {
+      for (int i = 0; i < MI; ++i) s_acc[w][i][l] = acc[i];
+      __syncthreads();
+      if (w == 0 && t0 + lr < count && c0 < rows) {  // rows are a multiple of 8: four at a time
 #pragma unroll
-      for (int i = 0; i < MI; ++i) acc[i] = (s_acc[0][i][l] + s_acc[1][i][l]) + (s_acc[2][i][l] + s_acc[3][i][l]);
-      const int c0 = tile * 16 + 4 * lg;
-      if (c0 < rows) {  // rows are a multiple of 8: four at a time
+        for (int i = 0; i < MI; ++i) acc[i] = (acc[i] + s_acc[1][i][l]) + (s_acc[2][i][l] + s_acc[3][i][l]);
         if constexpr (LAYER == 1) {
           const T* b = static_cast<const T*>(a.b1) + (int64_t)e * MI * a.h;
           T* out = static_cast<T*>(a.hid) + (int64_t)q * Halves<T>::N * a.h + c0;
+          quad<T> hid[Halves<T>::N];
 #pragma unroll
           for (int z = 0; z < 4; ++z) {
             float v = acc[0][z] + (a.b1 ? to_f32(b[c0 + z]) : 0.f);
@@ -148,61 +225,105 @@ __global__ void __launch_bounds__(256) k_few_layer(FewArgs a, int tiles) {
             }
             const Halves<T> p(v);
 #pragma unroll
-            for (int j = 0; j < Halves<T>::N; ++j) out[j * a.h + z] = p.part[j];
+            for (int j = 0; j < Halves<T>::N; ++j) hid[j][z] = p.part[j];
           }
+#pragma unroll
+          for (int j = 0; j < Halves<T>::N; ++j) *reinterpret_cast<quad<T>*>(out + j * a.h) = hid[j];
         } else {
-          *reinterpret_cast<floatx4*>(a.part + ((int64_t)split * a.n * a.k + q) * a.o + c0) = acc[0];
+          const T* b = static_cast<const T*>(a.b2) + (int64_t)e * a.o;
+          if (a.b2 && split == 0)
+#pragma unroll
+            for (int z = 0; z < 4; ++z) acc[0][z] += to_f32(b[c0 + z]);
+          if (a.counts == 0) {
+            const float weight = a.weight[q];
+            quad<T> y;
+#pragma unroll
+            for (int z = 0; z < 4; ++z) y[z] = from_f32<T>(weight * acc[0][z]);
+            *reinterpret_cast<quad<T>*>(static_cast<T*>(a.Y) + (int64_t)q * a.o + c0) = y;
+          } else {
+            store_through(a.part + ((int64_t)split * a.n * a.k + q) * a.o + c0, acc[0]);
+          }
         }
       }
+      __syncthreads();
+    }
+  }
+  if constexpr (LAYER == 2) {
+    if (a.counts == 0) return;
+    if (w == 0) {
+      // this wave's parts have arrived (it alone stores them) before they are counted
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      if (l == 0)
+        s_count = __hip_atomic_fetch_add(&a.count[tile], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
+                  (uint32_t)(slots * splits) - 1;
     }
     __syncthreads();
+    if (!s_count) return;
+    for (int i = threadIdx.x; i < a.n * 4; i += 256) {
+      const int t = i >> 2, c = tile * 16 + 4 * (i & 3);
+      if (c >= a.o) continue;
+      floatx4 y = {0.f, 0.f, 0.f, 0.f};
+      for (int j = 0; j < a.k; ++j) {
+        const int q = t * a.k + j;
+        if (a.chosen[q] < 0) continue;
+        floatx4 v = load_through(a.part + (int64_t)q * a.o + c);
+        for (int s = 1; s < splits; ++s) v += load_through(a.part + ((int64_t)s * a.n * a.k + q) * a.o + c);
+        y += a.weight[q] * v;
+      }
+      quad<T> out;
+#pragma unroll
+      for (int z = 0; z < 4; ++z) out[z] = from_f32<T>(y[z]);
+      *reinterpret_cast<quad<T>*>(static_cast<T*>(a.Y) + (int64_t)t * a.o + c) = out;
+    }
   }
 }
 
-// Y = sum over the choices, in their order, of weight (sum of the splits + b2).
-template <typename T>
-__global__ void __launch_bounds__(256) k_few_combine(FewArgs a) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= (int64_t)a.n * a.o) return;
-  const int t = (int)(i / a.o), c = (int)(i - (int64_t)t * a.o);
-  float y = 0.f;
-  for (int j = 0; j < a.k; ++j) {
-    const int q = t * a.k + j, e = a.chosen[q];
-    if (e < 0) continue;
-    float v = a.b2 ? to_f32(static_cast<const T*>(a.b2)[(int64_t)e * a.o + c]) : 0.f;
-    for (int s = 0; s < a.splits; ++s) v += a.part[((int64_t)s * a.n * a.k + q) * a.o + c];
-    y = fmaf(a.weight[q], v, y);
-  }
-  static_cast<T*>(a.Y)[i] = from_f32<T>(y);
-}
+int64_t few_slots(int64_t n, int k, int K) { return n * k < K ? n * k : K; }
 
+// Splits of the second layer's reduction: where there are fewer workgroups than CUs (one sample, 4096 ->
+// 1024: 64 of them 8.2 us, split in four 5.7).
 int few_splits(const hmoe_few_params_t* p, int64_t n) {
-  const int64_t slots = n * p->top_k < p->K ? n * p->top_k : p->K;
-  const int64_t s = 1024 / (slots * cdiv(p->d_out, 16));
-  return (int)(s < 1 ? 1 : (s > 8 ? 8 : s));
+  const int64_t s = device_cus() / (few_slots(n, p->top_k, p->K) * cdiv(p->d_out, 16)), steps = p->d_hid / 256;
+  const int64_t most = s < steps ? s : steps;
+  return (int)(most < 1 ? 1 : (most > 8 ? 8 : most));
+}
+
+template <typename T, int LAYER, bool GATED>
+int few_layer(const FewArgs& a, hipStream_t st) {
+  const int slots = (int)few_slots(a.n, a.k, a.K), tiles = (int)cdiv(LAYER == 1 ? a.h : a.o, 16);
+  const char* label = LAYER == 1 ? "few layer 1" : "few layer 2";
+  const dim3 grid((unsigned)(slots * tiles * (LAYER == 1 ? 1 : a.splits))), block(256);
+  if (LAYER == 1 && (int64_t)slots * tiles <= 2 * device_cus())
+    HMOE_LAUNCH(label, (k_few_layer<T, LAYER, GATED, (GATED ? 8 : 16)>), grid, block, 0, st, a, tiles, slots);
+  else
+    HMOE_LAUNCH(label, (k_few_layer<T, LAYER, GATED, 4>), grid, block, 0, st, a, tiles, slots);
+  return HMOE_OK;
 }
 
 template <typename T>
 int moe_few_t(const FewArgs& a, bool gated, hipStream_t st) {
-  const int64_t slots = (int64_t)a.n * a.k < a.K ? (int64_t)a.n * a.k : a.K;
-  const int t1 = (int)cdiv(a.h, 16), t2 = (int)cdiv(a.o, 16);
-  HMOE_LAUNCH("few route", k_few_route<T>, dim3(a.n), dim3(64 * kRouteWaves), 0, st, a);
-  if (gated)
-    HMOE_LAUNCH("few layer 1", (k_few_layer<T, 1, true>), dim3((unsigned)(slots * t1)), dim3(256), 0, st, a, t1);
-  else
-    HMOE_LAUNCH("few layer 1", (k_few_layer<T, 1, false>), dim3((unsigned)(slots * t1)), dim3(256), 0, st, a, t1);
-  HMOE_LAUNCH("few layer 2", (k_few_layer<T, 2, false>), dim3((unsigned)(slots * t2 * a.splits)), dim3(256), 0, st, a,
-              t2);
-  HMOE_LAUNCH("few combine", k_few_combine<T>, dim3((unsigned)cdiv((int64_t)a.n * a.o, 256)), dim3(256), 0, st, a);
-  return HMOE_OK;
+  // a router of up to 128 KB in one launch (64 KB: 4.1 us, 512 KB: 13), larger ones in two
+  if (a.K <= kRouteMost && (int64_t)a.K * a.d * sizeof(T) <= (128 << 10)) {
+    HMOE_LAUNCH("few route", k_few_route<T>, dim3(a.n), dim3(64 * kRouteWaves), 0, st, a);
+  } else {
+    HMOE_LAUNCH("few score", k_few_score<T>, dim3((unsigned)cdiv(a.K, 16), (unsigned)cdiv(a.n, 16)),
+                dim3(64 * kScoreWaves), 0, st, a);
+    HMOE_LAUNCH("few choose", k_few_choose<T>, dim3(a.n), dim3(64), 0, st, a);
+  }
+  HMOE_TRY(gated ? few_layer<T, 1, true>(a, st) : few_layer<T, 1, false>(a, st));
+  return few_layer<T, 2, false>(a, st);
 }
 
 void few_carve(const hmoe_few_params_t* p, int64_t n, Workspace& ws, FewArgs& a) {
   const size_t rows = (size_t)n * p->top_k;
   a.splits = few_splits(p, n);
+  const bool parts = p->top_k > 1 || a.splits > 1;
+  a.counts = parts ? (int)cdiv(p->d_out, 16) : 0;
   a.chosen = ws.take<int32_t>(rows);
+  a.score = ws.take<float>((size_t)n * p->K);
   a.hid = ws.take<char>(rows * p->d_hid * 4);  // two bf16 or one fp32
-  a.part = ws.take<float>(rows * p->d_out * a.splits);
+  a.part = ws.take<float>(parts * a.splits * rows * p->d_out);
+  a.count = ws.take<uint32_t>(a.counts);
 }
 
 }  // namespace
@@ -217,7 +338,7 @@ size_t moe_few_ws(const hmoe_few_params_t* p, int64_t n) {
 int launch_moe_few(const hmoe_few_params_t* p, int64_t n, const void* X, int32_t* expert, float* weight, void* Y,
                    Workspace& ws, hipStream_t st) {
   FewArgs a = {X, p->R, p->W1, p->b1, p->W2, p->b2, p->r_bias, (int)n, p->K, p->d_in, p->d_hid, p->d_out, p->top_k,
-               expert, weight, nullptr, nullptr, nullptr, 1, Y};
+               expert, weight, nullptr, nullptr, nullptr, 1, nullptr, nullptr, 0, Y};
   few_carve(p, n, ws, a);
   const bool gated = p->act == HMOE_ACT_SILU_GATED;
   return p->dt == HMOE_BF16 ? moe_few_t<bf16>(a, gated, st) : moe_few_t<float>(a, gated, st);
