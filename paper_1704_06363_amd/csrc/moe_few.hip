@@ -293,7 +293,7 @@ int few_layer(const FewArgs& a, hipStream_t st) {
   const int slots = (int)few_slots(a.n, a.k, a.K), tiles = (int)cdiv(LAYER == 1 ? a.h : a.o, 16);
   const char* label = LAYER == 1 ? "few layer 1" : "few layer 2";
   const dim3 grid((unsigned)(slots * tiles * (LAYER == 1 ? 1 : a.splits))), block(256);
-  if (LAYER == 1 && (int64_t)slots * tiles <= 2 * device_cus())
+  if (LAYER == 1 && (int64_t)slots * tiles <= 2 * device_cus() && a.d > 4 * 8 * (int)(64 / sizeof(T)))
     HMOE_LAUNCH(label, (k_few_layer<T, LAYER, GATED, (GATED ? 8 : 16)>), grid, block, 0, st, a, tiles, slots);
   else
     HMOE_LAUNCH(label, (k_few_layer<T, LAYER, GATED, 4>), grid, block, 0, st, a, tiles, slots);

@@ -198,6 +198,11 @@ def _stream():
     return torch.cuda.current_stream().cuda_stream
 
 
+def _raw_stream(device):
+    """The current stream's handle on `device`, without the Stream object around it (1 us a call)."""
+    return torch._C._cuda_getCurrentRawStream(device.index)
+
+
 def _dt(t):
     try:
         return _DT[t.dtype]
@@ -214,6 +219,37 @@ def _expect(t, shape, dtype, what):
         raise HmoeError(f"{what}: dtype {t.dtype}, {dtype} expected")
     if len(t.shape) != len(shape) or any(e is not None and a != e for a, e in zip(t.shape, shape)):
         raise HmoeError(f"{what}: shape {tuple(t.shape)}, {tuple(shape)} expected")
+
+
+def _arg(t, shape, dtype, what):
+    """The pointer of t (None for None), a contiguous tensor of this shape and dtype; _on_gpu checks the rest.
+    For the calls whose kernels take no longer than a more leisurely check."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape:
+        _expect(t, shape, dtype, what)
+    if not t.is_contiguous():
+        raise HmoeError("tensor is not contiguous")
+    return t.data_ptr()
+
+
+def _on_gpu(*tensors):
+    for t in tensors:
+        if t is not None and not t.is_cuda:
+            raise HmoeError("tensor is not on the GPU")
+
+
+def _out_arg(o, key, shape, dtype, device):
+    """(o[key] or a new tensor, its pointer)."""
+    t = o[key] if key in o else torch.empty(shape, dtype=dtype, device=device)
+    return t, _arg(t, shape, dtype, key)
+
+
+def _ws_arg(ws, nbytes, device):
+    """(pointer, bytes) of ws, or of a new tensor of nbytes() bytes."""
+    if ws is None:
+        ws = torch.empty(nbytes(), dtype=torch.uint8, device=device)
+    return _ptr(ws), ws.numel() * ws.element_size()
 
 
 def _workspace(nbytes, ws, device):
@@ -559,8 +595,6 @@ def topm_hits(idx, row_ptr, tag, q_sample=None, q_tag=None, out=None):
 def _rows_ptr(t, what):
     """(pointer, row stride in elements) of a matrix whose rows are contiguous."""
     n, w = t.shape
-    if not t.is_cuda:
-        raise HmoeError("tensor is not on the GPU")
     if w > 1 and t.stride(1) != 1:
         raise HmoeError(f"{what}: the entries of a row are not contiguous")
     return t.data_ptr(), (t.stride(0) if n > 1 else max(w, 1))
@@ -577,27 +611,29 @@ def token_logprob(logits, token=None, m: int = 0, scale: float = 1.0, anchor=Non
     entropy, lse [n], stat [n, 2] (for token_logprob_backward) and, with m > 0, top_idx [n, m] int32 and
     top_logp [n, m] fp32.  Of these, `out` (a dict) passes buffers; an entry of None is not computed."""
     n, V = logits.shape
-    o = out or {}
+    o = {} if out is None else out
     dev = logits.device
     f32, i32 = torch.float32, torch.int32
     dt = _dt(logits)
-    _expect(token, (n,), i32, "token")
-    _expect(anchor, anchor_shape(n, V), f32, "anchor")
-    r = {}
-    for k, shape, dtype in (("logp", (n,), f32), ("entropy", (n,), f32), ("lse", (n,), f32), ("stat", (n, 2), f32),
-                            ("top_idx", (n, m), i32), ("top_logp", (n, m), f32)):
-        if (k == "logp" and token is None) or (m == 0 and k[0] == "t"):
-            r[k] = None
-        elif k in o:
-            r[k] = o[k]
-            _expect(r[k], shape, dtype, k)
-        else:
-            r[k] = torch.empty(shape, dtype=dtype, device=dev)
+    r = dict.fromkeys(("logp", "top_idx", "top_logp"))
+    logp = idx = tlp = None
+    if token is not None:
+        r["logp"], logp = _out_arg(o, "logp", (n,), f32, dev)
+    r["entropy"], ent = _out_arg(o, "entropy", (n,), f32, dev)
+    r["lse"], lse = _out_arg(o, "lse", (n,), f32, dev)
+    r["stat"], stat = _out_arg(o, "stat", (n, 2), f32, dev)
+    if m > 0:
+        r["top_idx"], idx = _out_arg(o, "top_idx", (n, m), i32, dev)
+        r["top_logp"], tlp = _out_arg(o, "top_logp", (n, m), f32, dev)
+    tok = _arg(token, (n,), i32, "token")
+    anc = None if anchor is None else _arg(anchor, anchor_shape(n, V), f32, "anchor")
     at, ld = _rows_ptr(logits, "logits")
-    w, wb = _workspace(lib().hmoe_token_logprob_workspace(n, V, m, dt), ws, dev)
-    _chk(lib().hmoe_token_logprob(at, ld, _ptr(anchor), dt, n, V, scale, _ptr(token), m, _ptr(r["logp"]),
-                                  _ptr(r["entropy"]), _ptr(r["lse"]), _ptr(r["stat"]), _ptr(r["top_idx"]),
-                                  _ptr(r["top_logp"]), _ptr(w), wb, _stream()), "token_logprob")
+    _on_gpu(logits, token, anchor, *r.values())
+    L = lib()
+    w, wb = _ws_arg(ws, lambda: L.hmoe_token_logprob_workspace(n, V, m, dt), dev)
+    rc = L.hmoe_token_logprob(at, ld, anc, dt, n, V, scale, tok, m, logp, ent, lse, stat, idx, tlp, w, wb, _raw_stream(dev))
+    if rc:
+        _chk(rc, "token_logprob")
     return r
 
 
@@ -608,19 +644,21 @@ def token_logprob_backward(logits, token, stat, entropy=None, g_logp=None, g_ent
     n, V = logits.shape
     f32 = torch.float32
     dt = _dt(logits)
-    _expect(token, (n,), torch.int32, "token")
-    _expect(stat, (n, 2), f32, "stat")
-    for t, k in ((entropy, "entropy"), (g_logp, "g_logp"), (g_entropy, "g_entropy")):
-        _expect(t, (n,), f32, k)
-    _expect(anchor, anchor_shape(n, V), f32, "anchor")
-    _expect(out, (n, V), logits.dtype, "out")
+    tok = _arg(token, (n,), torch.int32, "token")
+    st = _arg(stat, (n, 2), f32, "stat")
+    ent = _arg(entropy, (n,), f32, "entropy")
+    gl, ge = _arg(g_logp, (n,), f32, "g_logp"), _arg(g_entropy, (n,), f32, "g_entropy")
+    anc = None if anchor is None else _arg(anchor, anchor_shape(n, V), f32, "anchor")
     if out is None:
         out = torch.empty((n, V), dtype=logits.dtype, device=logits.device)
+    _expect(out, (n, V), logits.dtype, "out")
     at, ld = _rows_ptr(logits, "logits")
     to, ldo = _rows_ptr(out, "out")
-    _chk(lib().hmoe_token_logprob_backward(at, ld, _ptr(anchor), dt, n, V, scale, _ptr(token), _ptr(stat),
-                                           _ptr(entropy), _ptr(g_logp), _ptr(g_entropy), to, ldo, _stream()),
-         "token_logprob_backward")
+    _on_gpu(logits, token, stat, entropy, g_logp, g_entropy, anchor, out)
+    rc = lib().hmoe_token_logprob_backward(at, ld, anc, dt, n, V, scale, tok, st, ent, gl, ge, to, ldo,
+                                           _raw_stream(logits.device))
+    if rc:
+        _chk(rc, "token_logprob_backward")
     return out
 
 
@@ -635,15 +673,17 @@ def make_few_params(p: dict, top_k: int = 1, act: str = "relu") -> FewParams:
     activation), b1 or None, W2 [K, o, h], b2 [K, o] or None."""
     if act not in _ACT:
         raise HmoeError(f"unknown activation {act!r}")
-    K, o, h = p["W2"].shape
-    dt = p["W1"].dtype
-    d = p["W1"].shape[2]
+    W1, W2 = p["W1"], p["W2"]
+    K, o, h = W2.shape
+    dt = W1.dtype
+    d = W1.shape[2]
     rows = 2 * h if act == "silu" else h
-    for k, shape, t in (("W1", (K, rows, d), dt), ("W2", (K, o, h), dt), ("R", (K, d), dt), ("b1", (K, rows), dt),
-                        ("b2", (K, o), dt), ("r_bias", (K,), torch.float32)):
-        _expect(p.get(k), shape, t, k)
-    return FewParams(K, d, h, o, top_k, _dt(p["W1"]), _ACT[act], _ptr(p["R"]), _ptr(p.get("r_bias")), _ptr(p["W1"]),
-                     _ptr(p.get("b1")), _ptr(p["W2"]), _ptr(p.get("b2")))
+    R, rb, b1, b2 = p["R"], p.get("r_bias"), p.get("b1"), p.get("b2")
+    prm = FewParams(K, d, h, o, top_k, _dt(W1), _ACT[act], _arg(R, (K, d), dt, "R"),
+                    _arg(rb, (K,), torch.float32, "r_bias"), _arg(W1, (K, rows, d), dt, "W1"),
+                    _arg(b1, (K, rows), dt, "b1"), _arg(W2, (K, o, h), dt, "W2"), _arg(b2, (K, o), dt, "b2"))
+    _on_gpu(R, rb, W1, b1, W2, b2)
+    return prm
 
 
 def moe_few_workspace(p, n, top_k: int = 1, act: str = "relu") -> int:
@@ -658,21 +698,23 @@ def moe_few(p, X, top_k: int = 1, act: str = "relu", out=None, ws=None):
     [n, top_k] and weight fp32 [n, top_k]."""
     prm = p if isinstance(p, FewParams) else make_few_params(p, top_k, act)
     n = X.shape[0]
-    dev = X.device
-    o = out or {}
+    dev, dt = X.device, X.dtype
+    o = {} if out is None else out
     if _dt(X) != prm.dt:
-        raise HmoeError(f"X: dtype {X.dtype}, the parameters' expected")
+        raise HmoeError(f"X: dtype {dt}, the parameters' expected")
     k = prm.top_k
-    _expect(X, (n, prm.d_in), None, "X")
-    r = {}
-    for key, shape, dtype in (("Y", (n, prm.d_out), X.dtype), ("expert", (n, k), torch.int32),
-                              ("weight", (n, k), torch.float32)):
-        r[key] = o[key] if key in o else torch.empty(shape, dtype=dtype, device=dev)
-        _expect(r[key], shape, dtype, key)
-    w, wb = _workspace(lib().hmoe_moe_few_workspace(ctypes.byref(prm), n), ws, dev)
-    _chk(lib().hmoe_moe_few(ctypes.byref(prm), n, _ptr(X), _ptr(r["expert"]), _ptr(r["weight"]), _ptr(r["Y"]), _ptr(w),
-                            wb, _stream()), "moe_few")
-    return r
+    Y, y = _out_arg(o, "Y", (n, prm.d_out), dt, dev)
+    expert, e = _out_arg(o, "expert", (n, k), torch.int32, dev)
+    weight, wt = _out_arg(o, "weight", (n, k), torch.float32, dev)
+    x = _arg(X, (n, prm.d_in), dt, "X")
+    _on_gpu(X, Y, expert, weight)
+    ref = ctypes.byref(prm)
+    L = lib()
+    w, wb = _ws_arg(ws, lambda: L.hmoe_moe_few_workspace(ref, n), dev)
+    rc = L.hmoe_moe_few(ref, n, x, e, wt, y, w, wb, _raw_stream(dev))
+    if rc:
+        _chk(rc, "moe_few")
+    return {"Y": Y, "expert": expert, "weight": weight}
 
 
 # ------------------------------------------------------------------ low-rank adapters
@@ -680,20 +722,21 @@ def moe_few(p, X, top_k: int = 1, act: str = "relu", out=None, ws=None):
 def make_lora(p: dict) -> Lora:
     """p: the shared W [o, d] with b [o] or None, the adapters A [E, r, d], B [E, o, r], and scale [E] (fp32) or
     None."""
-    E, r, d = p["A"].shape
-    o = p["W"].shape[0]
-    dt = p["W"].dtype
-    for k, shape, t in (("W", (o, d), dt), ("b", (o,), dt), ("A", (E, r, d), dt), ("B", (E, o, r), dt),
-                        ("scale", (E,), torch.float32)):
-        _expect(p.get(k), shape, t, k)
-    return Lora(E, d, o, r, _dt(p["W"]), _ptr(p["W"]), _ptr(p.get("b")), _ptr(p["A"]), _ptr(p["B"]), _ptr(p.get("scale")))
+    W, A = p["W"], p["A"]
+    E, r, d = A.shape
+    o = W.shape[0]
+    dt = W.dtype
+    B, b, scale = p["B"], p.get("b"), p.get("scale")
+    prm = Lora(E, d, o, r, _dt(W), _arg(W, (o, d), dt, "W"), _arg(b, (o,), dt, "b"), _arg(A, (E, r, d), dt, "A"),
+               _arg(B, (E, o, r), dt, "B"), _arg(scale, (E,), torch.float32, "scale"))
+    _on_gpu(W, b, A, B, scale)
+    return prm
 
 
 def _lora(p, X):
     prm = p if isinstance(p, Lora) else make_lora(p)
     if _dt(X) != prm.dt:
         raise HmoeError(f"X: dtype {X.dtype}, the parameters' expected")
-    _expect(X, (None, prm.d_in), None, "X")
     return prm
 
 
@@ -717,12 +760,18 @@ def lora_few(p, X, adapter, out=None, ws=None):
     id outside [0, E) for none.  p: a dict as in make_lora, or the Lora made from one.  Returns Y [n, o]."""
     prm = _lora(p, X)
     n = X.shape[0]
-    _expect(adapter, (n,), torch.int32, "adapter")
+    dev = X.device
     if out is None:
-        out = torch.empty((n, prm.d_out), dtype=X.dtype, device=X.device)
-    _expect(out, (n, prm.d_out), X.dtype, "out")
-    w, wb = _workspace(lib().hmoe_lora_few_workspace(ctypes.byref(prm), n), ws, X.device)
-    _chk(lib().hmoe_lora_few(ctypes.byref(prm), n, _ptr(X), _ptr(adapter), _ptr(out), _ptr(w), wb, _stream()), "lora_few")
+        out = torch.empty((n, prm.d_out), dtype=X.dtype, device=dev)
+    x, a = _arg(X, (n, prm.d_in), X.dtype, "X"), _arg(adapter, (n,), torch.int32, "adapter")
+    y = _arg(out, (n, prm.d_out), X.dtype, "out")
+    _on_gpu(X, adapter, out)
+    ref = ctypes.byref(prm)
+    L = lib()
+    w, wb = _ws_arg(ws, lambda: L.hmoe_lora_few_workspace(ref, n), dev)
+    rc = L.hmoe_lora_few(ref, n, x, a, y, w, wb, _raw_stream(dev))
+    if rc:
+        _chk(rc, "lora_few")
     return out
 
 
@@ -732,18 +781,20 @@ def lora_forward(p, X_sorted, offsets, perm=None, out=None, ws=None):
     Returns Y [n, o] in sample order and U, which lora_backward needs."""
     prm = _lora(p, X_sorted)
     n = X_sorted.shape[0]
-    o = out or {}
-    dt = X_sorted.dtype
-    _expect(offsets, (prm.E + 1,), torch.int32, "offsets")
-    _expect(perm, (n,), torch.int32, "perm")
-    r = {}
-    for k, shape in (("Y", (n, prm.d_out)), ("U", (n, lib().hmoe_lora_saved_width(prm.rank, prm.dt)))):
-        r[k] = o[k] if k in o else torch.empty(shape, dtype=dt, device=X_sorted.device)
-        _expect(r[k], shape, dt, k)
-    w, wb = _workspace(lib().hmoe_lora_workspace(ctypes.byref(prm), n), ws, X_sorted.device)
-    _chk(lib().hmoe_lora_forward(ctypes.byref(prm), n, _ptr(X_sorted), _ptr(offsets), _ptr(perm), _ptr(r["U"]),
-                                 _ptr(r["Y"]), _ptr(w), wb, _stream()), "lora_forward")
-    return r
+    o = {} if out is None else out
+    dt, dev, i32 = X_sorted.dtype, X_sorted.device, torch.int32
+    L = lib()
+    Y, y = _out_arg(o, "Y", (n, prm.d_out), dt, dev)
+    U, u = _out_arg(o, "U", (n, L.hmoe_lora_saved_width(prm.rank, prm.dt)), dt, dev)
+    x = _arg(X_sorted, (n, prm.d_in), dt, "X_sorted")
+    off, pm = _arg(offsets, (prm.E + 1,), i32, "offsets"), _arg(perm, (n,), i32, "perm")
+    _on_gpu(X_sorted, offsets, perm, Y, U)
+    ref = ctypes.byref(prm)
+    w, wb = _ws_arg(ws, lambda: L.hmoe_lora_workspace(ref, n), dev)
+    rc = L.hmoe_lora_forward(ref, n, x, off, pm, u, y, w, wb, _raw_stream(dev))
+    if rc:
+        _chk(rc, "lora_forward")
+    return {"Y": Y, "U": U}
 
 
 def lora_backward(p, X_sorted, offsets, dY, U, perm=None, want_dX=True, want_adapters=True, out=None, ws=None):
@@ -751,23 +802,26 @@ def lora_backward(p, X_sorted, offsets, dY, U, perm=None, want_dX=True, want_ada
     order, from dY [n, o] in sample order and the forward's U.  W, b and scale are fixed."""
     prm = _lora(p, X_sorted)
     n = X_sorted.shape[0]
-    o = out or {}
-    dt, dev, f32 = X_sorted.dtype, X_sorted.device, torch.float32
-    _expect(offsets, (prm.E + 1,), torch.int32, "offsets")
-    _expect(perm, (n,), torch.int32, "perm")
-    _expect(dY, (n, prm.d_out), dt, "dY")
-    _expect(U, (n, lib().hmoe_lora_saved_width(prm.rank, prm.dt)), dt, "U")
-    r = {}
-    for k, want, shape, t in (("dX", want_dX, (n, prm.d_in), dt), ("dA", want_adapters, (prm.E, prm.rank, prm.d_in), f32),
-                              ("dB", want_adapters, (prm.E, prm.d_out, prm.rank), f32)):
-        r[k] = None
-        if want:
-            r[k] = o[k] if k in o else torch.empty(shape, dtype=t, device=dev)
-            _expect(r[k], shape, t, k)
-    w, wb = _workspace(lib().hmoe_lora_workspace(ctypes.byref(prm), n), ws, dev)
-    _chk(lib().hmoe_lora_backward(ctypes.byref(prm), n, _ptr(X_sorted), _ptr(offsets), _ptr(perm), _ptr(U), _ptr(dY),
-                                  _ptr(r["dX"]), _ptr(r["dA"]), _ptr(r["dB"]), _ptr(w), wb, _stream()), "lora_backward")
-    return r
+    o = {} if out is None else out
+    dt, dev, f32, i32 = X_sorted.dtype, X_sorted.device, torch.float32, torch.int32
+    L = lib()
+    dX = dA = dB = gx = ga = gb = None
+    if want_dX:
+        dX, gx = _out_arg(o, "dX", (n, prm.d_in), dt, dev)
+    if want_adapters:
+        dA, ga = _out_arg(o, "dA", (prm.E, prm.rank, prm.d_in), f32, dev)
+        dB, gb = _out_arg(o, "dB", (prm.E, prm.d_out, prm.rank), f32, dev)
+    x = _arg(X_sorted, (n, prm.d_in), dt, "X_sorted")
+    off, pm = _arg(offsets, (prm.E + 1,), i32, "offsets"), _arg(perm, (n,), i32, "perm")
+    u = _arg(U, (n, L.hmoe_lora_saved_width(prm.rank, prm.dt)), dt, "U")
+    dy = _arg(dY, (n, prm.d_out), dt, "dY")
+    _on_gpu(X_sorted, offsets, perm, U, dY, dX, dA, dB)
+    ref = ctypes.byref(prm)
+    w, wb = _ws_arg(ws, lambda: L.hmoe_lora_workspace(ref, n), dev)
+    rc = L.hmoe_lora_backward(ref, n, x, off, pm, u, dy, gx, ga, gb, w, wb, _raw_stream(dev))
+    if rc:
+        _chk(rc, "lora_backward")
+    return {"dX": dX, "dA": dA, "dB": dB}
 
 
 # ------------------------------------------------------------------ parameter update
