@@ -238,21 +238,24 @@ __global__ void __launch_bounds__(256) k_token_logprob(LogprobArgs a) {
         float best = cm[0];
 #pragma unroll
         for (int u = 1; u < U; ++u) best = fmaxf(best, cm[u]);
-        uint64_t k = (uint64_t)sortable(best) << 32;
-        wave_sort(k, true);
-        top.floor = lane_value(k, a.m - 1);
+        top.floor = (uint64_t)sortable(mth_lane_value(best, a.m, l)) << 32;
       }
-      const float floor_v = top.floor == 0 ? -INFINITY : key_value(top.floor);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
+        const float floor_v = top.floor == 0 ? -INFINITY : key_value(top.floor);
         if (__ballot(start ? cm[u] >= floor_v : cm[u] > floor_v) == 0) continue;
+        // the lanes' entries that may enter, one of each lane at a time
         const int v = b + 64 * u + l;
-#pragma clang loop unroll(disable)
-        for (int z = 0; z < N; ++z) {
+        uint32_t bits = 0;
+#pragma unroll
+        for (int z = 0; z < N; ++z) bits |= ((start ? f[u][z] >= floor_v : f[u][z] > floor_v) && v < end ? 1u : 0u) << z;
+        while (__ballot(bits != 0) != 0) {
+          const int z = __builtin_ctz(bits | 256u);
           float y = f[u][0];
 #pragma unroll
           for (int q = 1; q < N; ++q) y = z == q ? f[u][q] : y;
-          top.add(y, (uint32_t)(v * N + z), v < end, buf, a.m);
+          top.add(y, (uint32_t)(v * N + z), bits != 0, buf, a.m);
+          bits &= bits - 1;
         }
       }
     }
@@ -304,17 +307,25 @@ __global__ void __launch_bounds__(256) k_token_logprob(LogprobArgs a) {
   }
 }
 
-// The pieces of a row joined, a wave to a row.
+// The pieces of a row joined, a workgroup to a row: the waves sort the keys 64 at a time, the first the best
+// of theirs.
 template <typename T, bool ANC>
-__global__ void __launch_bounds__(64) k_logprob_join(LogprobArgs a) {
-  const int l = threadIdx.x;
+__global__ void __launch_bounds__(256) k_logprob_join(LogprobArgs a) {
+  __shared__ uint64_t s_key[4][kLpTop];
+  const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int64_t row = a.row0 + blockIdx.x;
+  const int keys = a.pieces * a.m;
   const float c2 = a.scale * kLog2e;
+  uint64_t best = 0;
+  for (int b = 64 * w; b < keys; b += 256) wave_merge(best, b + l < keys ? a.part_key[row * keys + b + l] : 0);
+  if (l < kLpTop) s_key[w][l] = best;
+  __syncthreads();
+  if (w != 0) return;
   RowSums r;
   r.clear();
-  for (int p = l; p < a.pieces; p += 64) {
-    const Piece q = a.part[row * a.pieces + p];
-    r.join(RowSums{q.M, q.S, q.T}, c2);
+  if (l < a.pieces) {
+    const Piece q = a.part[row * a.pieces + l];
+    r = RowSums{q.M, q.S, q.T};
   }
   float M = r.M;
 #pragma unroll
@@ -322,9 +333,10 @@ __global__ void __launch_bounds__(64) k_logprob_join(LogprobArgs a) {
   r.raise(M, c2);
   r.S = wave_sum(r.S);
   r.T = wave_sum(r.T);
-  uint64_t best = 0;
-  const int keys = a.pieces * a.m;
-  for (int b = 0; b < keys; b += 64) wave_merge(best, b + l < keys ? a.part_key[row * keys + b + l] : 0);
+  if (keys > 64) {
+    best = s_key[l / kLpTop][l % kLpTop];
+    wave_sort(best, true);
+  }
   finish_row<T, ANC>(a, row, r, best);
 }
 
@@ -433,7 +445,7 @@ int logprob_t(LogprobArgs a, hipStream_t st) {
       HMOE_LAUNCH("token logprob", (k_token_logprob<T, ANC, TOP, 4>), dim3((unsigned)(rows * a.pieces)), block, 0, st,
                   a);
     if (a.pieces > 1)
-      HMOE_LAUNCH("token logprob join", (k_logprob_join<T, ANC>), dim3((unsigned)rows), dim3(64), 0, st, a);
+      HMOE_LAUNCH("token logprob join", (k_logprob_join<T, ANC>), dim3((unsigned)rows), block, 0, st, a);
     return (int)HMOE_OK;
   });
 }
