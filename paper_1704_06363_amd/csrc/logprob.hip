@@ -11,8 +11,8 @@
 //
 // The alternatives: a wave keeps a bound on its m-th best entry, lists what is above it in LDS, and sorts the
 // list 64 keys at a time (lanes.hpp).  The first bound is the m-th largest of the lanes' maxima over
-// the first step, which m entries reach; later entries have larger indexes, so only strictly
-// larger ones enter.
+// the first step, which m entries reach; the best of the row's waves' bounds is everyone's, so that the
+// waves with the tail of a vocabulary in order of frequency list next to nothing.
 //
 // Bound: HBM, the logits are read once (a bf16 entry costs 10 to 11 vector cycles of a lane, which
 // 256 CUs have time for at 7 TB/s).
@@ -106,6 +106,16 @@ struct TopList {
     const uint64_t last = lane_value(best, m - 1);
     floor = last > floor ? last : floor;
   }
+  // A bound found by another wave of the row: entries equal to it may still be among the m best.
+  __device__ __forceinline__ void raise_to(uint32_t value) {
+    const uint64_t k = (uint64_t)value << 32;
+    floor = k > floor ? k : floor;
+  }
+  // Entries not above this are not listed (of -inf none are: finish_row finds those).
+  __device__ __forceinline__ float below() const {
+    const uint32_t hi = (uint32_t)(floor >> 32) - ((uint32_t)floor == 0 ? 1u : 0u);
+    return (uint32_t)(floor >> 32) <= kKeyMinusInf ? -INFINITY : key_value((uint64_t)hi << 32);
+  }
   // Lists the lanes' entries x at `index` that are `in` and above the floor.
   __device__ __forceinline__ void add(float x, uint32_t index, bool in, lds<uint64_t>* buf, int m) {
     const uint64_t key = rank_key(x, index);
@@ -172,6 +182,11 @@ __global__ void __launch_bounds__(256) k_token_logprob(LogprobArgs a) {
   constexpr int N = RowVec<T>::N, U = kLpUnroll;
   __shared__ uint64_t s_list[TOP ? 4 : 1][TOP ? kLpList : 1];
   __shared__ float s_sum[4][3];
+  __shared__ uint32_t s_floor[1];
+  if constexpr (TOP && W > 1) {
+    if (threadIdx.x == 0) *s_floor = 0;
+    __syncthreads();
+  }
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int64_t job = a.row0 * a.pieces + (int64_t)blockIdx.x * (4 / W) + w / W;
   const int64_t row = job / a.pieces;
@@ -189,31 +204,43 @@ __global__ void __launch_bounds__(256) k_token_logprob(LogprobArgs a) {
   TopList top;
   Vec raw[U];
   float an[U];
-  const auto load = [&](int b) {
+  const int step = 64 * U * W, b0 = first + (w % W) * 64 * U;
+  // 64 vectors are whole tiles of anchors, so this lane's move by the same distance with each
+  constexpr int TILES = 64 * N / kAnchorTile;
+  const int64_t tile = a.n * kAnchorSlots;
+  const float* anc = nullptr;
+  if constexpr (ANC) anc = a.anc + anchor_index(a.n, row, (int64_t)(b0 + l) * N);
+  const auto load = [&](int b) {  // each step once, in order
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int v = b + 64 * u + l;
       if (v < end) {
         raw[u] = *reinterpret_cast<const Vec*>(x + (int64_t)v * N);
-        if constexpr (ANC) an[u] = a.anc[anchor_index(a.n, row, (int64_t)v * N)];
+        if constexpr (ANC) an[u] = anc[u * TILES * tile];
       }
     }
+    if constexpr (ANC) anc += U * W * TILES * tile;
   };
-  const int step = 64 * U * W, b0 = first + (w % W) * 64 * U;
   if (b0 < end) load(b0);
   for (int b = b0; b < end; b += step) {
-    float f[U][N], cm[U];
+    // stored values, the anchors that are added to them, and each vector's largest entry
+    float f[U][N], base[U], cm[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const bool in = b + 64 * u + l < end;
-      const T* e = reinterpret_cast<const T*>(&raw[u]);
-      cm[u] = -INFINITY;
+      constexpr int kNone = sizeof(T) == 2 ? (int)0xff80ff80u : (int)0xff800000u;  // -inf
+      i32x4 q = raw[u];
 #pragma unroll
-      for (int z = 0; z < N; ++z) {
-        const float y = ANC ? an[u] + to_f32(e[z]) : to_f32(e[z]);
-        f[u][z] = in ? y : -INFINITY;
-        cm[u] = fmaxf(cm[u], f[u][z]);
+      for (int i = 0; i < 4; ++i) q[i] = in ? q[i] : kNone;
+      const T* e = reinterpret_cast<const T*>(&q);
+      base[u] = ANC && in ? an[u] : 0.f;
+      f[u][0] = cm[u] = to_f32(e[0]);
+#pragma unroll
+      for (int z = 1; z < N; ++z) {
+        f[u][z] = to_f32(e[z]);
+        cm[u] = max_of(cm[u], f[u][z]);
       }
+      cm[u] = ANC ? base[u] + cm[u] : cm[u];
     }
     if (b + step < end) load(b + step);
     float mx = r.M;
@@ -222,33 +249,39 @@ __global__ void __launch_bounds__(256) k_token_logprob(LogprobArgs a) {
     r.raise(mx, c2);
     float S = 0.f, Tn = 0.f;
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int u = 0; u < U; ++u) {
+      const float ref = ANC ? mx - base[u] : mx;
 #pragma unroll
       for (int z = 0; z < N; ++z) {
-        const float d = f[u][z] - mx;
+        const float d = f[u][z] - ref;
         const float e = __builtin_amdgcn_exp2f(d * c2);
         S += e;
         Tn = fmaf(e, fmaxf(d, -FLT_MAX), Tn);
       }
+    }
     r.S += S;
     r.T += Tn;
     if constexpr (TOP) {
-      const bool start = b == b0;
-      if (start) {  // the m-th largest of the lanes' maxima
+      if (b == b0) {  // the m-th largest of the lanes' maxima
         float best = cm[0];
 #pragma unroll
         for (int u = 1; u < U; ++u) best = fmaxf(best, cm[u]);
         top.floor = (uint64_t)sortable(mth_lane_value(best, a.m, l)) << 32;
+        if (W > 1 && l == 0) atomicMax(s_floor, (uint32_t)(top.floor >> 32));
       }
+      if (W > 1) top.raise_to(*(volatile uint32_t*)s_floor);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const float floor_v = top.floor == 0 ? -INFINITY : key_value(top.floor);
-        if (__ballot(start ? cm[u] >= floor_v : cm[u] > floor_v) == 0) continue;
+        const float below = top.below();
+        if (__ballot(cm[u] > below) == 0) continue;
+        if constexpr (ANC)
+#pragma unroll
+          for (int z = 0; z < N; ++z) f[u][z] += base[u];  // the entries, as fp32 sums
         // the lanes' entries that may enter, one of each lane at a time
         const int v = b + 64 * u + l;
         uint32_t bits = 0;
 #pragma unroll
-        for (int z = 0; z < N; ++z) bits |= ((start ? f[u][z] >= floor_v : f[u][z] > floor_v) && v < end ? 1u : 0u) << z;
+        for (int z = 0; z < N; ++z) bits |= (f[u][z] > below && v < end ? 1u : 0u) << z;
         while (__ballot(bits != 0) != 0) {
           const int z = __builtin_ctz(bits | 256u);
           float y = f[u][0];
@@ -369,12 +402,14 @@ __global__ void __launch_bounds__(256) k_logprob_grad(LogprobGrad a) {
   const int v0 = chunk * 256 * U + threadIdx.x;
   Vec raw[U];
   float an[U];
+  const float* anc = nullptr;
+  if constexpr (ANC) anc = a.anc + anchor_index(a.n, row, (int64_t)v0 * N);
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int v = v0 + 256 * u;
     if (v < nvec) {
       raw[u] = *reinterpret_cast<const Vec*>(x + (int64_t)v * N);
-      if constexpr (ANC) an[u] = a.anc[anchor_index(a.n, row, (int64_t)v * N)];
+      if constexpr (ANC) an[u] = anc[u * (256 * N / kAnchorTile) * a.n * kAnchorSlots];
     }
   }
   const float M = a.stat[2 * row], ls = a.stat[2 * row + 1];
