@@ -70,6 +70,7 @@ enum {
 
 #define HMOE_FEW_ROWS 64  /* most rows of the entry points for a few of them */
 #define HMOE_FEW_EXPERTS 8 /* most experts of a sample */
+#define HMOE_FEW_WIDTH (1 << 20) /* largest d_in, d_hid and d_out */
 
 /* A mixture layer that routes by itself.  R [K][d_in] the router's rows, r_bias float[K] or NULL; W2
  * [K][d_out][d_hid], b2 [K][d_out]; biases may be NULL; matrices and biases in dtype dt.

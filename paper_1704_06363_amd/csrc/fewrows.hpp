@@ -8,6 +8,8 @@ namespace hmoe {
 template <typename T>
 using quad = T __attribute__((ext_vector_type(4)));
 
+__device__ __forceinline__ int uniform_int(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
 // acc += A B^T over one step of 64 bytes of K: lane l holds 16 bytes (bf16: 8, fp32: 4 elements) of
 // row l % 16 at byte 16 (l / 16) of the step.  Lane l of acc has rows 4 (l / 16) .. + 3 of A against row l % 16 of B.
 template <typename T>
@@ -22,40 +24,101 @@ __device__ __forceinline__ void step_mfma(i32x4 a, i32x4 b, floatx4& acc) {
   }
 }
 
-// body(wv, xv) for the steps s0 <= s < s1 of a reduction over kd elements, with this lane's 16 bytes of the
-// rows at w and x.  The loads of U steps go out together: under a bound on K of their own (which the
-// compiler does not move loads across) they ran one step at a time.  kd is a multiple of 8: past it, in
-// the last step, both operands are zeros.
-template <typename T, int U, int MI, int NX, class Body>
-__device__ __forceinline__ void stream_steps(const T* const (&w)[MI], const T* const (&x)[NX], int kd, int s0, int s1,
-                                             Body body) {
-  constexpr int N = 16 / sizeof(T), STEP = 4 * N;
-  const int lg = (threadIdx.x & 63) >> 4;
-  const int ragged = kd % STEP ? kd / STEP : -1;  // the step with less than STEP elements
-  for (int s = s0; s < s1; s += U) {
-    i32x4 wv[U][MI], xv[U][NX];
+// v[f] of lane 4 i + q becomes v[q] of lane 4 i + f, for each of the four dwords.
+__device__ __forceinline__ void quad_transpose(i32x4 (&v)[4]) {
+  const bool odd = threadIdx.x & 1, high = threadIdx.x & 2;
+  // every lane takes part in the moves, whichever value it keeps
+  const auto pick1 = [&](bool other, int x, int mine) {
+    const int o = __builtin_amdgcn_update_dpp(0, x, 0xB1, 0xf, 0xf, true);
+    return other ? o : mine;
+  };
+  const auto pick2 = [&](bool other, int x, int mine) {
+    const int o = __builtin_amdgcn_update_dpp(0, x, 0x4E, 0xf, 0xf, true);
+    return other ? o : mine;
+  };
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int at = (s + u < s1 ? s + u : s1 - 1) * STEP + lg * N;
-      const int in = at < kd ? at : kd - N;
+  for (int d = 0; d < 4; ++d) {
+    const int a0 = v[0][d], a1 = v[1][d], a2 = v[2][d], a3 = v[3][d];
+    const int b0 = pick1(odd, a1, a0), b1 = pick1(!odd, a0, a1);
+    const int b2 = pick1(odd, a3, a2), b3 = pick1(!odd, a2, a3);
+    v[0][d] = pick2(high, b2, b0);
+    v[2][d] = pick2(!high, b0, b2);
+    v[1][d] = pick2(high, b3, b1);
+    v[3][d] = pick2(!high, b1, b3);
+  }
+}
+
+// The reduction runs over groups of 256 bytes of K, four MFMA steps.  In load f of a group this lane takes 16
+// bytes of row group_row(f) of the tile at byte 16 group_chunk(): four rows of 256 contiguous bytes to a
+// load, where adjacent lanes read adjacent bytes.  After quad_transpose register f has row l % 16, chunk
+// 4 (l / 16) + f -- an MFMA operand, the lane groups' chunks standing for other places of K than
+// usual, the same ones for both operands.  (Loaded as the MFMA holds them, adjacent lanes are in different
+// rows and every lane's 16 bytes are a request of their own, 64 cycles of the CU's address unit
+// for a load instead of 16: that alone was 52 of the 54 us of 48 rows against 50000 columns of 1024 with 16
+// adapters.)
+__device__ __forceinline__ int group_row(int f) { return (threadIdx.x & 12) + f; }
+__device__ __forceinline__ int group_chunk() { return ((threadIdx.x & 48) >> 2) + (threadIdx.x & 3); }
+template <typename T>
+__host__ __device__ constexpr int group_size() {  // elements of K
+  return 256 / (int)sizeof(T);
+}
+template <typename T>
+__host__ __device__ inline int groups_of(int kd) {
+  return (kd + group_size<T>() - 1) / group_size<T>();
+}
+
+// body(wv, xv) with the operands of each step of the groups g0 <= g < g1.  wo and xo: byte offsets from the
+// tiles' wb, and from xb, of this lane's row of load f (kd elements from there); below 2^32.  The loads of UG groups go out together.  kd is a
+// multiple of 8: past it, in the last group, both operands are zeros.
+template <typename T, int UG, int MI, int NX, class Body>
+__device__ __forceinline__ void stream_groups(const T* const (&wb)[MI], const uint32_t (&wo)[MI][4], const T* xb,
+                                              const uint32_t (&xo)[NX][4], int kd, int g0, int g1, Body body) {
+  constexpr int N = 16 / sizeof(T), GROUP = group_size<T>();
+  const int own = group_chunk() * N;
+  const char* xc = reinterpret_cast<const char*>(xb);
+  for (int g = g0; g < g1; g += UG) {
+    i32x4 wv[UG][MI][4], xv[UG][NX][4];
 #pragma unroll
-      for (int i = 0; i < MI; ++i) wv[u][i] = *reinterpret_cast<const i32x4*>(w[i] + in);
+    for (int u = 0; u < UG; ++u) {
+      const int at = (g + u < g1 ? g + u : g1 - 1) * GROUP + own;
+      const uint32_t in = (at < kd ? at : 0) * (uint32_t)sizeof(T);
 #pragma unroll
-      for (int j = 0; j < NX; ++j) xv[u][j] = *reinterpret_cast<const i32x4*>(x[j] + in);
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int f = 0; f < 4; ++f) wv[u][i][f] = *reinterpret_cast<const i32x4*>(reinterpret_cast<const char*>(wb[i]) + (wo[i][f] + in));
+#pragma unroll
+      for (int j = 0; j < NX; ++j)
+#pragma unroll
+        for (int f = 0; f < 4; ++f) xv[u][j][f] = *reinterpret_cast<const i32x4*>(xc + (xo[j][f] + in));
     }
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (s + u >= s1) break;
-      if (s + u == ragged) {
-        const bool out = ragged * STEP + lg * N >= kd;
+    for (int u = 0; u < UG; ++u) {
+      if (g + u >= g1) break;
+      if ((g + u + 1) * GROUP > kd) {
+        const bool out = (g + u) * GROUP + own >= kd;
 #pragma unroll
-        for (int i = 0; i < MI; ++i)
-          if (out) wv[u][i] = i32x4{0, 0, 0, 0};
+        for (int f = 0; f < 4; ++f) {
 #pragma unroll
-        for (int j = 0; j < NX; ++j)
-          if (out) xv[u][j] = i32x4{0, 0, 0, 0};
+          for (int i = 0; i < MI; ++i)
+            if (out) wv[u][i][f] = i32x4{0, 0, 0, 0};
+#pragma unroll
+          for (int j = 0; j < NX; ++j)
+            if (out) xv[u][j][f] = i32x4{0, 0, 0, 0};
+        }
       }
-      body(wv[u], xv[u]);
+#pragma unroll
+      for (int i = 0; i < MI; ++i) quad_transpose(wv[u][i]);
+#pragma unroll
+      for (int j = 0; j < NX; ++j) quad_transpose(xv[u][j]);
+#pragma unroll
+      for (int f = 0; f < 4; ++f) {
+        i32x4 a[MI], x[NX];
+#pragma unroll
+        for (int i = 0; i < MI; ++i) a[i] = wv[u][i][f];
+#pragma unroll
+        for (int j = 0; j < NX; ++j) x[j] = xv[u][j][f];
+        body(a, x);
+      }
     }
   }
 }

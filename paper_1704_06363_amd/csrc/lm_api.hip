@@ -81,6 +81,8 @@ static int check_few(const hmoe_few_params_t* p, int64_t n) {
   HMOE_TRY(check_width("d_in", p->d_in));
   HMOE_TRY(check_width("d_hid", p->d_hid));
   HMOE_TRY(check_width("d_out", p->d_out));
+  for (int32_t w : {p->d_in, p->d_hid, p->d_out})
+    if (w > HMOE_FEW_WIDTH) return fail(HMOE_EINVAL, "width %d exceeds %d", w, HMOE_FEW_WIDTH);
   if (p->top_k < 1 || p->top_k > HMOE_FEW_EXPERTS || p->top_k > p->K)
     return fail(HMOE_EINVAL, "top_k = %d outside [1, min(%d, K)]", p->top_k, HMOE_FEW_EXPERTS);
   if (p->act != HMOE_ACT_RELU && p->act != HMOE_ACT_SILU_GATED) return fail(HMOE_EINVAL, "unknown act %d", p->act);

@@ -99,23 +99,31 @@ struct LoraFew {
 constexpr int kFewShrinkWaves = 8;
 template <typename T>
 __global__ void __launch_bounds__(64 * kFewShrinkWaves) k_lora_few_shrink(LoraFew a) {
-  constexpr int STEP = 64 / sizeof(T), NW = kFewShrinkWaves;
+  constexpr int NW = kFewShrinkWaves;
   __shared__ int s_group, s_count, s_rows[HMOE_FEW_ROWS];
   __shared__ floatx4 s_acc[NW][64];
   const int blocks = u_blocks(a.rank), kb = blockIdx.x % blocks;
   if (!few_group<64 * NW>(a.adapter, a.n, a.E, blockIdx.x / blocks, &s_group, s_rows, &s_count)) return;
   const int e = s_group, count = s_count, ldu = u_width<T>(a.rank);
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6, lr = l & 15, lg = l >> 4;
-  const int r = 16 * kb + lr < a.rank ? 16 * kb + lr : a.rank - 1;
-  const T* A = static_cast<const T*>(a.A) + ((int64_t)e * a.rank + r) * a.d;
-  const int steps = (a.d + STEP - 1) / STEP, s0 = steps * w / NW, s1 = steps * (w + 1) / NW;
+  const T* A = static_cast<const T*>(a.A) + ((int64_t)uniform_int(e) * a.rank + 16 * kb) * a.d;
+  uint32_t ao[1][4];
+#pragma unroll
+  for (int f = 0; f < 4; ++f) {
+    const int r = group_row(f);
+    ao[0][f] = (uint32_t)(16 * kb + r < a.rank ? r : a.rank - 1 - 16 * kb) * a.d * sizeof(T);
+  }
+  const int groups = groups_of<T>(a.d), g0 = groups * w / NW, g1 = groups * (w + 1) / NW;
   const float scale = a.scale ? a.scale[e] : 1.f;
   for (int t0 = 0; t0 < count; t0 += 16) {
-    const int row = s_rows[t0 + lr < count ? t0 + lr : count - 1];
-    const T* x = static_cast<const T*>(a.X) + (int64_t)row * a.d;
+    const auto row_of = [&](int i) { return s_rows[t0 + i < count ? t0 + i : count - 1]; };
+    const int row = row_of(lr);
+    uint32_t xo[1][4];
+#pragma unroll
+    for (int f = 0; f < 4; ++f) xo[0][f] = (uint32_t)row_of(group_row(f)) * a.d * sizeof(T);
     floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-    stream_steps<T, 8>({A}, {x}, a.d, s0, s1,
-                       [&](const i32x4(&av)[1], const i32x4(&xv)[1]) { step_mfma<T>(av[0], xv[0], acc); });
+    stream_groups<T, 2>({A}, ao, static_cast<const T*>(a.X), xo, a.d, g0, g1,
+                        [&](const i32x4(&av)[1], const i32x4(&xv)[1]) { step_mfma<T>(av[0], xv[0], acc); });
     s_acc[w][l] = acc;
     __syncthreads();
     if (w == 0 && t0 + lr < count) {
@@ -131,24 +139,30 @@ __global__ void __launch_bounds__(64 * kFewShrinkWaves) k_lora_few_shrink(LoraFe
 // 16 MI columns of Y for all rows (16 NT at most); the waves split d, and the adapters of the rows.
 template <typename T, int MI, int NT>
 __global__ void __launch_bounds__(256) k_lora_few(LoraFew a) {
-  constexpr int STEP = 64 / sizeof(T);
   __shared__ floatx4 s_acc[4][MI][NT][64];
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6, lr = l & 15, lg = l >> 4;
   const int c0 = blockIdx.x * 16 * MI;
   const T* W[MI];
-  int col[MI];
+  uint32_t wo[MI][4], xo[NT][4];
+  int col[MI], row[NT], mine[NT];
 #pragma unroll
   for (int i = 0; i < MI; ++i) {
-    col[i] = c0 + 16 * i + lr < a.o ? c0 + 16 * i + lr : a.o - 1;
-    W[i] = static_cast<const T*>(a.W) + (int64_t)col[i] * a.d;
+    const int ci = c0 + 16 * i < a.o ? c0 + 16 * i : a.o - 1;  // a tile past the columns repeats the last
+    col[i] = ci + lr < a.o ? ci + lr : a.o - 1;
+    W[i] = static_cast<const T*>(a.W) + (int64_t)ci * a.d;
+#pragma unroll
+    for (int f = 0; f < 4; ++f)
+      wo[i][f] = (uint32_t)(ci + group_row(f) < a.o ? group_row(f) : a.o - 1 - ci) * a.d * sizeof(T);
   }
-  const T* x[NT];
-  int row[NT], mine[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     row[t] = 16 * t + lr < a.n ? 16 * t + lr : a.n - 1;
-    x[t] = static_cast<const T*>(a.X) + (int64_t)row[t] * a.d;
     mine[t] = a.adapter[row[t]];
+#pragma unroll
+    for (int f = 0; f < 4; ++f) {
+      const int r = 16 * t + group_row(f);
+      xo[t][f] = (uint32_t)(r < a.n ? r : a.n - 1) * a.d * sizeof(T);
+    }
   }
   const int all = a.adapter[l < a.n ? l : a.n - 1];  // a lane to a row
   floatx4 acc[MI][NT];
@@ -156,13 +170,14 @@ __global__ void __launch_bounds__(256) k_lora_few(LoraFew a) {
   for (int i = 0; i < MI; ++i)
 #pragma unroll
     for (int t = 0; t < NT; ++t) acc[i][t] = floatx4{0.f, 0.f, 0.f, 0.f};
-  const int steps = (a.d + STEP - 1) / STEP, s0 = steps * w / 4, s1 = steps * (w + 1) / 4;
-  stream_steps<T, 4>(W, x, a.d, s0, s1, [&](const i32x4(&wv)[MI], const i32x4(&xv)[NT]) {
+  const int groups = groups_of<T>(a.d);
+  stream_groups<T, (MI * NT > 1 ? 1 : 4)>(W, wo, static_cast<const T*>(a.X), xo, a.d, groups * w / 4, groups * (w + 1) / 4,
+                                          [&](const i32x4(&wv)[MI], const i32x4(&xv)[NT]) {
 #pragma unroll
-    for (int i = 0; i < MI; ++i)
+                                            for (int i = 0; i < MI; ++i)
 #pragma unroll
-      for (int t = 0; t < NT; ++t) step_mfma<T>(wv[i], xv[t], acc[i][t]);
-  });
+                                              for (int t = 0; t < NT; ++t) step_mfma<T>(wv[i], xv[t], acc[i][t]);
+                                          });
   // the adapters in the order of their first rows, one to a wave in turn
   uint64_t left = __ballot(l < a.n && all >= 0 && all < a.E);
   const int ldu = u_width<T>(a.rank), blocks = u_blocks(a.rank);
@@ -244,7 +259,6 @@ template <typename T, int RT, int MT>
 __global__ void __launch_bounds__(256) k_lora_shrink(const T* __restrict__ X, int K, const T* __restrict__ A, int rank,
                                                      const float* __restrict__ scale, const int32_t* __restrict__ seg,
                                                      int E, T* __restrict__ U) {
-  constexpr int STEP = 64 / sizeof(T);
   __shared__ floatx4 s_acc[4][RT][MT][64];
   Run run;
   if (!find_run(seg, E, 16 * MT, blockIdx.x, run)) return;
@@ -253,26 +267,31 @@ __global__ void __launch_bounds__(256) k_lora_shrink(const T* __restrict__ X, in
   const int rows = seg[e + 1] - r0 < 16 * MT ? (int)(seg[e + 1] - r0) : 16 * MT;
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6, lr = l & 15, lg = l >> 4;
   const int kb0 = blockIdx.y * RT;
-  const T *x[MT], *ar[RT];
+  const T* Ab[RT];
 #pragma unroll
-  for (int t = 0; t < MT; ++t) x[t] = X + (r0 + (16 * t + lr < rows ? 16 * t + lr : rows - 1)) * K;
+  for (int i = 0; i < RT; ++i) Ab[i] = A + (int64_t)uniform_int(e) * rank * K;
+  uint32_t xo[MT][4], ao[RT][4];
 #pragma unroll
-  for (int i = 0; i < RT; ++i) {
-    const int r = 16 * (kb0 + i) + lr;
-    ar[i] = A + ((int64_t)e * rank + (r < rank ? r : rank - 1)) * K;
+  for (int f = 0; f < 4; ++f) {
+    const int r = group_row(f);
+#pragma unroll
+    for (int t = 0; t < MT; ++t) xo[t][f] = (uint32_t)(16 * t + r < rows ? 16 * t + r : rows - 1) * K * sizeof(T);
+#pragma unroll
+    for (int i = 0; i < RT; ++i) ao[i][f] = (uint32_t)(16 * (kb0 + i) + r < rank ? 16 * (kb0 + i) + r : rank - 1) * K * sizeof(T);
   }
   floatx4 acc[RT][MT];
 #pragma unroll
   for (int i = 0; i < RT; ++i)
 #pragma unroll
     for (int t = 0; t < MT; ++t) acc[i][t] = floatx4{0.f, 0.f, 0.f, 0.f};
-  const int steps = (K + STEP - 1) / STEP, s0 = (int)((int64_t)steps * w / 4), s1 = (int)((int64_t)steps * (w + 1) / 4);
-  stream_steps<T, RT == 1 ? 8 : 4>(ar, x, K, s0, s1, [&](const i32x4(&av)[RT], const i32x4(&xv)[MT]) {
+  const int groups = groups_of<T>(K);
+  stream_groups<T, (RT == 1 ? 2 : 1)>(Ab, ao, X + uniform(r0) * K, xo, K, groups * w / 4,
+                                      groups * (w + 1) / 4, [&](const i32x4(&av)[RT], const i32x4(&xv)[MT]) {
 #pragma unroll
-    for (int i = 0; i < RT; ++i)
+                                        for (int i = 0; i < RT; ++i)
 #pragma unroll
-      for (int t = 0; t < MT; ++t) step_mfma<T>(av[i], xv[t], acc[i][t]);
-  });
+                                          for (int t = 0; t < MT; ++t) step_mfma<T>(av[i], xv[t], acc[i][t]);
+                                      });
 #pragma unroll
   for (int i = 0; i < RT; ++i)
 #pragma unroll

@@ -105,17 +105,23 @@ __global__ void __launch_bounds__(64 * kRouteWaves) k_few_route(FewArgs a) {
 constexpr int kScoreWaves = 8;
 template <typename T>
 __global__ void __launch_bounds__(64 * kScoreWaves) k_few_score(FewArgs a) {
-  constexpr int STEP = 64 / sizeof(T), NW = kScoreWaves;
+  constexpr int NW = kScoreWaves;
   __shared__ floatx4 s_acc[NW][64];
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6, lr = l & 15, lg = l >> 4;
-  const int e0 = blockIdx.x * 16, t = blockIdx.y * 16 + lr;
+  const int e0 = blockIdx.x * 16, t0 = blockIdx.y * 16, t = t0 + lr;
   clear_counts(a);
-  const T* const x[1] = {static_cast<const T*>(a.X) + (int64_t)(t < a.n ? t : a.n - 1) * a.d};
-  const T* const r[1] = {static_cast<const T*>(a.R) + (int64_t)(e0 + lr < a.K ? e0 + lr : a.K - 1) * a.d};
-  const int steps = (a.d + STEP - 1) / STEP;
+  uint32_t xo[1][4], ro[1][4];
+#pragma unroll
+  for (int f = 0; f < 4; ++f) {
+    const int row = group_row(f);
+    xo[0][f] = (uint32_t)(t0 + row < a.n ? row : a.n - 1 - t0) * a.d * sizeof(T);
+    ro[0][f] = (uint32_t)(e0 + row < a.K ? row : a.K - 1 - e0) * a.d * sizeof(T);
+  }
+  const int groups = groups_of<T>(a.d);
   floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-  stream_steps<T, 8>(r, x, a.d, (int)((int64_t)steps * w / NW), (int)((int64_t)steps * (w + 1) / NW),
-                     [&](const i32x4(&rv)[1], const i32x4(&xv)[1]) { step_mfma<T>(rv[0], xv[0], acc); });
+  stream_groups<T, 2>({static_cast<const T*>(a.R) + (int64_t)e0 * a.d}, ro, static_cast<const T*>(a.X) + (int64_t)t0 * a.d, xo,
+                      a.d, groups * w / NW, groups * (w + 1) / NW,
+                      [&](const i32x4(&rv)[1], const i32x4(&xv)[1]) { step_mfma<T>(rv[0], xv[0], acc); });
   s_acc[w][l] = acc;
   __syncthreads();
   if (w != 0 || t >= a.n) return;
@@ -162,9 +168,8 @@ __device__ __forceinline__ floatx4 load_through(const float* p) {
 // experts each, U = 4 / 8: 334 / 343 us for the first layer (2048 -> 2 x 2048), 114 / 132 for the second
 // (2048 -> 1024); one sample with one of 16, U = 4 / 8 / 16: 6.9 / 6.5 / 5.3 us for the first
 // (2048 -> 4096), whose waves have 16 steps each.
-template <typename T, int LAYER, bool GATED, int U>
+template <typename T, int LAYER, bool GATED, int UG>
 __global__ void __launch_bounds__(256) k_few_layer(FewArgs a, int tiles, int slots) {
-  constexpr int STEP = 64 / sizeof(T);
   constexpr int MI = LAYER == 1 && GATED ? 2 : 1;
   constexpr int NX = LAYER == 2 ? Halves<T>::N : 1;  // operands of an activation
   __shared__ int s_expert, s_count, s_rows[HMOE_FEW_ROWS];
@@ -178,32 +183,42 @@ __global__ void __launch_bounds__(256) k_few_layer(FewArgs a, int tiles, int slo
                             : few_group<256>(a.chosen, a.n * a.k, a.K, slot, &s_expert, s_rows, &s_count);
   if (LAYER == 1 && !any) return;
   if (any) {
-    const int e = a.n == 1 ? a.chosen[slot] : s_expert, count = a.n == 1 ? 1 : s_count;
+    const int e = uniform_int(a.n == 1 ? a.chosen[slot] : s_expert), count = a.n == 1 ? 1 : s_count;
     const int kd = LAYER == 1 ? a.d : a.h, rows = LAYER == 1 ? a.h : a.o;
-    const int r = tile * 16 + lr < rows ? tile * 16 + lr : rows - 1;
     const T* W[MI];
+    uint32_t wo[MI][4];
 #pragma unroll
-    for (int i = 0; i < MI; ++i)
-      W[i] = LAYER == 1 ? static_cast<const T*>(a.W1) + ((int64_t)e * MI * a.h + (int64_t)i * a.h + r) * kd
-                        : static_cast<const T*>(a.W2) + ((int64_t)e * a.o + r) * kd;
-    const int steps = (kd + STEP - 1) / STEP, shares = 4 * splits, share = split * 4 + w;
-    const int s0 = (int)((int64_t)steps * share / shares), s1 = (int)((int64_t)steps * (share + 1) / shares);
+    for (int i = 0; i < MI; ++i) {
+      W[i] = LAYER == 1 ? static_cast<const T*>(a.W1) + ((int64_t)(e * MI + i) * a.h + tile * 16) * kd
+                        : static_cast<const T*>(a.W2) + ((int64_t)e * a.o + tile * 16) * kd;
+#pragma unroll
+      for (int f = 0; f < 4; ++f) {
+        const int r = group_row(f);
+        wo[i][f] = (uint32_t)(tile * 16 + r < rows ? r : rows - 1 - tile * 16) * kd * sizeof(T);
+      }
+    }
+    const int groups = groups_of<T>(kd), shares = 4 * splits, share = split * 4 + w;
+    const int g0 = (int)((int64_t)groups * share / shares), g1 = (int)((int64_t)groups * (share + 1) / shares);
     for (int t0 = 0; t0 < count; t0 += 16) {
-      const int q = a.n == 1 ? slot : s_rows[t0 + lr < count ? t0 + lr : count - 1];
-      const T* x[NX];
+      const auto row_of = [&](int i) { return a.n == 1 ? slot : s_rows[t0 + i < count ? t0 + i : count - 1]; };
+      const int q = row_of(lr);
+      uint32_t xo[NX][4];
 #pragma unroll
-      for (int j = 0; j < NX; ++j)
-        x[j] = LAYER == 1 ? static_cast<const T*>(a.X) + (int64_t)(q / a.k) * kd
-                          : static_cast<const T*>(a.hid) + ((int64_t)q * NX + j) * kd;
+      for (int f = 0; f < 4; ++f) {
+        const int qf = row_of(group_row(f));
+#pragma unroll
+        for (int j = 0; j < NX; ++j) xo[j][f] = (uint32_t)(LAYER == 1 ? qf / a.k : qf * NX + j) * kd * sizeof(T);
+      }
       floatx4 acc[MI];
 #pragma unroll
       for (int i = 0; i < MI; ++i) acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
-      stream_steps<T, U>(W, x, kd, s0, s1, [&](const i32x4(&wv)[MI], const i32x4(&xv)[NX]) {
+      stream_groups<T, UG>(W, wo, static_cast<const T*>(LAYER == 1 ? a.X : a.hid), xo, kd, g0, g1,
+                           [&](const i32x4(&wv)[MI], const i32x4(&xv)[NX]) {
 #pragma unroll
-        for (int i = 0; i < MI; ++i)
+                             for (int i = 0; i < MI; ++i)
 #pragma unroll
-          for (int j = 0; j < NX; ++j) step_mfma<T>(wv[i], xv[j], acc[i]);
-      });
+                               for (int j = 0; j < NX; ++j) step_mfma<T>(wv[i], xv[j], acc[i]);
+                           });
 #pragma unroll
       for (int i = 0; i < MI; ++i) s_acc[w][i][l] = acc[i];
       __syncthreads();
@@ -293,10 +308,10 @@ int few_layer(const FewArgs& a, hipStream_t st) {
   const int slots = (int)few_slots(a.n, a.k, a.K), tiles = (int)cdiv(LAYER == 1 ? a.h : a.o, 16);
   const char* label = LAYER == 1 ? "few layer 1" : "few layer 2";
   const dim3 grid((unsigned)(slots * tiles * (LAYER == 1 ? 1 : a.splits))), block(256);
-  if (LAYER == 1 && (int64_t)slots * tiles <= 2 * device_cus() && a.d > 4 * 8 * (int)(64 / sizeof(T)))
-    HMOE_LAUNCH(label, (k_few_layer<T, LAYER, GATED, (GATED ? 8 : 16)>), grid, block, 0, st, a, tiles, slots);
+  if (LAYER == 1 && (int64_t)slots * tiles <= 2 * device_cus() && groups_of<T>(a.d) > 8)
+    HMOE_LAUNCH(label, (k_few_layer<T, LAYER, GATED, (GATED ? 2 : 4)>), grid, block, 0, st, a, tiles, slots);
   else
-    HMOE_LAUNCH(label, (k_few_layer<T, LAYER, GATED, 4>), grid, block, 0, st, a, tiles, slots);
+    HMOE_LAUNCH(label, (k_few_layer<T, LAYER, GATED, 1>), grid, block, 0, st, a, tiles, slots);
   return HMOE_OK;
 }
 
