@@ -36,6 +36,30 @@ __device__ __forceinline__ i32x4 r_frag(const T* __restrict__ row, int kb, int l
   const int c = sizeof(T) == 2 ? 16 * kb + 8 * (lg & 1) : 16 * kb + 4 * lg;
   return c < rank ? *reinterpret_cast<const i32x4*>(row + c) : i32x4{0, 0, 0, 0};
 }
+// The same fragments for 16 rows at once, loaded with adjacent lanes in one row (64 contiguous bytes of each, cf.
+// fewrows.hpp) and moved through LDS' crossbar: rank_load j of the row l / 4 feeds the steps of rank_steps.
+template <typename T>
+__host__ __device__ constexpr int rank_steps() {  // steps to a load
+  return sizeof(T) == 2 ? 2 : 1;
+}
+template <typename T>
+__device__ __forceinline__ i32x4 rank_load(const T* __restrict__ row, int j, int rank) {
+  const int c = (4 * j + (threadIdx.x & 3)) * (16 / (int)sizeof(T));
+  return *reinterpret_cast<const i32x4*>(row + (c < rank ? c : 0));
+}
+template <typename T>
+__device__ __forceinline__ i32x4 rank_pick(i32x4 v, int kb, int lr, int lg, int rank) {
+  const int from = 4 * (4 * lr + (sizeof(T) == 2 ? 2 * (kb & 1) + (lg & 1) : lg));
+  const bool in = (sizeof(T) == 2 ? 16 * kb + 8 * (lg & 1) : 16 * kb + 4 * lg) < rank;
+  i32x4 o;
+#pragma unroll
+  for (int d = 0; d < 4; ++d) {
+    const int x = __builtin_amdgcn_ds_bpermute(from, v[d]);
+    o[d] = in ? x : 0;
+  }
+  return o;
+}
+
 // Stores four values 16 kb + 4 lg .. of a row of U (those past the rank as zeros).
 template <typename T>
 __device__ __forceinline__ void u_store(T* __restrict__ U, int64_t row, int ldu, int kb, int lg, int rank, floatx4 v) {
@@ -137,18 +161,35 @@ __global__ void __launch_bounds__(64 * kFewShrinkWaves) k_lora_few_shrink(LoraFe
 }
 
 // 16 MI columns of Y for all rows (16 NT at most); the waves split d, and the adapters of the rows.
-template <typename T, int MI, int NT>
+// RB > 0: one row, whose 16 RB values of U the workgroup forms itself, the rows of A going past x with its rows
+// of W: for a narrow A the reads of it (from L2) take less than the launch that U otherwise comes from.
+template <typename T, int MI, int NT, int RB>
 __global__ void __launch_bounds__(256) k_lora_few(LoraFew a) {
-  __shared__ floatx4 s_acc[4][MI][NT][64];
+  static_assert(RB == 0 || (MI == 1 && NT == 1), "one row");
+  constexpr int UROW = HMOE_LORA_RANK * 4 + 16;  // bytes of a row of U at most, and a bank shift
+  constexpr int ACC = 4 * MI * NT * 64 * 16, ULDS = 16 * NT * UROW;
+  __shared__ __attribute__((aligned(16))) char s_mem[ACC > ULDS ? ACC : ULDS];
+  __shared__ floatx4 s_a[RB > 0 ? 4 : 1][RB > 0 ? RB : 1][64];
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6, lr = l & 15, lg = l >> 4;
   const int c0 = blockIdx.x * 16 * MI;
-  const T* W[MI];
-  uint32_t wo[MI][4], xo[NT][4];
+  const int ldu = u_width<T>(a.rank), blocks = u_blocks(a.rank), urow = ldu * (int)sizeof(T) + 16;
+  const int all = a.adapter[l < a.n ? l : a.n - 1];  // a lane to a row
+  lds<char>* s_u = (lds<char>*)s_mem;
+  if constexpr (RB == 0) {  // U, 16-byte pieces
+    const int per = ldu * (int)sizeof(T) / 16;
+    for (int q = threadIdx.x; q < per * a.n; q += 256) {
+      const int r = q / per, v = q - r * per;
+      *reinterpret_cast<lds<i32x4>*>(s_u + r * urow + 16 * v) =
+          *reinterpret_cast<const i32x4*>(static_cast<const char*>(a.U) + (int64_t)r * ldu * sizeof(T) + 16 * v);
+    }
+  }
+  const T* W[MI + RB];
+  uint32_t wo[MI + RB][4], xo[NT][4];
   int col[MI], row[NT], mine[NT];
 #pragma unroll
   for (int i = 0; i < MI; ++i) {
     const int ci = c0 + 16 * i < a.o ? c0 + 16 * i : a.o - 1;  // a tile past the columns repeats the last
-    col[i] = ci + lr < a.o ? ci + lr : a.o - 1;
+    col[i] = ci;
     W[i] = static_cast<const T*>(a.W) + (int64_t)ci * a.d;
 #pragma unroll
     for (int f = 0; f < 4; ++f)
@@ -164,47 +205,85 @@ __global__ void __launch_bounds__(256) k_lora_few(LoraFew a) {
       xo[t][f] = (uint32_t)(r < a.n ? r : a.n - 1) * a.d * sizeof(T);
     }
   }
-  const int all = a.adapter[l < a.n ? l : a.n - 1];  // a lane to a row
-  floatx4 acc[MI][NT];
+  if constexpr (RB > 0) {
+    const int e = uniform_int(all);
+    const bool some = e >= 0 && e < a.E;
 #pragma unroll
-  for (int i = 0; i < MI; ++i)
+    for (int i = 0; i < RB; ++i) {  // without an adapter: any rows, for sums that are not used
+      W[MI + i] = some ? static_cast<const T*>(a.A) + (int64_t)e * a.rank * a.d : static_cast<const T*>(a.A);
+#pragma unroll
+      for (int f = 0; f < 4; ++f) {
+        const int r = 16 * i + group_row(f);
+        wo[MI + i][f] = (uint32_t)(r < a.rank ? r : a.rank - 1) * a.d * sizeof(T);
+      }
+    }
+  }
+  floatx4 acc[MI + RB][NT];
+#pragma unroll
+  for (int i = 0; i < MI + RB; ++i)
 #pragma unroll
     for (int t = 0; t < NT; ++t) acc[i][t] = floatx4{0.f, 0.f, 0.f, 0.f};
   const int groups = groups_of<T>(a.d);
-  stream_groups<T, (MI * NT > 1 ? 1 : 4)>(W, wo, static_cast<const T*>(a.X), xo, a.d, groups * w / 4, groups * (w + 1) / 4,
-                                          [&](const i32x4(&wv)[MI], const i32x4(&xv)[NT]) {
+  stream_groups<T, (RB > 0 ? 2 : (MI * NT > 1 ? 1 : 4))>(
+      W, wo, static_cast<const T*>(a.X), xo, a.d, groups * w / 4, groups * (w + 1) / 4,
+      [&](const i32x4(&wv)[MI + RB], const i32x4(&xv)[NT]) {
 #pragma unroll
-                                            for (int i = 0; i < MI; ++i)
+        for (int i = 0; i < MI + RB; ++i)
 #pragma unroll
-                                              for (int t = 0; t < NT; ++t) step_mfma<T>(wv[i], xv[t], acc[i][t]);
-                                          });
-  // the adapters in the order of their first rows, one to a wave in turn
+          for (int t = 0; t < NT; ++t) step_mfma<T>(wv[i], xv[t], acc[i][t]);
+      });
+  if constexpr (RB > 0) {
+#pragma unroll
+    for (int i = 0; i < RB; ++i) s_a[w][i][l] = acc[MI + i][0];
+    __syncthreads();
+    if (w < RB && lr == 0) {
+      const int e = all >= 0 && all < a.E ? all : 0;
+      floatx4 u = (s_a[0][w][l] + s_a[1][w][l]) + (s_a[2][w][l] + s_a[3][w][l]);
+      u_store((T*)s_mem, 0, ldu, w, lg, a.rank, u * (a.scale ? a.scale[e] : 1.f));
+    }
+  }
+  __syncthreads();
+  // The adapters in the order of their first rows, one to a wave in turn, with sums of their own, which only
+  // their rows take: another row's zeros times an infinite B would not be zeros.
   uint64_t left = __ballot(l < a.n && all >= 0 && all < a.E);
-  const int ldu = u_width<T>(a.rank), blocks = u_blocks(a.rank);
   for (int turn = 0; left != 0; ++turn) {
     const int e = __builtin_amdgcn_readlane(all, __builtin_ctzll(left));
     const uint64_t with = __ballot(all == e) & left;
     left &= ~with;
     if (turn % 4 != w) continue;
-    const T* B = static_cast<const T*>(a.B) + (int64_t)e * a.o * a.rank;
-    // sums of their own, which only the adapter's rows take: another row's zeros times an infinite B would
-    // not be zeros
+    const T* B[MI];
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      const int c = col[i] + (l >> 2);
+      B[i] = static_cast<const T*>(a.B) + ((int64_t)e * a.o + (c < a.o ? c : a.o - 1)) * a.rank;
+    }
     floatx4 own[MI][NT];
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
       for (int t = 0; t < NT; ++t) own[i][t] = floatx4{0.f, 0.f, 0.f, 0.f};
-    for (int kb = 0; kb < blocks; ++kb) {
-      i32x4 bv[MI];
+    constexpr int PER = rank_steps<T>();
+    for (int j = 0; j * PER < blocks; ++j) {
+      i32x4 raw[MI];
 #pragma unroll
-      for (int i = 0; i < MI; ++i) bv[i] = r_frag(B + (int64_t)col[i] * a.rank, kb, lg, a.rank);
+      for (int i = 0; i < MI; ++i) raw[i] = rank_load(B[i], j, a.rank);
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        if (((with >> (16 * t)) & 0xffff) == 0) continue;
-        i32x4 uv = {0, 0, 0, 0};
-        if (mine[t] == e) uv = u_frag(static_cast<const T*>(a.U), row[t], ldu, kb, lg, a.rank);
+      for (int p = 0; p < PER; ++p) {
+        const int kb = j * PER + p;
+        if (kb >= blocks) break;
+        i32x4 bv[MI];
 #pragma unroll
-        for (int i = 0; i < MI; ++i) step_mfma<T>(bv[i], uv, own[i][t]);
+        for (int i = 0; i < MI; ++i) bv[i] = rank_pick<T>(raw[i], kb, lr, lg, a.rank);
+        const int at = (sizeof(T) == 2 ? 64 * kb : 64 * kb) + 16 * lg;  // bytes of the row of U
+        const bool in = at < ldu * (int)sizeof(T);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          if (((with >> (16 * t)) & 0xffff) == 0) continue;
+          i32x4 uv = *reinterpret_cast<const lds<i32x4>*>(s_u + row[t] * urow + (in ? at : 0));
+          uv = in && mine[t] == e ? uv : i32x4{0, 0, 0, 0};
+#pragma unroll
+          for (int i = 0; i < MI; ++i) step_mfma<T>(bv[i], uv, own[i][t]);
+        }
       }
     }
 #pragma unroll
@@ -213,6 +292,8 @@ __global__ void __launch_bounds__(256) k_lora_few(LoraFew a) {
       for (int t = 0; t < NT; ++t)
         if (mine[t] == e) acc[i][t] += own[i][t];
   }
+  __syncthreads();
+  floatx4(*s_acc)[MI][NT][64] = reinterpret_cast<floatx4(*)[MI][NT][64]>(s_mem);
 #pragma unroll
   for (int i = 0; i < MI; ++i)
 #pragma unroll
@@ -222,10 +303,10 @@ __global__ void __launch_bounds__(256) k_lora_few(LoraFew a) {
     const int i = q / NT, t = q % NT, c = c0 + 16 * i + 4 * lg;
     floatx4 v = (s_acc[0][i][t][l] + s_acc[1][i][t][l]) + (s_acc[2][i][t][l] + s_acc[3][i][t][l]);
     if (16 * t + lr >= a.n || c >= a.o) continue;
-    vec4<T> y;
+    quad<T> y;
 #pragma unroll
     for (int z = 0; z < 4; ++z) y[z] = from_f32<T>(v[z] + (a.b ? to_f32(static_cast<const T*>(a.b)[c + z]) : 0.f));
-    *reinterpret_cast<vec4<T>*>(static_cast<T*>(a.Y) + (int64_t)(16 * t + lr) * a.o + c) = y;
+    *reinterpret_cast<quad<T>*>(static_cast<T*>(a.Y) + (int64_t)(16 * t + lr) * a.o + c) = y;
   }
 }
 
@@ -233,19 +314,27 @@ template <typename T, int MI>
 int lora_few_mi(const LoraFew& a, hipStream_t st) {
   const dim3 grid((unsigned)cdiv(a.o, 16 * MI)), block(256);
   switch ((a.n + 15) / 16) {
-    case 1: HMOE_LAUNCH("lora few", (k_lora_few<T, MI, 1>), grid, block, 0, st, a); break;
-    case 2: HMOE_LAUNCH("lora few", (k_lora_few<T, MI, 2>), grid, block, 0, st, a); break;
-    case 3: HMOE_LAUNCH("lora few", (k_lora_few<T, MI, 3>), grid, block, 0, st, a); break;
-    default: HMOE_LAUNCH("lora few", (k_lora_few<T, MI, 4>), grid, block, 0, st, a); break;
+    case 1: HMOE_LAUNCH("lora few", (k_lora_few<T, MI, 1, 0>), grid, block, 0, st, a); break;
+    case 2: HMOE_LAUNCH("lora few", (k_lora_few<T, MI, 2, 0>), grid, block, 0, st, a); break;
+    case 3: HMOE_LAUNCH("lora few", (k_lora_few<T, MI, 3, 0>), grid, block, 0, st, a); break;
+    default: HMOE_LAUNCH("lora few", (k_lora_few<T, MI, 4, 0>), grid, block, 0, st, a); break;
   }
   return HMOE_OK;
 }
 
 template <typename T>
 int lora_few_t(const LoraFew& a, hipStream_t st) {
-  const int slots = a.n < a.E ? a.n : a.E;
-  HMOE_LAUNCH("lora few shrink", k_lora_few_shrink<T>, dim3((unsigned)(slots * u_blocks(a.rank))),
-              dim3(64 * kFewShrinkWaves), 0, st, a);
+  const int slots = a.n < a.E ? a.n : a.E, blocks = u_blocks(a.rank);
+  // One row: in one launch where reading A for every 16 columns (up to 20 MB from L2 per 16 of the rank,
+  // 4 us) takes less than a second one.
+  if (a.n == 1 && blocks <= 2 && (int64_t)a.o * a.d * sizeof(T) * blocks <= (20 << 20)) {
+    const dim3 grid((unsigned)cdiv(a.o, 16)), block(256);
+    if (blocks == 1) HMOE_LAUNCH("lora few", (k_lora_few<T, 1, 1, 1>), grid, block, 0, st, a);
+    else HMOE_LAUNCH("lora few", (k_lora_few<T, 1, 1, 2>), grid, block, 0, st, a);
+    return HMOE_OK;
+  }
+  HMOE_LAUNCH("lora few shrink", k_lora_few_shrink<T>, dim3((unsigned)(slots * blocks)), dim3(64 * kFewShrinkWaves), 0, st,
+              a);
   // wide outputs: two blocks of columns to a workgroup, which halves the reads of X
   if (a.o >= 16 * 1024) return lora_few_mi<T, 2>(a, st);
   return lora_few_mi<T, 1>(a, st);
