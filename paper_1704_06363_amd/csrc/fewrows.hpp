@@ -70,12 +70,11 @@ __host__ __device__ inline int groups_of(int kd) {
 // body(wv, xv) with the operands of each step of the groups g0 <= g < g1.  wo and xo: byte offsets from the
 // tiles' wb, and from xb, of this lane's row of load f (kd elements from there); below 2^32.  The loads of UG groups go out together.  kd is a
 // multiple of 8: past it, in the last group, both operands are zeros.
-template <typename T, int UG, int MI, int NX, class Body>
-__device__ __forceinline__ void stream_groups(const T* const (&wb)[MI], const uint32_t (&wo)[MI][4], const T* xb,
-                                              const uint32_t (&xo)[NX][4], int kd, int g0, int g1, Body body) {
+template <typename T, int UG, int MI, int NX, class Row, class Body>
+__device__ __forceinline__ void stream_groups_of(const T* const (&wb)[MI], const uint32_t (&wo)[MI][4], Row xrow, int kd,
+                                                 int g0, int g1, Body body) {
   constexpr int N = 16 / sizeof(T), GROUP = group_size<T>();
   const int own = group_chunk() * N;
-  const char* xc = reinterpret_cast<const char*>(xb);
   for (int g = g0; g < g1; g += UG) {
     i32x4 wv[UG][MI][4], xv[UG][NX][4];
 #pragma unroll
@@ -89,7 +88,7 @@ __device__ __forceinline__ void stream_groups(const T* const (&wb)[MI], const ui
 #pragma unroll
       for (int j = 0; j < NX; ++j)
 #pragma unroll
-        for (int f = 0; f < 4; ++f) xv[u][j][f] = *reinterpret_cast<const i32x4*>(xc + (xo[j][f] + in));
+        for (int f = 0; f < 4; ++f) xv[u][j][f] = *reinterpret_cast<const i32x4*>(xrow(j, f, in));
     }
 #pragma unroll
     for (int u = 0; u < UG; ++u) {
@@ -121,6 +120,20 @@ __device__ __forceinline__ void stream_groups(const T* const (&wb)[MI], const ui
       }
     }
   }
+}
+
+template <typename T, int UG, int MI, int NX, class Body>
+__device__ __forceinline__ void stream_groups(const T* const (&wb)[MI], const uint32_t (&wo)[MI][4], const T* xb,
+                                              const uint32_t (&xo)[NX][4], int kd, int g0, int g1, Body body) {
+  const char* xc = reinterpret_cast<const char*>(xb);
+  stream_groups_of<T, UG, MI, NX>(wb, wo, [&](int j, int f, uint32_t at) { return xc + (xo[j][f] + at); }, kd, g0, g1, body);
+}
+// The same with x's rows anywhere.
+template <typename T, int UG, int MI, int NX, class Body>
+__device__ __forceinline__ void stream_groups(const T* const (&wb)[MI], const uint32_t (&wo)[MI][4],
+                                              const T* const (&xr)[NX][4], int kd, int g0, int g1, Body body) {
+  stream_groups_of<T, UG, MI, NX>(
+      wb, wo, [&](int j, int f, uint32_t at) { return reinterpret_cast<const char*>(xr[j][f]) + at; }, kd, g0, g1, body);
 }
 
 // A value that feeds a bf16 product without losing its low bits: v = hi + lo up to 2^-16 of it, each a

@@ -342,12 +342,13 @@ int lora_few_t(const LoraFew& a, hipStream_t st) {
 
 // ------------------------------------------------------------------ rows in adapter order
 
-// U = s_e rows A_e^T for 16 MT rows of one adapter and 16 RT values of the rank: rows [n][K], A [E][rank][K].
+// U = s_e rows A_e^T for 16 MT rows of one adapter and 16 RT values of the rank: rows [n][K] (row map[p] for slot
+// p, if there is a map), A [E][rank][K].
 // The four waves split K.
 template <typename T, int RT, int MT>
 __global__ void __launch_bounds__(256) k_lora_shrink(const T* __restrict__ X, int K, const T* __restrict__ A, int rank,
                                                      const float* __restrict__ scale, const int32_t* __restrict__ seg,
-                                                     int E, T* __restrict__ U) {
+                                                     int E, const int32_t* __restrict__ map, T* __restrict__ U) {
   __shared__ floatx4 s_acc[4][RT][MT][64];
   Run run;
   if (!find_run(seg, E, 16 * MT, blockIdx.x, run)) return;
@@ -359,12 +360,18 @@ __global__ void __launch_bounds__(256) k_lora_shrink(const T* __restrict__ X, in
   const T* Ab[RT];
 #pragma unroll
   for (int i = 0; i < RT; ++i) Ab[i] = A + (int64_t)uniform_int(e) * rank * K;
-  uint32_t xo[MT][4], ao[RT][4];
+  // rows by 64-bit distance from the tile's first, which offsets below 2^32 from the least of them cannot
+  // always hold once they are scattered
+  const T* xr[MT][4];
+  uint32_t ao[RT][4];
 #pragma unroll
   for (int f = 0; f < 4; ++f) {
     const int r = group_row(f);
 #pragma unroll
-    for (int t = 0; t < MT; ++t) xo[t][f] = (uint32_t)(16 * t + r < rows ? 16 * t + r : rows - 1) * K * sizeof(T);
+    for (int t = 0; t < MT; ++t) {
+      const int64_t slot = r0 + (16 * t + r < rows ? 16 * t + r : rows - 1);
+      xr[t][f] = X + (map ? map[slot] : slot) * K;
+    }
 #pragma unroll
     for (int i = 0; i < RT; ++i) ao[i][f] = (uint32_t)(16 * (kb0 + i) + r < rank ? 16 * (kb0 + i) + r : rank - 1) * K * sizeof(T);
   }
@@ -374,7 +381,7 @@ __global__ void __launch_bounds__(256) k_lora_shrink(const T* __restrict__ X, in
 #pragma unroll
     for (int t = 0; t < MT; ++t) acc[i][t] = floatx4{0.f, 0.f, 0.f, 0.f};
   const int groups = groups_of<T>(K);
-  stream_groups<T, (RT == 1 ? 2 : 1)>(Ab, ao, X + uniform(r0) * K, xo, K, groups * w / 4,
+  stream_groups<T, (RT == 1 ? 2 : 1)>(Ab, ao, xr, K, groups * w / 4,
                                       groups * (w + 1) / 4, [&](const i32x4(&av)[RT], const i32x4(&xv)[MT]) {
 #pragma unroll
                                         for (int i = 0; i < RT; ++i)
@@ -456,8 +463,49 @@ struct LoraRow {  // destination row
   __device__ __forceinline__ int64_t operator()(int r) const { return map ? map[m0 + r] : m0 + r; }
 };
 
-// out[map[m]] = A[m] W^T + bias + U[m] B_e^T.   W_KC: W [cols][Kd], otherwise [Kd][cols].
-template <class C, bool W_KC>
+// The pipelined engine's tile with row map[m0 + r] of A as its row r; A below 4 GB (32-bit offsets).
+template <class C, bool B_KC>
+struct GatherTile : PipeTile<C, true, B_KC> {
+  using P = PipeTile<C, true, B_KC>;
+  __device__ __forceinline__ void prime(const bf16* __restrict__ A_, int64_t lda_, const int32_t* __restrict__ map,
+                                        int a_rows_, const bf16* __restrict__ B_, int64_t ldb_, int b_rows_, int k_len,
+                                        lds<char>* smem) {
+    this->A = uniform(reinterpret_cast<const char*>(A_));
+    this->B = uniform(reinterpret_cast<const char*>(B_));
+    this->lda = lda_;
+    this->ldb = ldb_;
+    this->a_rows = a_rows_;
+    this->b_rows = b_rows_;
+    k_len = __builtin_amdgcn_readfirstlane(k_len);
+    this->nk = (k_len + C::BK - 1) / C::BK;
+    this->k_last = k_len - (this->nk - 1) * C::BK;
+    this->step_a = C::BK * 2;
+    this->step_b = B_KC ? C::BK * 2 : C::BK * 2 * ldb_;
+    const int t = thread_id();
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int q = 0; q < P::OA::NQ; ++q) {
+        const int piece = q * C::THREADS + t, tr = P::OA::tile_row(h, piece >> 3);
+        const int64_t row = map[tr < a_rows_ ? tr : a_rows_ - 1];
+        this->oa.off[h][q] = (uint32_t)((row * lda_ + P::OA::k_of(piece)) * 2);
+      }
+    this->ob.init(ldb_, b_rows_);
+    this->template load_b<0>(0, P::slot_b(smem, 0, 0));
+    this->template load_a<0>(0, P::slot_a(smem, 0, 0));
+    this->template load_b<1>(0, P::slot_b(smem, 0, 1));
+    this->template load_a<1>(0, P::slot_a(smem, 0, 1));
+    if (this->nk > 1) {
+      this->template load_b<0>(1, P::slot_b(smem, 1, 0));
+      this->template load_a<0>(1, P::slot_a(smem, 1, 0));
+      this->template load_b<1>(1, P::slot_b(smem, 1, 1));
+    }
+  }
+};
+
+// out[map[m]] = A[m] W^T + bias + U[m] B_e^T.   W_KC: W [cols][Kd], otherwise [Kd][cols].  GATHER: A's rows are
+// in out's order, too.
+template <class C, bool W_KC, bool GATHER>
 __global__ void __launch_bounds__(C::THREADS)
     k_lora_gemm(const typename C::type* __restrict__ A, const typename C::type* __restrict__ W,
                 const typename C::type* __restrict__ bias, const typename C::type* __restrict__ U,
@@ -469,8 +517,14 @@ __global__ void __launch_bounds__(C::THREADS)
   const TileCoord tc = tile_plain<C>(n, cols, Kd);
   if (!tc.valid) return;
   floatx4 acc[C::MI][C::NJ];
-  gemm_tile<C, true, W_KC>(A + tc.m0 * Kd, Kd, tc.m_rows, W_KC ? W + (int64_t)tc.n0 * Kd : W + tc.n0, W_KC ? Kd : cols,
-                           tc.n_cols, Kd, smem, acc);
+  const T* Wt = W_KC ? W + (int64_t)tc.n0 * Kd : W + tc.n0;
+  if constexpr (GATHER) {
+    GatherTile<C, W_KC> g;
+    g.prime(A, Kd, map + tc.m0, tc.m_rows, Wt, W_KC ? Kd : cols, tc.n_cols, Kd, smem);
+    g.run(smem, acc);
+  } else {
+    gemm_tile<C, true, W_KC>(A + tc.m0 * Kd, Kd, tc.m_rows, Wt, W_KC ? Kd : cols, tc.n_cols, Kd, smem, acc);
+  }
   lora_extend<C>(tc, acc, U, B, rank, cols, seg, E);
   using F = Frag<C>;
   const F f;
@@ -548,12 +602,101 @@ struct GradTile {
   using type = typename std::conditional<U_LEFT, Cfg<T, UW, BW, V, W>, Cfg<T, BW, UW, W, V>>::type;
 };
 
+// A K-strided operand (gemm.hpp's Stager) whose K row k is at base + rows[k] ld.
+template <typename T, int ROWS, int THREADS>
+struct MapStager : Stager<T, ROWS, THREADS, false> {
+  using S = Stager<T, ROWS, THREADS, false>;
+  __device__ __forceinline__ void load(const T* __restrict__ base, int64_t ld, int cols_valid, int k0, int k_valid,
+                                       const lds<int32_t>* rows) {
+    constexpr int RQ = ROWS / 4;
+#pragma unroll
+    for (int q = 0; q < S::NPIECE; ++q) {
+      const int pc = threadIdx.x + THREADS * q;
+      if (S::SPARE && pc >= S::PIECES) continue;
+      const int r = pc % RQ * 4, kb = pc / RQ;
+      if constexpr (S::BF) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int k = 8 * kb + 2 * i;  // of the stage
+          uint2 e = make_uint2(0u, 0u), o = make_uint2(0u, 0u);
+          if (r < cols_valid && k0 + k < k_valid) e = *reinterpret_cast<const uint2*>(base + (int64_t)rows[k] * ld + r);
+          if (r < cols_valid && k0 + k + 1 < k_valid)
+            o = *reinterpret_cast<const uint2*>(base + (int64_t)rows[k + 1] * ld + r);
+          this->v[q * 4 + i] = i32x4{(int)e.x, (int)e.y, (int)o.x, (int)o.y};
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int k = 4 * kb + i;
+          if (r < cols_valid && k0 + k < k_valid)
+            this->v[q * 4 + i] = *reinterpret_cast<const i32x4*>(base + (int64_t)rows[k] * ld + r);
+          else
+            this->v[q * 4 + i] = i32x4{0, 0, 0, 0};
+        }
+      }
+    }
+  }
+};
+
+// acc = U^T D or D^T U over `rows` slots from p0 on (pu is there already), on the register-staged engine.  A
+// stage's rows of D are looked up a stage before its loads go out: s_row holds those of two stages.
+template <class C, int BW, int UW, bool U_LEFT>
+__device__ __forceinline__ void grad_tile(const typename C::type* __restrict__ D, int width, int dv,
+                                          const int32_t* __restrict__ map, int64_t p0,
+                                          const typename C::type* __restrict__ pu, int ldu, int uv, int rows,
+                                          lds<char>* smem, floatx4 (&acc)[C::MI][C::NJ]) {
+  using T = typename C::type;
+  __shared__ int32_t s_row[2][C::BK];
+  MapStager<T, BW, C::THREADS> sd;
+  Stager<T, UW, C::THREADS, false> su;
+  constexpr int D_BYTES = BW * kStageRowBytes, U_BYTES = UW * kStageRowBytes;
+  lds<char>* const bd = smem;
+  lds<char>* const bu = smem + 2 * D_BYTES;
+#pragma unroll
+  for (int i = 0; i < C::MI; ++i)
+#pragma unroll
+    for (int j = 0; j < C::NJ; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+  const int nk = (rows + C::BK - 1) / C::BK, t = threadIdx.x;
+  const auto look_up = [&](int s) {
+    const int k = s * C::BK + t;
+    return t < C::BK && k < rows ? (map ? map[p0 + k] : (int32_t)(p0 + k)) : 0;
+  };
+  const auto load = [&](int s) {
+    sd.load(D, width, dv, s * C::BK, rows, (const lds<int32_t>*)s_row[s & 1]);
+    su.load(pu, ldu, uv, s * C::BK, rows);
+  };
+  const auto store = [&](int s) {
+    sd.store(bd + (s & 1) * D_BYTES);
+    su.store(bu + (s & 1) * U_BYTES);
+  };
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    const int32_t r = look_up(s);
+    if (t < C::BK) s_row[s][t] = r;
+  }
+  __syncthreads();
+  load(0);
+  store(0);
+  __syncthreads();
+  for (int kt = 0; kt < nk; ++kt) {
+    if (kt + 1 < nk) load(kt + 1);
+    const int32_t r = look_up(kt + 2);
+    const lds<char>*d = bd + (kt & 1) * D_BYTES, *u = bu + (kt & 1) * U_BYTES;
+    if constexpr (U_LEFT) mfma_stage<C>(u, d, acc);
+    else mfma_stage<C>(d, u, acc);
+    if (kt + 1 < nk) store(kt + 1);
+    if (t < C::BK) s_row[kt & 1][t] = r;  // stage kt's rows: last read before the last barrier
+    __syncthreads();
+  }
+}
+
 // For one piece of adapter e's rows:  U_LEFT: out[c][m] = sum_rows U[c] D[m] (dA: [rank][width]),
 // otherwise out[m][c] = sum_rows D[m] U[c] (dB: [width][rank]).  D [n][width] with U or V as u_width says.
+// D's row of slot p is map[p], or p without a map.
 template <typename T, int UW, int BW, bool U_LEFT>
-__global__ void __launch_bounds__(256) k_lora_grad(const T* __restrict__ D, int width, const T* __restrict__ U, int rank,
-                                                   const int32_t* __restrict__ seg, int E, int piece,
-                                                   float* __restrict__ out, float* __restrict__ part) {
+__global__ void __launch_bounds__(256) k_lora_grad(const T* __restrict__ D, int width, const int32_t* __restrict__ map,
+                                                   const T* __restrict__ U, int rank, const int32_t* __restrict__ seg,
+                                                   int E, int piece, float* __restrict__ out, float* __restrict__ part) {
   using C = typename GradTile<T, UW, BW, U_LEFT>::type;
   static_assert(C::THREADS == 256, "four waves");
   extern __shared__ __attribute__((aligned(16))) char smem_raw[];
@@ -567,10 +710,8 @@ __global__ void __launch_bounds__(256) k_lora_grad(const T* __restrict__ D, int 
   const int ldu = u_width<T>(rank);
   const int d0 = blockIdx.y * BW, u0 = blockIdx.z * UW;
   const int dv = width - d0 < BW ? width - d0 : BW, uv = ldu - u0 < UW ? ldu - u0 : UW;
-  const T *pd = D + p0 * width + d0, *pu = U + p0 * ldu + u0;
   floatx4 acc[C::MI][C::NJ];
-  if constexpr (U_LEFT) gemm_tile<C, false, false>(pu, ldu, uv, pd, width, dv, rows, smem, acc);
-  else gemm_tile<C, false, false>(pd, width, dv, pu, ldu, uv, rows, smem, acc);
+  grad_tile<C, BW, UW, U_LEFT>(D + d0, width, dv, map, p0, U + p0 * ldu + u0, ldu, uv, rows, smem, acc);
   const int64_t size = (int64_t)width * rank;
   float* to = seg[e + 1] - seg[e] > piece ? part + lora_piece_slot(seg[e], local, piece) * size : out + e * size;
   const Frag<C> f;
@@ -611,59 +752,66 @@ __global__ void __launch_bounds__(256) k_lora_grad_join(const float* __restrict_
 
 template <typename T>
 int lora_shrink(const T* X, int K, const T* A, int rank, const float* scale, const int32_t* seg, int E,
-                int64_t n, T* U, hipStream_t st) {
+                int64_t n, const int32_t* map, T* U, hipStream_t st) {
   const int blocks = u_blocks(rank);
   const auto bound = [&](int rows) { return (unsigned)(n / rows + (E < n ? E : n)); };
   if (blocks == 1)
-    HMOE_LAUNCH("lora shrink", (k_lora_shrink<T, 1, 1>), dim3(bound(16)), dim3(256), 0, st, X, K, A, rank, scale, seg, E, U);
+    HMOE_LAUNCH("lora shrink", (k_lora_shrink<T, 1, 1>), dim3(bound(16)), dim3(256), 0, st, X, K, A, rank, scale, seg, E, map, U);
   else if (blocks == 2)
-    HMOE_LAUNCH("lora shrink", (k_lora_shrink<T, 2, 2>), dim3(bound(32)), dim3(256), 0, st, X, K, A, rank, scale, seg, E, U);
+    HMOE_LAUNCH("lora shrink", (k_lora_shrink<T, 2, 2>), dim3(bound(32)), dim3(256), 0, st, X, K, A, rank, scale, seg, E, map, U);
   else
     HMOE_LAUNCH("lora shrink", (k_lora_shrink<T, 4, 2>), dim3(bound(32), (unsigned)cdiv(blocks, 4)), dim3(256), 0, st, X, K,
-                A, rank, scale, seg, E, U);
+                A, rank, scale, seg, E, map, U);
   return HMOE_OK;
 }
 
-// Fewer of the type's tiles (gemm.hpp) than CUs: quarter tiles.
+// Tiles for the type (gemm.hpp), quarter tiles where there are fewer of them than CUs.
+template <typename T, bool W_KC>
+using LoraTile = typename std::conditional<W_KC, typename Pick<T>::C, typename Pick<T>::CK>::type;
+template <typename T, bool W_KC>
+bool lora_small(int64_t n, int cols) {
+  using C = LoraTile<T, W_KC>;
+  return cdiv(n, C::BM) * cdiv(cols, C::BN) < device_cus();
+}
+template <class C, bool W_KC, bool GATHER, typename T>
+int lora_gemm_on(const T* A, const T* W, const T* bias, const T* U, const T* B, int rank, const int32_t* seg, int E,
+                 int64_t n, int cols, int Kd, const int32_t* map, T* out, hipStream_t st) {
+  HMOE_LAUNCH(W_KC ? "lora forward" : "lora input gradient", (k_lora_gemm<C, W_KC, GATHER>),
+              dim3((unsigned)(cdiv(n, C::BM) * cdiv(cols, C::BN))), dim3(C::THREADS), C::LDS, st, A, W, bias, U, B, rank, seg,
+              E, n, cols, Kd, map, out);
+  return HMOE_OK;
+}
 template <typename T, bool W_KC>
 int lora_gemm(const T* A, const T* W, const T* bias, const T* U, const T* B, int rank, const int32_t* seg, int E,
               int64_t n, int cols, int Kd, const int32_t* map, T* out, hipStream_t st) {
-  using C = typename std::conditional<W_KC, typename Pick<T>::C, typename Pick<T>::CK>::type;
-  using Q = CfgQuarter<T>;
-  const char* label = W_KC ? "lora forward" : "lora input gradient";
-  const int64_t tiles = cdiv(n, C::BM) * cdiv(cols, C::BN);
-  if (tiles < device_cus())
-    HMOE_LAUNCH(label, (k_lora_gemm<Q, W_KC>), dim3((unsigned)(cdiv(n, Q::BM) * cdiv(cols, Q::BN))), dim3(Q::THREADS),
-                Q::LDS, st, A, W, bias, U, B, rank, seg, E, n, cols, Kd, map, out);
-  else
-    HMOE_LAUNCH(label, (k_lora_gemm<C, W_KC>), dim3((unsigned)tiles), dim3(C::THREADS), C::LDS, st, A, W, bias, U, B, rank,
-                seg, E, n, cols, Kd, map, out);
-  return HMOE_OK;
+  if (lora_small<T, W_KC>(n, cols))
+    return lora_gemm_on<CfgQuarter<T>, W_KC, false>(A, W, bias, U, B, rank, seg, E, n, cols, Kd, map, out, st);
+  return lora_gemm_on<LoraTile<T, W_KC>, W_KC, false>(A, W, bias, U, B, rank, seg, E, n, cols, Kd, map, out, st);
 }
 
 template <typename T, int UW, int BW, bool U_LEFT>
-int lora_grad_tiles(const T* D, int width, const T* U, int rank, const int32_t* seg, int E, int64_t n, float* out,
+int lora_grad_tiles(const T* D, int width, const int32_t* map, const T* U, int rank, const int32_t* seg, int E, int64_t n, float* out,
                     float* part, hipStream_t st) {
   using C = typename GradTile<T, UW, BW, U_LEFT>::type;
   const int piece = lora_piece(n);
   HMOE_LAUNCH(U_LEFT ? "lora dA" : "lora dB", (k_lora_grad<T, UW, BW, U_LEFT>),
               dim3((unsigned)(n / piece + (E < n ? E : n)), (unsigned)cdiv(width, BW),
                    (unsigned)cdiv(u_width<T>(rank), UW)),
-              dim3(256), C::LDS, st, D, width, U, rank, seg, E, piece, out, part);
+              dim3(256), C::LDS, st, D, width, map, U, rank, seg, E, piece, out, part);
   const int64_t size = (int64_t)width * rank;
   HMOE_LAUNCH("lora gradient join", k_lora_grad_join, dim3((unsigned)cdiv(size, 1024), (unsigned)E), dim3(256), 0, st,
               part, seg, piece, size, out);
   return HMOE_OK;
 }
 template <typename T, bool U_LEFT>
-int lora_grad(const T* D, int width, const T* U, int rank, const int32_t* seg, int E, int64_t n, float* out, float* part,
+int lora_grad(const T* D, int width, const int32_t* map, const T* U, int rank, const int32_t* seg, int E, int64_t n, float* out, float* part,
               hipStream_t st) {
   const int ldu = u_width<T>(rank);
   if ((n / lora_piece(n) + (E < n ? E : n)) * cdiv(width, 256) < device_cus())
-    return lora_grad_tiles<T, 64, 64, U_LEFT>(D, width, U, rank, seg, E, n, out, part, st);
-  if (ldu <= 32) return lora_grad_tiles<T, 32, 256, U_LEFT>(D, width, U, rank, seg, E, n, out, part, st);
-  if (ldu <= 64) return lora_grad_tiles<T, 64, 256, U_LEFT>(D, width, U, rank, seg, E, n, out, part, st);
-  return lora_grad_tiles<T, 128, 256, U_LEFT>(D, width, U, rank, seg, E, n, out, part, st);
+    return lora_grad_tiles<T, 64, 64, U_LEFT>(D, width, map, U, rank, seg, E, n, out, part, st);
+  if (ldu <= 32) return lora_grad_tiles<T, 32, 256, U_LEFT>(D, width, map, U, rank, seg, E, n, out, part, st);
+  if (ldu <= 64) return lora_grad_tiles<T, 64, 256, U_LEFT>(D, width, map, U, rank, seg, E, n, out, part, st);
+  return lora_grad_tiles<T, 128, 256, U_LEFT>(D, width, map, U, rank, seg, E, n, out, part, st);
 }
 
 struct LoraSpace {
@@ -687,7 +835,7 @@ LoraSpace lora_carve(const hmoe_lora_t* p, int64_t n, Workspace& ws) {
 template <typename T>
 int lora_forward_t(const hmoe_lora_t* p, int64_t n, const T* X, const int32_t* offsets, const int32_t* perm, T* U, T* Y,
                    const LoraSpace& w, hipStream_t st) {
-  HMOE_TRY(lora_shrink<T>(X, p->d_in, (const T*)p->A, p->rank, p->scale, offsets, p->E, n, U, st));
+  HMOE_TRY(lora_shrink<T>(X, p->d_in, (const T*)p->A, p->rank, p->scale, offsets, p->E, n, nullptr, U, st));
   return lora_gemm<T, true>(X, (const T*)p->W, (const T*)p->b, U, (const T*)p->B, p->rank, offsets, p->E, n, p->d_out,
                                p->d_in, perm, Y, st);
 }
@@ -702,23 +850,32 @@ int lora_transpose(const void* in, void* out, int E, int rows, int cols, const i
 template <typename T>
 int lora_backward_t(const hmoe_lora_t* p, int64_t n, const T* X, const int32_t* offsets, const int32_t* perm, const T* U,
                     const T* dY, T* dX, float* dA, float* dB, const LoraSpace& w, hipStream_t st) {
-  if (perm) {
+  // dY's rows are gathered by whoever reads them (a copy in slot order took 45 us of 670 at 16384 rows of
+  // 4096), but for the input gradient on tiles that cannot
+  const bool gather = perm && (!dX || (sizeof(T) == 2 && !lora_small<T, false>(n, p->d_in) &&
+                                       (int64_t)n * p->d_out * (int64_t)sizeof(T) < (int64_t(1) << 32)));
+  const int32_t* map = gather ? perm : nullptr;
+  if (perm && !gather) {
     HMOE_TRY(launch_permute(dY, w.dYs, perm, n, p->d_out, p->dt, st));
     dY = (const T*)w.dYs;
   }
   if (dX || dA) {
     HMOE_TRY(lora_transpose<T, true>(p->B, w.Bt, p->E, p->d_out, p->rank, offsets, st));
-    HMOE_TRY(lora_shrink<T>(dY, p->d_out, (const T*)w.Bt, p->rank, p->scale, offsets, p->E, n, (T*)w.V, st));
+    HMOE_TRY(lora_shrink<T>(dY, p->d_out, (const T*)w.Bt, p->rank, p->scale, offsets, p->E, n, map, (T*)w.V, st));
   }
   if (dX) {
     HMOE_TRY(lora_transpose<T, false>(p->A, w.At, p->E, p->rank, p->d_in, offsets, st));
-    HMOE_TRY(lora_gemm<T, false>(dY, (const T*)p->W, nullptr, (const T*)w.V, (const T*)w.At, p->rank, offsets, p->E, n,
-                                    p->d_in, p->d_out, perm, dX, st));
+    const T *W = (const T*)p->W, *V = (const T*)w.V, *At = (const T*)w.At;
+    if constexpr (sizeof(T) == 2) {
+      if (gather)
+        HMOE_TRY(lora_gemm_on<LoraTile<T, false>, false, true>(dY, W, (const T*)nullptr, V, At, p->rank, offsets, p->E, n,
+                                                               p->d_in, p->d_out, perm, dX, st));
+    }
+    if (!gather)
+      HMOE_TRY(lora_gemm<T, false>(dY, W, nullptr, V, At, p->rank, offsets, p->E, n, p->d_in, p->d_out, perm, dX, st));
   }
-  if (dB)
-    HMOE_TRY(lora_grad<T, false>(dY, p->d_out, U, p->rank, offsets, p->E, n, dB, w.part, st));
-  if (dA)
-    HMOE_TRY(lora_grad<T, true>(X, p->d_in, (const T*)w.V, p->rank, offsets, p->E, n, dA, w.part, st));
+  if (dB) HMOE_TRY(lora_grad<T, false>(dY, p->d_out, map, U, p->rank, offsets, p->E, n, dB, w.part, st));
+  if (dA) HMOE_TRY(lora_grad<T, true>(X, p->d_in, nullptr, (const T*)w.V, p->rank, offsets, p->E, n, dA, w.part, st));
   return HMOE_OK;
 }
 
