@@ -504,13 +504,15 @@ struct GatherTile : PipeTile<C, true, B_KC> {
 };
 
 // out[map[m]] = A[m] W^T + bias + U[m] B_e^T.   W_KC: W [cols][Kd], otherwise [Kd][cols].  GATHER: A's rows are
-// in out's order, too.
+// in out's order, too.  blockIdx.y: the split of the reduction where gridDim.y > 1; the sums of split s then go to
+// part[s][n][cols], for k_lora_gemm_join.
 template <class C, bool W_KC, bool GATHER>
 __global__ void __launch_bounds__(C::THREADS)
     k_lora_gemm(const typename C::type* __restrict__ A, const typename C::type* __restrict__ W,
                 const typename C::type* __restrict__ bias, const typename C::type* __restrict__ U,
                 const typename C::type* __restrict__ B, int rank, const int32_t* __restrict__ seg, int E, int64_t n,
-                int cols, int Kd, const int32_t* __restrict__ map, typename C::type* __restrict__ out) {
+                int cols, int Kd, const int32_t* __restrict__ map, typename C::type* __restrict__ out,
+                float* __restrict__ part) {
   using T = typename C::type;
   extern __shared__ __attribute__((aligned(16))) char smem_raw[];
   lds<char>* smem = (lds<char>*)smem_raw;
@@ -522,8 +524,17 @@ __global__ void __launch_bounds__(C::THREADS)
     GatherTile<C, W_KC> g;
     g.prime(A, Kd, map + tc.m0, tc.m_rows, Wt, W_KC ? Kd : cols, tc.n_cols, Kd, smem);
     g.run(smem, acc);
-  } else {
+  } else if (C::PIPE || gridDim.y == 1) {
     gemm_tile<C, true, W_KC>(A + tc.m0 * Kd, Kd, tc.m_rows, Wt, W_KC ? Kd : cols, tc.n_cols, Kd, smem, acc);
+  } else {
+    const int stages = (Kd + C::BK - 1) / C::BK, s = blockIdx.y;
+    const int k0 = stages * s / gridDim.y * C::BK, to = stages * (s + 1) / gridDim.y * C::BK, k1 = to < Kd ? to : Kd;
+    gemm_tile<C, true, W_KC>(A + tc.m0 * Kd + k0, Kd, tc.m_rows, W_KC ? Wt + k0 : Wt + (int64_t)k0 * cols,
+                             W_KC ? Kd : cols, tc.n_cols, k1 - k0, smem, acc);
+    if (s == 0) lora_extend<C>(tc, acc, U, B, rank, cols, seg, E);
+    store_out<C, float>(tc, acc, smem, part + s * n * cols, cols, [](int, int, int, float v) { return v; }, RowId{tc.m0},
+                        NoVec{});
+    return;
   }
   lora_extend<C>(tc, acc, U, B, rank, cols, seg, E);
   using F = Frag<C>;
@@ -538,36 +549,55 @@ __global__ void __launch_bounds__(C::THREADS)
                   LoraRow{map, tc.m0}, NoVec{});
 }
 
-// out [E][cols][rows] = in [E][rows][cols] for the adapters that have rows, one to a blockIdx.y.  The short
-// side is the rank: a workgroup takes all of it (16-byte vectors, 128 at most) and 64 of the long side.
-// TALL: rows is the long side.
-template <typename T, bool TALL>
-__global__ void __launch_bounds__(256) k_lora_transpose(const T* __restrict__ in, T* __restrict__ out, int rows, int cols,
+// Four columns to a thread.
+template <typename T>
+__global__ void __launch_bounds__(256) k_lora_gemm_join(const float* __restrict__ part, int splits, int64_t n, int cols,
+                                                        const T* __restrict__ bias, const int32_t* __restrict__ map,
+                                                        T* __restrict__ out) {
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4, size = n * cols;
+  if (i >= size) return;
+  const int64_t m = i / cols;
+  const int c = (int)(i - m * cols);
+  floatx4 v = *reinterpret_cast<const floatx4*>(part + i);
+  for (int s = 1; s < splits; ++s) v += *reinterpret_cast<const floatx4*>(part + s * size + i);
+  quad<T> y;
+#pragma unroll
+  for (int z = 0; z < 4; ++z) y[z] = from_f32<T>(v[z] + (bias ? to_f32(bias[c + z]) : 0.f));
+  *reinterpret_cast<quad<T>*>(out + (map ? map[m] : m) * cols + c) = y;
+}
+
+// Bt [E][rank][o] = B [E][o][rank] and At [E][d][rank] = A [E][rank][d] for the adapters that have rows, one to
+// a blockIdx.y; blockIdx.x: 64 of o, then 64 of d.  A workgroup takes all of the rank, in 16-byte vectors.
+template <typename T>
+__global__ void __launch_bounds__(256) k_lora_transpose(const T* __restrict__ B, T* __restrict__ Bt, int o,
+                                                        const T* __restrict__ A, T* __restrict__ At, int d, int rank,
                                                         const int32_t* __restrict__ seg) {
   constexpr int N = 16 / sizeof(T);
-  __shared__ T s[64 * (HMOE_LORA_RANK + 1)];  // [long][short], odd rows of it
+  __shared__ T s[64 * (HMOE_LORA_RANK + 1)];  // [long][rank], odd rows of it
   const int e = blockIdx.y;
   if (seg[e] == seg[e + 1]) return;
-  const int rank = TALL ? cols : rows, size = TALL ? rows : cols;
-  const int p0 = blockIdx.x * 64, valid = size - p0 < 64 ? size - p0 : 64, ld = rank + 1;
-  const int64_t base = (int64_t)e * rows * cols;
-  const auto walk = [&](const bool tall, auto body) {  // vectors along the rank, or along the long side
-    const int vecs = tall ? rank / N : valid / N, lines = tall ? valid : rank;
+  const int of_b = (o + 63) / 64;
+  const bool tall = (int)blockIdx.x < of_b;  // the long side is the rows
+  const int size = tall ? o : d, p0 = (tall ? blockIdx.x : blockIdx.x - of_b) * 64;
+  const int valid = size - p0 < 64 ? size - p0 : 64, ld = rank + 1;
+  const T* in = (tall ? B : A) + (int64_t)e * size * rank;
+  T* out = (tall ? Bt : At) + (int64_t)e * size * rank;
+  const auto walk = [&](bool along_rank, auto body) {  // vectors along the rank, or along the long side
+    const int vecs = along_rank ? rank / N : valid / N, lines = along_rank ? valid : rank;
     for (int q = threadIdx.x; q < vecs * lines; q += 256) {
       const int line = q / vecs, v = (q - line * vecs) * N;
-      const int64_t at = tall ? (int64_t)(p0 + line) * rank + v : (int64_t)line * size + p0 + v;
-      const int first = tall ? line * ld + v : v * ld + line, step = tall ? 1 : ld;
-      body(base + at, first, step);
+      const int64_t at = along_rank ? (int64_t)(p0 + line) * rank + v : (int64_t)line * size + p0 + v;
+      body(at, along_rank ? line * ld + v : v * ld + line, along_rank ? 1 : ld);
     }
   };
-  walk(TALL, [&](int64_t at, int first, int step) {
+  walk(tall, [&](int64_t at, int first, int step) {
     const i32x4 v = *reinterpret_cast<const i32x4*>(in + at);
     const T* x = reinterpret_cast<const T*>(&v);
 #pragma unroll
     for (int z = 0; z < N; ++z) s[first + z * step] = x[z];
   });
   __syncthreads();
-  walk(!TALL, [&](int64_t at, int first, int step) {
+  walk(!tall, [&](int64_t at, int first, int step) {
     i32x4 v;
     T* x = reinterpret_cast<T*>(&v);
 #pragma unroll
@@ -736,13 +766,22 @@ __global__ void __launch_bounds__(256) k_lora_grad(const T* __restrict__ D, int 
       }
 }
 
-// The pieces of an adapter added in their order; adapters without rows get zeros.
-__global__ void __launch_bounds__(256) k_lora_grad_join(const float* __restrict__ part, const int32_t* __restrict__ seg,
-                                                        int piece, int64_t size, float* __restrict__ out) {
+// The pieces of an adapter added in their order; adapters without rows get zeros.  Both gradients in one launch:
+// blockIdx.x runs over dB's outputs and then dA's (either may be missing: size 0), four to a thread.
+struct GradJoin {
+  const float* part;
+  float* out;
+  int64_t size;  // of an adapter
+};
+__global__ void __launch_bounds__(256) k_lora_grad_join(GradJoin b, GradJoin a, const int32_t* __restrict__ seg, int piece) {
   const int e = blockIdx.y;
-  const int64_t pieces = cdiv(seg[e + 1] - seg[e], piece);
+  const int64_t pieces = cdiv(seg[e + 1] - seg[e], piece), first = cdiv(b.size, 1024);
   if (pieces == 1) return;
-  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  const bool is_b = blockIdx.x < first;
+  const float* part = is_b ? b.part : a.part;
+  float* out = is_b ? b.out : a.out;
+  const int64_t size = is_b ? b.size : a.size;
+  const int64_t i = ((blockIdx.x - (is_b ? 0 : first)) * 256 + threadIdx.x) * 4;
   if (i >= size) return;
   floatx4 s = {0.f, 0.f, 0.f, 0.f};
   const float* p = part + lora_piece_slot(seg[e], 0, piece) * size + i;
@@ -773,20 +812,40 @@ bool lora_small(int64_t n, int cols) {
   using C = LoraTile<T, W_KC>;
   return cdiv(n, C::BM) * cdiv(cols, C::BN) < device_cus();
 }
+// Splits of the reduction: for fewer quarter tiles than CUs, of two stages at least (777 x 64 fp32 outputs of 1000
+// products, 13 tiles: 36 us, 10 in eight splits with the launch that joins them).
+template <typename T>
+int lora_gemm_splits(int64_t n, int cols, int Kd) {
+  using Q = CfgQuarter<T>;
+  const int64_t tiles = cdiv(n, Q::BM) * cdiv(cols, Q::BN);
+  if (tiles >= device_cus()) return 1;
+  const int64_t fill = device_cus() / tiles, stages = Kd / (2 * Q::BK), s = fill < stages ? fill : stages;
+  return s < 4 ? 1 : (s > 8 ? 8 : (int)s);
+}
+template <typename T>
+size_t lora_gemm_part(int64_t n, int cols, int Kd) {
+  const int s = lora_gemm_splits<T>(n, cols, Kd);
+  return s > 1 ? (size_t)s * n * cols : 0;
+}
 template <class C, bool W_KC, bool GATHER, typename T>
 int lora_gemm_on(const T* A, const T* W, const T* bias, const T* U, const T* B, int rank, const int32_t* seg, int E,
-                 int64_t n, int cols, int Kd, const int32_t* map, T* out, hipStream_t st) {
+                 int64_t n, int cols, int Kd, const int32_t* map, T* out, int splits, float* part, hipStream_t st) {
   HMOE_LAUNCH(W_KC ? "lora forward" : "lora input gradient", (k_lora_gemm<C, W_KC, GATHER>),
-              dim3((unsigned)(cdiv(n, C::BM) * cdiv(cols, C::BN))), dim3(C::THREADS), C::LDS, st, A, W, bias, U, B, rank, seg,
-              E, n, cols, Kd, map, out);
+              dim3((unsigned)(cdiv(n, C::BM) * cdiv(cols, C::BN)), (unsigned)splits), dim3(C::THREADS), C::LDS, st, A, W,
+              bias, U, B, rank, seg, E, n, cols, Kd, map, out, part);
   return HMOE_OK;
 }
 template <typename T, bool W_KC>
 int lora_gemm(const T* A, const T* W, const T* bias, const T* U, const T* B, int rank, const int32_t* seg, int E,
-              int64_t n, int cols, int Kd, const int32_t* map, T* out, hipStream_t st) {
-  if (lora_small<T, W_KC>(n, cols))
-    return lora_gemm_on<CfgQuarter<T>, W_KC, false>(A, W, bias, U, B, rank, seg, E, n, cols, Kd, map, out, st);
-  return lora_gemm_on<LoraTile<T, W_KC>, W_KC, false>(A, W, bias, U, B, rank, seg, E, n, cols, Kd, map, out, st);
+              int64_t n, int cols, int Kd, const int32_t* map, T* out, float* part, hipStream_t st) {
+  if (!lora_small<T, W_KC>(n, cols))
+    return lora_gemm_on<LoraTile<T, W_KC>, W_KC, false>(A, W, bias, U, B, rank, seg, E, n, cols, Kd, map, out, 1, nullptr, st);
+  const int splits = lora_gemm_splits<T>(n, cols, Kd);
+  HMOE_TRY((lora_gemm_on<CfgQuarter<T>, W_KC, false>(A, W, bias, U, B, rank, seg, E, n, cols, Kd, map, out, splits, part, st)));
+  if (splits > 1)
+    HMOE_LAUNCH("lora join", k_lora_gemm_join<T>, dim3((unsigned)cdiv(n * cols, 1024)), dim3(256), 0, st, part, splits, n,
+                cols, bias, map, out);
+  return HMOE_OK;
 }
 
 template <typename T, int UW, int BW, bool U_LEFT>
@@ -798,9 +857,6 @@ int lora_grad_tiles(const T* D, int width, const int32_t* map, const T* U, int r
               dim3((unsigned)(n / piece + (E < n ? E : n)), (unsigned)cdiv(width, BW),
                    (unsigned)cdiv(u_width<T>(rank), UW)),
               dim3(256), C::LDS, st, D, width, map, U, rank, seg, E, piece, out, part);
-  const int64_t size = (int64_t)width * rank;
-  HMOE_LAUNCH("lora gradient join", k_lora_grad_join, dim3((unsigned)cdiv(size, 1024), (unsigned)E), dim3(256), 0, st,
-              part, seg, piece, size, out);
   return HMOE_OK;
 }
 template <typename T, bool U_LEFT>
@@ -816,7 +872,7 @@ int lora_grad(const T* D, int width, const int32_t* map, const T* U, int rank, c
 
 struct LoraSpace {
   void *dYs, *Bt, *At, *V;
-  float* part;
+  float *part_a, *part_b, *split;  // of the adapters' gradients' sums, and of the products'
 };
 
 LoraSpace lora_carve(const hmoe_lora_t* p, int64_t n, Workspace& ws) {
@@ -826,9 +882,13 @@ LoraSpace lora_carve(const hmoe_lora_t* p, int64_t n, Workspace& ws) {
   x.Bt = ws.take<char>((size_t)p->E * p->rank * p->d_out * s);
   x.At = ws.take<char>((size_t)p->E * p->rank * p->d_in * s);
   x.V = ws.take<char>((size_t)n * ldu * s);
-  const size_t wide = p->d_out > p->d_in ? p->d_out : p->d_in;
   const int64_t piece = lora_piece(n);
-  x.part = ws.take<float>(n > piece ? (2 * (n / piece) + 2) * wide * p->rank : 0);
+  const size_t pieces = n > piece ? 2 * (n / piece) + 2 : 0;
+  x.part_a = ws.take<float>(pieces * p->d_in * p->rank);
+  x.part_b = ws.take<float>(pieces * p->d_out * p->rank);
+  const size_t fwd = p->dt == HMOE_BF16 ? lora_gemm_part<bf16>(n, p->d_out, p->d_in) : lora_gemm_part<float>(n, p->d_out, p->d_in);
+  const size_t bwd = p->dt == HMOE_BF16 ? lora_gemm_part<bf16>(n, p->d_in, p->d_out) : lora_gemm_part<float>(n, p->d_in, p->d_out);
+  x.split = ws.take<float>(fwd > bwd ? fwd : bwd);
   return x;
 }
 
@@ -837,14 +897,7 @@ int lora_forward_t(const hmoe_lora_t* p, int64_t n, const T* X, const int32_t* o
                    const LoraSpace& w, hipStream_t st) {
   HMOE_TRY(lora_shrink<T>(X, p->d_in, (const T*)p->A, p->rank, p->scale, offsets, p->E, n, nullptr, U, st));
   return lora_gemm<T, true>(X, (const T*)p->W, (const T*)p->b, U, (const T*)p->B, p->rank, offsets, p->E, n, p->d_out,
-                               p->d_in, perm, Y, st);
-}
-
-template <typename T, bool TALL>
-int lora_transpose(const void* in, void* out, int E, int rows, int cols, const int32_t* seg, hipStream_t st) {
-  HMOE_LAUNCH("lora transpose", (k_lora_transpose<T, TALL>), dim3((unsigned)cdiv(TALL ? rows : cols, 64), (unsigned)E),
-              dim3(256), 0, st, (const T*)in, (T*)out, rows, cols, seg);
-  return HMOE_OK;
+                            p->d_in, perm, Y, w.split, st);
 }
 
 template <typename T>
@@ -860,22 +913,29 @@ int lora_backward_t(const hmoe_lora_t* p, int64_t n, const T* X, const int32_t* 
     dY = (const T*)w.dYs;
   }
   if (dX || dA) {
-    HMOE_TRY(lora_transpose<T, true>(p->B, w.Bt, p->E, p->d_out, p->rank, offsets, st));
+    HMOE_LAUNCH("lora transpose", k_lora_transpose<T>,
+                dim3((unsigned)(cdiv(p->d_out, 64) + (dX ? cdiv(p->d_in, 64) : 0)), (unsigned)p->E), dim3(256), 0, st,
+                (const T*)p->B, (T*)w.Bt, p->d_out, (const T*)p->A, (T*)w.At, p->d_in, p->rank, offsets);
     HMOE_TRY(lora_shrink<T>(dY, p->d_out, (const T*)w.Bt, p->rank, p->scale, offsets, p->E, n, map, (T*)w.V, st));
   }
   if (dX) {
-    HMOE_TRY(lora_transpose<T, false>(p->A, w.At, p->E, p->rank, p->d_in, offsets, st));
     const T *W = (const T*)p->W, *V = (const T*)w.V, *At = (const T*)w.At;
     if constexpr (sizeof(T) == 2) {
       if (gather)
         HMOE_TRY(lora_gemm_on<LoraTile<T, false>, false, true>(dY, W, (const T*)nullptr, V, At, p->rank, offsets, p->E, n,
-                                                               p->d_in, p->d_out, perm, dX, st));
+                                                               p->d_in, p->d_out, perm, dX, 1, nullptr, st));
     }
     if (!gather)
-      HMOE_TRY(lora_gemm<T, false>(dY, W, nullptr, V, At, p->rank, offsets, p->E, n, p->d_in, p->d_out, perm, dX, st));
+      HMOE_TRY(lora_gemm<T, false>(dY, W, nullptr, V, At, p->rank, offsets, p->E, n, p->d_in, p->d_out, perm, dX, w.split, st));
   }
-  if (dB) HMOE_TRY(lora_grad<T, false>(dY, p->d_out, map, U, p->rank, offsets, p->E, n, dB, w.part, st));
-  if (dA) HMOE_TRY(lora_grad<T, true>(X, p->d_in, nullptr, (const T*)w.V, p->rank, offsets, p->E, n, dA, w.part, st));
+  if (dB) HMOE_TRY(lora_grad<T, false>(dY, p->d_out, map, U, p->rank, offsets, p->E, n, dB, w.part_b, st));
+  if (dA) HMOE_TRY(lora_grad<T, true>(X, p->d_in, nullptr, (const T*)w.V, p->rank, offsets, p->E, n, dA, w.part_a, st));
+  if (dA || dB) {
+    const GradJoin b = {w.part_b, dB, dB ? (int64_t)p->d_out * p->rank : 0};
+    const GradJoin a = {w.part_a, dA, dA ? (int64_t)p->d_in * p->rank : 0};
+    HMOE_LAUNCH("lora gradient join", k_lora_grad_join, dim3((unsigned)(cdiv(b.size, 1024) + cdiv(a.size, 1024)), (unsigned)p->E),
+                dim3(256), 0, st, b, a, offsets, lora_piece(n));
+  }
   return HMOE_OK;
 }
 
