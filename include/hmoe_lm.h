@@ -130,7 +130,7 @@ int hmoe_lora_few(const hmoe_lora_t* p, int64_t n, const void* X, const int32_t*
  * perm int32[n] (slot -> sample, a permutation), or NULL: Y's rows are in slot order too.
  *   Y [n x d_out] out, sample order.
  *   U [n][hmoe_lora_saved_width] out, dtype dt: scale A x of every row with an adapter, for the
- *     backward: fp32 values; with bf16 data blocks of 16 values and 16 remainders, so that U is good to 2^-16. */
+ *     backward, in fp32: with bf16 data as three bf16 numbers a value, in blocks of 16 values. */
 int32_t hmoe_lora_saved_width(int32_t rank, hmoe_dtype_t dt);
 size_t hmoe_lora_workspace(const hmoe_lora_t* p, int64_t n);
 int hmoe_lora_forward(const hmoe_lora_t* p, int64_t n, const void* X_sorted, const int32_t* offsets,

@@ -136,23 +136,24 @@ __device__ __forceinline__ void stream_groups(const T* const (&wb)[MI], const ui
       wb, wo, [&](int j, int f, uint32_t at) { return reinterpret_cast<const char*>(xr[j][f]) + at; }, kd, g0, g1, body);
 }
 
-// A value that feeds a bf16 product without losing its low bits: v = hi + lo up to 2^-16 of it, each a
-// bf16 operand of its own MFMA.  hi is cut off rather than rounded, so that no finite v becomes
-// infinite.  (fp32 data: the value itself.)
-template <typename T>
-struct Halves {
-  static constexpr int N = sizeof(T) == 2 ? 2 : 1;
+// An fp32 value as M bf16 numbers that add up to it, each an operand of its own MFMA: two are good to 2^-16 of
+// the value, three hold all of its bits.  All but the last are cut off rather than rounded, so that no
+// finite value becomes infinite.  (fp32 data: the value itself.)
+template <typename T, int M>
+struct Parts {
+  static constexpr int N = sizeof(T) == 2 ? M : 1;
   T part[N];
-  __device__ __forceinline__ explicit Halves(float v) {
-    if constexpr (N == 1) {
-      part[0] = v;
-    } else {
-      const float hi = __uint_as_float(__float_as_uint(v) & 0xffff0000u);
-      part[0] = from_f32<T>(hi);
-      part[1] = from_f32<T>(fabsf(v) == INFINITY ? 0.f : v - hi);
+  __device__ __forceinline__ explicit Parts(float v) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float hi = i + 1 < N ? __uint_as_float(__float_as_uint(v) & 0xffff0000u) : v;
+      part[i] = from_f32<T>(hi);
+      v = fabsf(v) == INFINITY ? 0.f : v - hi;
     }
   }
 };
+template <typename T>
+using Halves = Parts<T, 2>;
 
 // The slot-th of the groups 0 .. G - 1 that have rows, in ascending order, and its rows of the `total`
 // in ascending order, at most HMOE_FEW_ROWS.  A row whose group is outside [0, G) has none.  False if

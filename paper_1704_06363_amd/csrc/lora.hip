@@ -3,10 +3,11 @@
 // and its gradients with W fixed:  with V_i = s_a B_a^T dY_i,
 //   dX_i = W^T dY_i + A_a^T V_i,   dB_a = sum_i dY_i (s_a A_a x_i)^T,   dA_a = sum_i V_i x_i^T.
 //
-// The narrow products U = s A x and V stay in fp32 accuracy: for bf16 data each value is kept as two
-// bf16 numbers, and since the fragments of one MFMA step hold 32 values of K, 16 values of U with their
-// remainders fill exactly one step against 16 values of B taken twice (row layout of U below).  The
-// second number costs no instruction and makes the fp32 gradients good to 2^-16 instead of 2^-9.
+// The narrow products U = s A x and V keep their fp32 accuracy: for bf16 data each value is kept as bf16
+// numbers that add up to it.  The fragments of one MFMA step hold 32 values of K, so 16 values of U with
+// their remainders fill exactly one step against 16 values of B taken twice: the products that Y and dX
+// take, which are rounded to bf16 once, are good to 2^-16 at no instruction more than rounded values would cost.
+// The adapters' gradients are fp32, and take a third number: all bits of U and V.
 #include "fewrows.hpp"
 #include "gemm.hpp"
 #include "lm_launch.hpp"
@@ -16,18 +17,19 @@ namespace hmoe {
 
 namespace {
 
-// A row of U or V: bf16: blocks of 32, 16 values of the rank (zeros past it) and then their
-// remainders; fp32: the values.
+// A row of U or V: bf16: blocks of 16 M, 16 values of the rank (zeros past it), then their remainders, and (M = 3)
+// the remainders of those; fp32: the values.  Few rows, which have no gradient, take M = 2.
+constexpr int kUParts = 3;
 __host__ __device__ inline int u_blocks(int rank) { return (rank + 15) / 16; }
-template <typename T>
+template <typename T, int M = kUParts>
 __host__ __device__ inline int u_width(int rank) {
-  return sizeof(T) == 2 ? 32 * u_blocks(rank) : rank;
+  return sizeof(T) == 2 ? 16 * M * u_blocks(rank) : rank;
 }
 
 // This lane's 16 bytes of step kb of row `row` of U.
 template <typename T>
 __device__ __forceinline__ i32x4 u_frag(const T* __restrict__ U, int64_t row, int ldu, int kb, int lg, int rank) {
-  if constexpr (sizeof(T) == 2) return *reinterpret_cast<const i32x4*>(U + row * ldu + 32 * kb + 8 * lg);
+  if constexpr (sizeof(T) == 2) return *reinterpret_cast<const i32x4*>(U + row * ldu + 16 * kUParts * kb + 8 * lg);
   return 16 * kb + 4 * lg < rank ? *reinterpret_cast<const i32x4*>(U + row * ldu + 16 * kb + 4 * lg) : i32x4{0, 0, 0, 0};
 }
 // And of the row of `rank` values that multiplies it (bf16: the same for the value and its remainder).
@@ -61,19 +63,19 @@ __device__ __forceinline__ i32x4 rank_pick(i32x4 v, int kb, int lr, int lg, int 
 }
 
 // Stores four values 16 kb + 4 lg .. of a row of U (those past the rank as zeros).
-template <typename T>
+template <typename T, int M>
 __device__ __forceinline__ void u_store(T* __restrict__ U, int64_t row, int ldu, int kb, int lg, int rank, floatx4 v) {
   const bool in = 16 * kb + 4 * lg < rank;  // the rank is a multiple of 8
   if constexpr (sizeof(T) == 2) {
-    vec4<T> hi, lo;
+    quad<T> q[M];
 #pragma unroll
     for (int z = 0; z < 4; ++z) {
-      const Halves<T> p(in ? v[z] : 0.f);
-      hi[z] = p.part[0];
-      lo[z] = p.part[1];
+      const Parts<T, M> p(in ? v[z] : 0.f);
+#pragma unroll
+      for (int i = 0; i < M; ++i) q[i][z] = p.part[i];
     }
-    *reinterpret_cast<vec4<T>*>(U + row * ldu + 32 * kb + 4 * lg) = hi;
-    *reinterpret_cast<vec4<T>*>(U + row * ldu + 32 * kb + 16 + 4 * lg) = lo;
+#pragma unroll
+    for (int i = 0; i < M; ++i) *reinterpret_cast<quad<T>*>(U + row * ldu + 16 * (M * kb + i) + 4 * lg) = q[i];
   } else if (in) {
     *reinterpret_cast<floatx4*>(U + row * ldu + 16 * kb + 4 * lg) = v;
   }
@@ -128,7 +130,7 @@ __global__ void __launch_bounds__(64 * kFewShrinkWaves) k_lora_few_shrink(LoraFe
   __shared__ floatx4 s_acc[NW][64];
   const int blocks = u_blocks(a.rank), kb = blockIdx.x % blocks;
   if (!few_group<64 * NW>(a.adapter, a.n, a.E, blockIdx.x / blocks, &s_group, s_rows, &s_count)) return;
-  const int e = s_group, count = s_count, ldu = u_width<T>(a.rank);
+  const int e = s_group, count = s_count, ldu = u_width<T, 2>(a.rank);
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6, lr = l & 15, lg = l >> 4;
   const T* A = static_cast<const T*>(a.A) + ((int64_t)uniform_int(e) * a.rank + 16 * kb) * a.d;
   uint32_t ao[1][4];
@@ -154,7 +156,7 @@ __global__ void __launch_bounds__(64 * kFewShrinkWaves) k_lora_few_shrink(LoraFe
       acc = s_acc[0][l];
 #pragma unroll
       for (int q = 1; q < NW; ++q) acc += s_acc[q][l];
-      u_store(static_cast<T*>(a.U), row, ldu, kb, lg, a.rank, acc * scale);
+      u_store<T, 2>(static_cast<T*>(a.U), row, ldu, kb, lg, a.rank, acc * scale);
     }
     __syncthreads();
   }
@@ -172,7 +174,7 @@ __global__ void __launch_bounds__(256) k_lora_few(LoraFew a) {
   __shared__ floatx4 s_a[RB > 0 ? 4 : 1][RB > 0 ? RB : 1][64];
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6, lr = l & 15, lg = l >> 4;
   const int c0 = blockIdx.x * 16 * MI;
-  const int ldu = u_width<T>(a.rank), blocks = u_blocks(a.rank), urow = ldu * (int)sizeof(T) + 16;
+  const int ldu = u_width<T, 2>(a.rank), blocks = u_blocks(a.rank), urow = ldu * (int)sizeof(T) + 16;
   const int all = a.adapter[l < a.n ? l : a.n - 1];  // a lane to a row
   lds<char>* s_u = (lds<char>*)s_mem;
   if constexpr (RB == 0) {  // U, 16-byte pieces
@@ -239,7 +241,7 @@ __global__ void __launch_bounds__(256) k_lora_few(LoraFew a) {
     if (w < RB && lr == 0) {
       const int e = all >= 0 && all < a.E ? all : 0;
       floatx4 u = (s_a[0][w][l] + s_a[1][w][l]) + (s_a[2][w][l] + s_a[3][w][l]);
-      u_store((T*)s_mem, 0, ldu, w, lg, a.rank, u * (a.scale ? a.scale[e] : 1.f));
+      u_store<T, 2>((T*)s_mem, 0, ldu, w, lg, a.rank, u * (a.scale ? a.scale[e] : 1.f));
     }
   }
   __syncthreads();
@@ -398,7 +400,7 @@ __global__ void __launch_bounds__(256) k_lora_shrink(const T* __restrict__ X, in
     const int i = q / MT, t = q % MT;
     if (kb0 + i >= u_blocks(rank) || 16 * t + lr >= rows) continue;
     const floatx4 v = (s_acc[0][i][t][l] + s_acc[1][i][t][l]) + (s_acc[2][i][t][l] + s_acc[3][i][t][l]);
-    u_store(U, r0 + 16 * t + lr, u_width<T>(rank), kb0 + i, lg, rank, v * sc);
+    u_store<T, kUParts>(U, r0 + 16 * t + lr, u_width<T>(rank), kb0 + i, lg, rank, v * sc);
   }
 }
 
@@ -628,8 +630,7 @@ __device__ __forceinline__ int64_t lora_piece_slot(int64_t seg_e, int64_t local,
 // each.  64 where 256 leave CUs idle.
 template <typename T, int UW, int BW, bool U_LEFT>
 struct GradTile {
-  static constexpr int W = BW / (BW == 256 ? 4 : 2), V = BW == 256 ? UW : UW / 2;
-  using type = typename std::conditional<U_LEFT, Cfg<T, UW, BW, V, W>, Cfg<T, BW, UW, W, V>>::type;
+  using type = typename std::conditional<U_LEFT, Cfg<T, UW, BW, UW, BW / 4>, Cfg<T, BW, UW, BW / 4, UW>>::type;
 };
 
 // A K-strided operand (gemm.hpp's Stager) whose K row k is at base + rows[k] ld.
@@ -749,6 +750,7 @@ __global__ void __launch_bounds__(256) k_lora_grad(const T* __restrict__ D, int 
     if (c < rank && m < width) to[U_LEFT ? (int64_t)c * width + m : (int64_t)m * rank + c] = v;
   };
   constexpr bool BF = sizeof(T) == 2;  // the sums with 16 values and with their remainders are one
+  static_assert(!BF || UW % (16 * kUParts) == 0, "whole blocks of U");
 #pragma unroll
   for (int i = 0; i < C::MI; ++i)
 #pragma unroll
@@ -756,9 +758,11 @@ __global__ void __launch_bounds__(256) k_lora_grad(const T* __restrict__ D, int 
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         if constexpr (BF && U_LEFT) {
-          if (i % 2 == 0) put((u0 + f.wm * C::WM) / 2 + 8 * i + 4 * f.lg + r, d0 + f.col(j, r), acc[i][j][r] + acc[i + 1][j][r]);
+          if (i % 3 == 0)
+            put(u0 / 3 + 16 * (i / 3) + 4 * f.lg + r, d0 + f.col(j, r), (acc[i + 2][j][r] + acc[i + 1][j][r]) + acc[i][j][r]);
         } else if constexpr (BF) {
-          if (j % 2 == 0) put((u0 + f.wn * C::WN) / 2 + 8 * j + f.lr, d0 + f.row(i, r), acc[i][j][r] + acc[i][j + 1][r]);
+          if (j % 3 == 0)
+            put(u0 / 3 + 16 * (j / 3) + f.lr, d0 + f.row(i, r), (acc[i][j + 2][r] + acc[i][j + 1][r]) + acc[i][j][r]);
         } else {
           if constexpr (U_LEFT) put(u0 + f.row(i, r), d0 + f.col(j, r), acc[i][j][r]);
           else put(u0 + f.col(j, r), d0 + f.row(i, r), acc[i][j][r]);
@@ -862,12 +866,12 @@ int lora_grad_tiles(const T* D, int width, const int32_t* map, const T* U, int r
 template <typename T, bool U_LEFT>
 int lora_grad(const T* D, int width, const int32_t* map, const T* U, int rank, const int32_t* seg, int E, int64_t n, float* out, float* part,
               hipStream_t st) {
-  const int ldu = u_width<T>(rank);
+  constexpr int NARROW = sizeof(T) == 2 ? 48 : 32;  // rank 16, 32
   if ((n / lora_piece(n) + (E < n ? E : n)) * cdiv(width, 256) < device_cus())
-    return lora_grad_tiles<T, 64, 64, U_LEFT>(D, width, map, U, rank, seg, E, n, out, part, st);
-  if (ldu <= 32) return lora_grad_tiles<T, 32, 256, U_LEFT>(D, width, map, U, rank, seg, E, n, out, part, st);
-  if (ldu <= 64) return lora_grad_tiles<T, 64, 256, U_LEFT>(D, width, map, U, rank, seg, E, n, out, part, st);
-  return lora_grad_tiles<T, 128, 256, U_LEFT>(D, width, map, U, rank, seg, E, n, out, part, st);
+    return lora_grad_tiles<T, NARROW, 64, U_LEFT>(D, width, map, U, rank, seg, E, n, out, part, st);
+  if (u_width<T>(rank) <= NARROW)
+    return lora_grad_tiles<T, NARROW, 256, U_LEFT>(D, width, map, U, rank, seg, E, n, out, part, st);
+  return lora_grad_tiles<T, 2 * NARROW, 256, U_LEFT>(D, width, map, U, rank, seg, E, n, out, part, st);
 }
 
 struct LoraSpace {
@@ -943,9 +947,13 @@ int lora_backward_t(const hmoe_lora_t* p, int64_t n, const T* X, const int32_t* 
 
 int lora_saved_width(int rank, hmoe_dtype_t dt) { return dt == HMOE_BF16 ? u_width<bf16>(rank) : u_width<float>(rank); }
 
+static int lora_few_width(const hmoe_lora_t* p) {
+  return p->dt == HMOE_BF16 ? u_width<bf16, 2>(p->rank) : u_width<float>(p->rank);
+}
+
 size_t lora_few_ws(const hmoe_lora_t* p, int64_t n) {
   Workspace w(nullptr, 0);
-  w.take<char>((size_t)n * lora_saved_width(p->rank, p->dt) * dtype_size(p->dt));
+  w.take<char>((size_t)n * lora_few_width(p) * dtype_size(p->dt));
   return w.off;
 }
 
@@ -958,7 +966,7 @@ size_t lora_ws(const hmoe_lora_t* p, int64_t n) {
 int launch_lora_few(const hmoe_lora_t* p, int64_t n, const void* X, const int32_t* adapter, void* Y, Workspace& ws,
                     hipStream_t st) {
   LoraFew a = {X, p->W, p->b, p->A, p->B, p->scale, adapter, (int)n, p->E, p->d_in, p->d_out, p->rank, nullptr, Y};
-  a.U = ws.take<char>((size_t)n * lora_saved_width(p->rank, p->dt) * dtype_size(p->dt));
+  a.U = ws.take<char>((size_t)n * lora_few_width(p) * dtype_size(p->dt));
   return p->dt == HMOE_BF16 ? lora_few_t<bf16>(a, st) : lora_few_t<float>(a, st);
 }
 

@@ -174,7 +174,7 @@ def test_lora_refusals(lib):
     refused(bwd(dX=8), -3, "dX")
     refused(bwd(dA=8), -3, "dA")
     assert few(n=0, X=None) == 0 and fwd(n=0, X=None) == 0
-    assert lib.hmoe_lora_saved_width(24, 1) == 64 and lib.hmoe_lora_saved_width(24, 0) == 24
+    assert lib.hmoe_lora_saved_width(24, 1) == 96 and lib.hmoe_lora_saved_width(24, 0) == 24
 
 
 def test_lora_binding_refusals():
