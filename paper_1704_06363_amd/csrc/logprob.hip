@@ -113,8 +113,11 @@ struct TopList {
   }
   // Entries not above this are not listed (of -inf none are: finish_row finds those).
   __device__ __forceinline__ float below() const {
-    const uint32_t hi = (uint32_t)(floor >> 32) - ((uint32_t)floor == 0 ? 1u : 0u);
-    return (uint32_t)(floor >> 32) <= kKeyMinusInf ? -INFINITY : key_value((uint64_t)hi << 32);
+    const uint32_t hi = (uint32_t)(floor >> 32);
+    // entries equal to a bound's value pass, to one that has its own index do not; what precedes +0 is -0, which
+    // is not below it
+    const uint32_t step = (uint32_t)floor != 0 ? 0u : (hi == 0x80000000u ? 2u : 1u);
+    return hi <= kKeyMinusInf ? -INFINITY : key_value((uint64_t)(hi - step) << 32);
   }
   // Lists the lanes' entries x at `index` that are `in` and above the floor.
   __device__ __forceinline__ void add(float x, uint32_t index, bool in, lds<uint64_t>* buf, int m) {

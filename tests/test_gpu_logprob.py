@@ -171,6 +171,20 @@ def test_masked_infinite_and_missing_entries(dtype, n, V):
     check(x, t, 16, 0.5)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,V,m", [(3, 5, 5), (6, 700, 16), (4, 30000, 9), (1300, 300, 3)])
+def test_zeros_of_either_sign_among_the_best(dtype, n, V, m):
+    """Rows whose m-th entry is +0 or -0 (equal, by index), and rows of nothing above 0."""
+    x = -rows(n, V, 0, dtype, 6).abs() - 0.5
+    at = torch.randint(0, V, (n, 40), generator=torch.Generator().manual_seed(7)).cuda()
+    x.scatter_(1, at[:, ::2], 0.0)
+    x.scatter_(1, at[:, 1::2], -0.0)
+    x[1::3, V // 2] = 1.0
+    x[2] = 0.0
+    f, lp, ent = check(x, tokens(n, V, 8), m, 1.0)
+    check_grad(x, tokens(n, V, 8), 1.0, f, lp, ent, 9)
+
+
 def test_rows_without_a_token():
     x, t = rows(40, 999, 0, "bf16", 1), tokens(40, 999, 1)
     t[::3] = -1
@@ -243,6 +257,22 @@ def test_rows_further_apart_than_32_bits():
     t = tokens(n, V, 2)
     f, lp, ent = check(x, t, 4, 1.0)
     check_grad(x, t, 1.0, f, lp, ent, 6, in_place=True)
+
+
+def test_more_rows_than_a_launch_takes():
+    n, V = (1 << 24) + 9, 4
+    x = torch.randn(n, V, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
+    t = torch.randint(0, V, (n,), generator=torch.Generator(device="cuda").manual_seed(2), device="cuda",
+                      dtype=torch.int32)
+    f = hmoe.token_logprob(x, t, m=1)
+    lp = torch.log_softmax(x.double(), 1)
+    assert (f["logp"] - lp.gather(1, t.long()[:, None])[:, 0]).abs().max() <= 1e-5 * 2
+    first = torch.where(x == x.amax(1, keepdim=True), torch.arange(V, device="cuda"), V).amin(1)  # of equal ones
+    assert torch.equal(f["top_idx"][:, 0].long(), first)
+    g = hmoe.token_logprob_backward(x, t, f["stat"], None, torch.ones(n, device="cuda"))
+    ref = -lp.exp()
+    ref.scatter_add_(1, t.long()[:, None], torch.ones(n, 1, dtype=torch.float64, device="cuda"))
+    assert (g - ref).abs().max() <= 1e-4
 
 
 def test_streams_workspace_and_repeated_calls():
