@@ -142,6 +142,29 @@ def test_many_rows_and_gradients(dtype, n, E, d, o, r, bias, with_perm):
         close(got[k], ref[k], k)
 
 
+@pytest.mark.parametrize("dtype,d,o,r", [("bf16", 264, 136, 24), ("f32", 72, 200, 16), ("bf16", 136, 72, 40),
+                                          ("bf16", 2056, 1032, 16), ("f32", 520, 88, 32)])
+@pytest.mark.parametrize("adapter", [2, -1, 5])
+def test_one_row(dtype, d, o, r, adapter):
+    """Formed in one launch (narrow adapters) and in two, with and without an adapter."""
+    p = adapters(5, d, o, r, dtype, True, d)
+    X, ids = rows(1, d, dtype, o), np.array([adapter], np.int32)
+    close(hmoe.lora_few(p, X, torch.tensor(ids).cuda()), plain(p, X, ids)["Y"], "Y")
+
+
+@pytest.mark.parametrize("dtype,n,E,d,o,r", [
+    ("bf16", 16500, 9, 1032, 136, 24),  # whole tiles that gather dY's rows
+    ("bf16", 9000, 5, 264, 2312, 40),   # whole tiles forward
+    ("bf16", 200, 3, 1032, 72, 24),     # reductions split among workgroups
+    ("f32", 130, 4, 72, 1032, 8), ("bf16", 17000, 3, 40, 72, 48)])  # adapters of many pieces
+def test_tilings(dtype, n, E, d, o, r):
+    p = adapters(E, d, o, r, dtype, True, n + o)
+    X, dY, ids = rows(n, d, dtype, n), rows(n, o, dtype, n + 1), ids_of(n, E, n)
+    got, ref = grouped(p, X, ids, dY), plain(p, X, ids, dY)
+    for k in ("Y", "dX", "dA", "dB"):
+        close(got[k], ref[k], k)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_rows_without_adapters_and_adapters_without_rows(dtype):
     n, E, d, o, r = 600, 6, 72, 88, 16

@@ -115,6 +115,14 @@ def test_sizes_types_and_choices(dtype, n, K, d, h, o, k, act, bias):
     check(p, draw(p, n, k, dtype, n + h), k, act)
 
 
+@pytest.mark.parametrize("dtype,K,d,h,o,k,act", [
+    ("bf16", 64, 1032, 2056, 520, 4, "silu"), ("f32", 9, 520, 1032, 72, 8, "relu"), ("bf16", 700, 264, 520, 24, 1, "relu")])
+def test_one_sample(dtype, K, d, h, o, k, act):
+    """Its choices are groups of their own, their reductions split and joined."""
+    p = params(K, d, h, o, dtype, act, True, K)
+    check(p, draw(p, 1, k, dtype, 3), k, act)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_every_sample_with_one_expert(dtype):
     p = params(9, 200, 136, 72, dtype, "relu", True, 3)
