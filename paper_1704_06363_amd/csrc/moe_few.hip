@@ -32,14 +32,15 @@ __device__ __forceinline__ void clear_counts(const FewArgs& a) {
     for (int i = threadIdx.x; i < a.counts; i += blockDim.x) a.count[i] = 0;
 }
 
-// The k best of a sample's K scores, by one wave: weights, and which experts are evaluated.
-template <typename T, class Score>
-__device__ __forceinline__ void few_choose(const FewArgs& a, int t, Score score) {
+// The k best of a sample's K scores, by one wave: weights, and which experts are evaluated.  put(q, expert,
+// weight) by the lane that has choice q; true if all weights are 0.
+template <class Score, class Put>
+__device__ __forceinline__ bool few_choose(const FewArgs& a, int t, Score score, Put put) {
   const int l = threadIdx.x & 63;
   uint64_t best = 0;
   for (int b = 0; b < a.K; b += 64) {
     const int e = b + l;
-    wave_merge(best, e < a.K ? rank_key(score(e) + (a.r_bias ? a.r_bias[e] : 0.f), (uint32_t)e) : 0);
+    wave_merge(best, e < a.K ? rank_key(score(e), (uint32_t)e) : 0);
   }
   const float s = (uint32_t)(best >> 32) == 0 ? NAN : key_value(best);
   const float top = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(s)));
@@ -48,13 +49,19 @@ __device__ __forceinline__ void few_choose(const FewArgs& a, int t, Score score)
   if (sum > 0.f || sum != sum) p /= sum;
   if (p < FLT_MIN) p = 0.f;  // NaN stays
   if (l < a.k) {
-    const int q = t * a.k + l;
-    a.expert[q] = (int32_t)key_index(best);
-    a.weight[q] = p;
-    a.chosen[q] = p == 0.f ? -1 : (int32_t)key_index(best);
+    a.expert[t * a.k + l] = (int32_t)key_index(best);
+    a.weight[t * a.k + l] = p;
+    put(l, (int32_t)key_index(best), p);
   }
-  if (a.counts == 0 && sum == 0.f)  // nobody else writes the row
-    for (int c = l; c < a.o; c += 64) static_cast<T*>(a.Y)[(int64_t)t * a.o + c] = from_f32<T>(0.f);
+  return sum == 0.f;
+}
+
+// For the kernels that follow.
+template <typename T, class Score>
+__device__ __forceinline__ void few_choose_row(const FewArgs& a, int t, Score score) {
+  const bool none = few_choose(a, t, score, [&](int q, int e, float p) { a.chosen[t * a.k + q] = p == 0.f ? -1 : e; });
+  if (a.counts == 0 && none)  // nobody else writes the row
+    for (int c = threadIdx.x & 63; c < a.o; c += 64) static_cast<T*>(a.Y)[(int64_t)t * a.o + c] = from_f32<T>(0.f);
 }
 
 // A workgroup to a sample: the scores of all experts, four at a time to a wave, and the k best.  One CU
@@ -98,7 +105,7 @@ __global__ void __launch_bounds__(64 * kRouteWaves) k_few_route(FewArgs a) {
     }
   }
   __syncthreads();
-  if (w == 0) few_choose<T>(a, t, [&](int e) { return s_score[e]; });
+  if (w == 0) few_choose_row<T>(a, t, [&](int e) { return s_score[e] + (a.r_bias ? a.r_bias[e] : 0.f); });
 }
 
 // Scores of 16 samples against 16 experts; eight waves split the reduction.
@@ -135,7 +142,138 @@ __global__ void __launch_bounds__(64 * kScoreWaves) k_few_score(FewArgs a) {
 template <typename T>
 __global__ void __launch_bounds__(64) k_few_choose(FewArgs a) {
   const int t = blockIdx.x;
-  few_choose<T>(a, t, [&](int e) { return a.score[(int64_t)t * a.K + e]; });
+  few_choose_row<T>(a, t, [&](int e) { return a.score[(int64_t)t * a.K + e] + (a.r_bias ? a.r_bias[e] : 0.f); });
+}
+
+// ------------------------------------------------------------------ all of a small layer
+
+// The sum over groups of `lanes` (a power of two) adjacent lanes, on every one of them.
+__device__ __forceinline__ float lanes_sum(float v, int lanes) {
+  if (lanes > 1) v += dpp<0xB1>(v);   // quad_perm [1,0,3,2]
+  if (lanes > 2) v += dpp<0x4E>(v);   // quad_perm [2,3,0,1]
+  if (lanes > 4) v += dpp<0x141>(v);  // half mirror: quads hold their sums
+  if (lanes > 8) v += dpp<0x140>(v);  // row mirror
+  if (lanes > 16) v += __shfl_xor(v, 16, 64);
+  if (lanes > 32) v += __shfl_xor(v, 32, 64);
+  return v;
+}
+
+// done(row, products, before(row)) with the MI products of each row < rows of W, W + rows kd, ... with the kd
+// values of x (LDS); by all THREADS, 16 bytes of a row to a lane, the loads of two rows and of what
+// before() takes together.  done runs on one lane of a row's, the same one in every call with the same kd.
+template <typename T, int THREADS, int MI, class Before, class Done>
+__device__ __forceinline__ void few_rows_dot(const T* __restrict__ W, int rows, int kd, const float* x, Before before,
+                                             Done done) {
+  constexpr int N = 16 / sizeof(T), R = 2 / MI;
+  const int nv = kd / N;
+  int lanes = 1;
+  while (lanes < nv && lanes < 64) lanes <<= 1;
+  const int sub = threadIdx.x & (lanes - 1), r0 = threadIdx.x / lanes, step = THREADS / lanes;
+  for (int base = 0; base < rows; base += R * step) {
+    float s[R][MI];
+    decltype(before(0)) pre[R];
+    const T* w[R][MI];
+#pragma unroll
+    for (int g = 0; g < R; ++g) {
+      const int r = base + g * step + r0 < rows ? base + g * step + r0 : rows - 1;
+      pre[g] = before(r);
+#pragma unroll
+      for (int i = 0; i < MI; ++i) {
+        w[g][i] = W + ((int64_t)i * rows + r) * kd;
+        s[g][i] = 0.f;
+      }
+    }
+    for (int v = sub; v < nv; v += lanes) {
+      i32x4 wv[R][MI];
+#pragma unroll
+      for (int g = 0; g < R; ++g)
+#pragma unroll
+        for (int i = 0; i < MI; ++i) wv[g][i] = *reinterpret_cast<const i32x4*>(w[g][i] + v * N);
+#pragma unroll
+      for (int q = 0; q < N; q += 4) {
+        const floatx4 xv = *reinterpret_cast<const floatx4*>(x + v * N + q);
+#pragma unroll
+        for (int z = 0; z < 4; ++z)
+#pragma unroll
+          for (int g = 0; g < R; ++g)
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+              s[g][i] = fmaf(to_f32(reinterpret_cast<const T*>(&wv[g][i])[q + z]), xv[z], s[g][i]);
+      }
+    }
+#pragma unroll
+    for (int g = 0; g < R; ++g) {
+      const int r = base + g * step + r0;
+#pragma unroll
+      for (int i = 0; i < MI; ++i) s[g][i] = lanes_sum(s[g][i], lanes);
+      if (sub == 0 && r < rows) done(r, s[g], pre[g]);
+    }
+  }
+}
+
+__device__ __forceinline__ float few_silu(float g, float up) { return g / (1.f + __expf(-g)) * up; }
+__device__ __forceinline__ float few_relu(float v) { return v < 0.f ? 0.f : v; }  // NaN stays
+
+// A workgroup to a sample, routing, experts and combine, h and Y's row in LDS in fp32: nothing goes through
+// HBM between the steps and there is one launch, but a sample's weights come through one CU.  5 samples,
+// fp32, 64 -> 128 -> 64 with one of 8 experts (66 KB a sample): 5.8 us, as the launches of larger layers
+// 12.9; bf16, one of 16 experts, 132 / 200 KB a sample: 8.2 / 10.2 us; 264 KB as those launches: 11.9.
+// (16 waves with two rows' loads each; with four rows' 7.6, 8 waves with two / four 6.4 / 6.5 us.)
+constexpr int kSampleThreads = 1024, kSampleBytes = 224 << 10, kSampleFloats = 12 << 10;
+template <typename T, bool GATED>
+__global__ void __launch_bounds__(kSampleThreads) k_few_sample(FewArgs a) {
+  constexpr int THREADS = kSampleThreads, MI = GATED ? 2 : 1;
+  extern __shared__ floatx4 s_values[];
+  __shared__ int s_expert[HMOE_FEW_EXPERTS];
+  __shared__ float s_weight[HMOE_FEW_EXPERTS];
+  float *s_x = reinterpret_cast<float*>(s_values), *s_hid = s_x + a.d, *s_y = s_hid + a.h, *s_score = s_y + a.o;
+  const int t = blockIdx.x;
+  const T* x = static_cast<const T*>(a.X) + (int64_t)t * a.d;
+  for (int c = threadIdx.x; c < a.d; c += THREADS) s_x[c] = to_f32(x[c]);
+  for (int c = threadIdx.x; c < a.o; c += THREADS) s_y[c] = 0.f;
+  __syncthreads();
+  few_rows_dot<T, THREADS, 1>(
+      static_cast<const T*>(a.R), a.K, a.d, s_x, [&](int e) { return a.r_bias ? a.r_bias[e] : 0.f; },
+      [&](int e, const float(&s)[1], float bias) { s_score[e] = s[0] + bias; });
+  __syncthreads();
+  if (threadIdx.x < 64)
+    few_choose(a, t, [&](int e) { return s_score[e]; }, [&](int q, int e, float p) {
+      s_expert[q] = e;
+      s_weight[q] = p;
+    });
+  __syncthreads();
+  for (int j = 0; j < a.k; ++j) {
+    const float weight = s_weight[j];
+    if (weight == 0.f) continue;
+    const int e = s_expert[j];
+    const T* b1 = static_cast<const T*>(a.b1) + (int64_t)e * MI * a.h;
+    const T* b2 = static_cast<const T*>(a.b2) + (int64_t)e * a.o;
+    few_rows_dot<T, THREADS, MI>(
+        static_cast<const T*>(a.W1) + (int64_t)e * MI * a.h * a.d, a.h, a.d, s_x,
+        [&](int r) {
+          return a.b1 ? float2{to_f32(b1[r]), GATED ? to_f32(b1[a.h + r]) : 0.f} : float2{0.f, 0.f};
+        },
+        [&](int r, const float(&s)[MI], float2 bias) {
+          if constexpr (GATED) s_hid[r] = few_silu(s[0] + bias.x, s[1] + bias.y);
+          else s_hid[r] = few_relu(s[0] + bias.x);
+        });
+    __syncthreads();
+    few_rows_dot<T, THREADS, 1>(
+        static_cast<const T*>(a.W2) + (int64_t)e * a.o * a.h, a.o, a.h, s_hid,
+        [&](int c) { return a.b2 ? to_f32(b2[c]) : 0.f; },
+        [&](int c, const float(&s)[1], float bias) { s_y[c] += weight * (s[0] + bias); });
+    __syncthreads();
+  }
+  T* y = static_cast<T*>(a.Y) + (int64_t)t * a.o;
+  for (int c = threadIdx.x; c < a.o; c += THREADS) y[c] = from_f32<T>(s_y[c]);
+}
+
+// What a sample reads and computes is a workgroup's work.
+bool few_small(const hmoe_few_params_t* p) {
+  const int64_t mi = p->act == HMOE_ACT_SILU_GATED ? 2 : 1, size = p->dt == HMOE_BF16 ? 2 : 4;
+  const int64_t d = p->d_in, h = p->d_hid, o = p->d_out;
+  return d + h + o + p->K <= kSampleFloats &&
+         (p->K * d + p->top_k * (mi * h * d + o * h)) * size <= kSampleBytes;
 }
 
 // ------------------------------------------------------------------ experts
@@ -234,9 +372,9 @@ __global__ void __launch_bounds__(256) k_few_layer(FewArgs a, int tiles, int slo
             float v = acc[0][z] + (a.b1 ? to_f32(b[c0 + z]) : 0.f);
             if constexpr (GATED) {
               const float up = acc[1][z] + (a.b1 ? to_f32(b[a.h + c0 + z]) : 0.f);
-              v = v / (1.f + __expf(-v)) * up;
+              v = few_silu(v, up);
             } else {
-              v = v < 0.f ? 0.f : v;  // NaN stays
+              v = few_relu(v);
             }
             const Halves<T> p(v);
 #pragma unroll
@@ -316,7 +454,13 @@ int few_layer(const FewArgs& a, hipStream_t st) {
 }
 
 template <typename T>
-int moe_few_t(const FewArgs& a, bool gated, hipStream_t st) {
+int moe_few_t(const FewArgs& a, bool gated, bool small, hipStream_t st) {
+  if (small) {
+    const size_t bytes = (size_t)(a.d + a.h + a.o + a.K) * sizeof(float);
+    if (gated) HMOE_LAUNCH("few sample", (k_few_sample<T, true>), dim3(a.n), dim3(kSampleThreads), bytes, st, a);
+    else HMOE_LAUNCH("few sample", (k_few_sample<T, false>), dim3(a.n), dim3(kSampleThreads), bytes, st, a);
+    return HMOE_OK;
+  }
   // a router of up to 128 KB in one launch (64 KB: 4.1 us, 512 KB: 13), larger ones in two
   if (a.K <= kRouteMost && (int64_t)a.K * a.d * sizeof(T) <= (128 << 10)) {
     HMOE_LAUNCH("few route", k_few_route<T>, dim3(a.n), dim3(64 * kRouteWaves), 0, st, a);
@@ -355,8 +499,8 @@ int launch_moe_few(const hmoe_few_params_t* p, int64_t n, const void* X, int32_t
   FewArgs a = {X, p->R, p->W1, p->b1, p->W2, p->b2, p->r_bias, (int)n, p->K, p->d_in, p->d_hid, p->d_out, p->top_k,
                expert, weight, nullptr, nullptr, nullptr, 1, nullptr, nullptr, 0, Y};
   few_carve(p, n, ws, a);
-  const bool gated = p->act == HMOE_ACT_SILU_GATED;
-  return p->dt == HMOE_BF16 ? moe_few_t<bf16>(a, gated, st) : moe_few_t<float>(a, gated, st);
+  const bool gated = p->act == HMOE_ACT_SILU_GATED, small = few_small(p);
+  return p->dt == HMOE_BF16 ? moe_few_t<bf16>(a, gated, small, st) : moe_few_t<float>(a, gated, small, st);
 }
 
 }  // namespace hmoe

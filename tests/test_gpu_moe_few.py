@@ -256,3 +256,23 @@ def test_streams_workspace_and_graphs():
 def test_no_samples():
     p = params(4, 16, 8, 8, "bf16", "relu", False, 1)
     assert hmoe.moe_few(p, torch.empty(0, 16, dtype=torch.bfloat16, device="cuda"))["Y"].shape == (0, 8)
+
+
+@pytest.mark.parametrize("dtype,n,K,d,h,o,k,act,bias", [
+    # a sample's weights just below and above what one workgroup takes (224 KB)
+    ("bf16", 7, 16, 224, 256, 208, 1, "relu", True), ("bf16", 7, 16, 224, 256, 216, 1, "relu", True),
+    ("f32", 6, 3, 72, 104, 328, 3, "silu", False), ("f32", 6, 3, 72, 104, 144, 3, "silu", False),
+    # few experts and rows of one vector, or of many
+    ("bf16", 64, 500, 8, 24, 16, 8, "silu", True), ("f32", 3, 40, 8, 1000, 8, 2, "relu", True),
+    ("bf16", 4, 2, 5000, 8, 2000, 1, "relu", True), ("bf16", 4, 2, 8, 5000, 8, 1, "silu", True)])
+def test_layers_of_one_workgroup_a_sample(dtype, n, K, d, h, o, k, act, bias):
+    p = params(K, d, h, o, dtype, act, bias, K + d)
+    check(p, draw(p, n, k, dtype, n + h), k, act)
+
+
+@pytest.mark.parametrize("K,d,h,o", [(4, 16, 24, 5000 * 8), (4, 32, 520, 264)])
+@pytest.mark.parametrize("k", [1, 2])
+def test_small_routers_before_large_experts(K, d, h, o, k):
+    p = params(K, d, h, o, "bf16", "relu", True, K + d)
+    p["r_bias"][1] = float("-inf")
+    check(p, draw(p, 21, min(k, 2), "bf16", 5), k, "relu")
