@@ -66,7 +66,7 @@ __device__ __forceinline__ void few_choose_row(const FewArgs& a, int t, Score sc
 
 // A workgroup to a sample: the scores of all experts, four at a time to a wave, and the k best.  One CU
 // draws some 40 GB/s from its L2 here, so this is for small routers.
-constexpr int kRouteWaves = 16, kRouteEach = 4, kRouteMost = 512;
+constexpr int kRouteWaves = 16, kRouteEach = 4, kRouteMost = 128;
 template <typename T>
 __global__ void __launch_bounds__(64 * kRouteWaves) k_few_route(FewArgs a) {
   constexpr int N = 16 / sizeof(T), G = kRouteEach;
