@@ -626,8 +626,8 @@ __device__ __forceinline__ int64_t lora_piece_slot(int64_t seg_e, int64_t local,
 
 // Tiles of the gradients: BW columns of D by UW of U, four waves.  The reduction over an adapter's rows is
 // often short, a stage or two, and then a workgroup is all latency: 256 columns rather than 64 (111 us for
-// dB and 74 for dA at 16384 rows of 128 adapters, 4096 and 2048 columns) keep 36 KB of loads in flight in
-// each.  64 where 256 leave CUs idle.
+// dB and 74 for dA at 16384 rows of 128 adapters of rank 16, 4096 and 2048 columns; with 256, and both in one
+// launch, 84) keep 36 KB of loads in flight in each.  64 where 256 leave CUs idle.
 template <typename T, int UW, int BW, bool U_LEFT>
 struct GradTile {
   using type = typename std::conditional<U_LEFT, Cfg<T, UW, BW, UW, BW / 4>, Cfg<T, BW, UW, BW / 4, UW>>::type;
@@ -670,7 +670,10 @@ struct MapStager : Stager<T, ROWS, THREADS, false> {
 };
 
 // acc = U^T D or D^T U over `rows` slots from p0 on (pu is there already), on the register-staged engine.  A
-// stage's rows of D are looked up a stage before its loads go out: s_row holds those of two stages.
+// stage's rows of D are looked up a stage before its loads go out: s_row holds those of two stages.  LDS holds
+// one stage, the next one's loads are in registers: with two stages in LDS there are fewer workgroups
+// to a CU to hide each other's latency (64 values of the rank, 16 adapters, 16384 rows: 214 us, 141 with
+// one; and of rank 16 with three workgroups to a CU rather than two 84 us instead of 103).
 template <class C, int BW, int UW, bool U_LEFT>
 __device__ __forceinline__ void grad_tile(const typename C::type* __restrict__ D, int width, int dv,
                                           const int32_t* __restrict__ map, int64_t p0,
@@ -682,7 +685,7 @@ __device__ __forceinline__ void grad_tile(const typename C::type* __restrict__ D
   Stager<T, UW, C::THREADS, false> su;
   constexpr int D_BYTES = BW * kStageRowBytes, U_BYTES = UW * kStageRowBytes;
   lds<char>* const bd = smem;
-  lds<char>* const bu = smem + 2 * D_BYTES;
+  lds<char>* const bu = smem + D_BYTES;
 #pragma unroll
   for (int i = 0; i < C::MI; ++i)
 #pragma unroll
@@ -696,9 +699,9 @@ __device__ __forceinline__ void grad_tile(const typename C::type* __restrict__ D
     sd.load(D, width, dv, s * C::BK, rows, (const lds<int32_t>*)s_row[s & 1]);
     su.load(pu, ldu, uv, s * C::BK, rows);
   };
-  const auto store = [&](int s) {
-    sd.store(bd + (s & 1) * D_BYTES);
-    su.store(bu + (s & 1) * U_BYTES);
+  const auto store = [&] {
+    sd.store(bd);
+    su.store(bu);
   };
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
@@ -707,15 +710,15 @@ __device__ __forceinline__ void grad_tile(const typename C::type* __restrict__ D
   }
   __syncthreads();
   load(0);
-  store(0);
+  store();
   __syncthreads();
   for (int kt = 0; kt < nk; ++kt) {
     if (kt + 1 < nk) load(kt + 1);
     const int32_t r = look_up(kt + 2);
-    const lds<char>*d = bd + (kt & 1) * D_BYTES, *u = bu + (kt & 1) * U_BYTES;
-    if constexpr (U_LEFT) mfma_stage<C>(u, d, acc);
-    else mfma_stage<C>(d, u, acc);
-    if (kt + 1 < nk) store(kt + 1);
+    if constexpr (U_LEFT) mfma_stage<C>((const lds<char>*)bu, (const lds<char>*)bd, acc);
+    else mfma_stage<C>((const lds<char>*)bd, (const lds<char>*)bu, acc);
+    __syncthreads();
+    if (kt + 1 < nk) store();
     if (t < C::BK) s_row[kt & 1][t] = r;  // stage kt's rows: last read before the last barrier
     __syncthreads();
   }
@@ -731,10 +734,10 @@ struct GradSide {
 };
 
 // For one piece of adapter e's rows:  U_LEFT: out[c][m] = sum_rows U[c] D[m] (dA: [rank][width]),
-// otherwise out[m][c] = sum_rows D[m] U[c] (dB: [width][rank]), m from d0 on.
+// otherwise out[m][c] = sum_rows D[m] U[c] (dB: [width][rank]), m from d0 and U's columns from u0 on.
 template <typename T, int UW, int BW, bool U_LEFT>
-__device__ __forceinline__ void lora_grad_side(const GradSide& g, int d0, int rank, const int32_t* __restrict__ seg, int E,
-                                               int piece) {
+__device__ __forceinline__ void lora_grad_side(const GradSide& g, int d0, int u0, int rank,
+                                               const int32_t* __restrict__ seg, int E, int piece) {
   using C = typename GradTile<T, UW, BW, U_LEFT>::type;
   static_assert(C::THREADS == 256, "four waves");
   extern __shared__ __attribute__((aligned(16))) char smem_raw[];
@@ -746,7 +749,7 @@ __device__ __forceinline__ void lora_grad_side(const GradSide& g, int d0, int ra
   const int64_t len = seg[e + 1] - p0;
   const int rows = (int)(len < piece ? len : piece);
   const int ldu = u_width<T>(rank);
-  const int u0 = blockIdx.z * UW, width = g.width;
+  const int width = g.width;
   const T *D = static_cast<const T*>(g.D), *U = static_cast<const T*>(g.U);
   const int dv = width - d0 < BW ? width - d0 : BW, uv = ldu - u0 < UW ? ldu - u0 : UW;
   floatx4 acc[C::MI][C::NJ];
@@ -779,13 +782,17 @@ __device__ __forceinline__ void lora_grad_side(const GradSide& g, int d0, int ra
 }
 
 // Both gradients: blockIdx.y runs over dB's tiles and then dA's.  (One launch each: 24 us for 777 rows of the tiny
-// decoder, 13 together; 112 and 103 for 16384 rows of 128 adapters of rank 16, 2048 -> 4096.)
+// decoder, 13 together.)  The chunks of the rank that read the same part of D come one after the other on
+// the same XCD, gridDim.x being a multiple of 8 (rank 128, 16 adapters of 16384 rows: 270 us, 254 so).
+template <typename T>
+constexpr int kNarrow = sizeof(T) == 2 ? 48 : 32;  // of U: rank 16, 32
 template <typename T, int UW, int BW>
-__global__ void __launch_bounds__(256) k_lora_grad(GradSide b, GradSide a, int rank, const int32_t* __restrict__ seg, int E,
-                                                   int piece) {
-  const int tiles_b = (b.width + BW - 1) / BW, y = blockIdx.y;
-  if (y < tiles_b) lora_grad_side<T, UW, BW, false>(b, y * BW, rank, seg, E, piece);
-  else lora_grad_side<T, UW, BW, true>(a, (y - tiles_b) * BW, rank, seg, E, piece);
+__global__ void __launch_bounds__(256, UW == kNarrow<T> ? 3 : 2)
+    k_lora_grad(GradSide b, GradSide a, int rank, const int32_t* __restrict__ seg, int E, int piece) {
+  const int tiles_b = (b.width + BW - 1) / BW, chunks = (u_width<T>(rank) + UW - 1) / UW;
+  const int y = blockIdx.y / chunks, u0 = blockIdx.y % chunks * UW;
+  if (y < tiles_b) lora_grad_side<T, UW, BW, false>(b, y * BW, u0, rank, seg, E, piece);
+  else lora_grad_side<T, UW, BW, true>(a, (y - tiles_b) * BW, u0, rank, seg, E, piece);
 }
 
 // The pieces of an adapter added in their order; adapters without rows get zeros.  Both gradients in one launch:
@@ -871,14 +878,14 @@ int lora_grad_tiles(const GradSide& b, const GradSide& a, int rank, const int32_
   static_assert(C::LDS == GradTile<T, UW, BW, true>::type::LDS, "one launch for both");
   const int piece = lora_piece(n);
   HMOE_LAUNCH("lora gradients", (k_lora_grad<T, UW, BW>),
-              dim3((unsigned)(n / piece + (E < n ? E : n)), (unsigned)(cdiv(b.width, BW) + cdiv(a.width, BW)),
-                   (unsigned)cdiv(u_width<T>(rank), UW)),
-              dim3(256), C::LDS, st, b, a, rank, seg, E, piece);
+              dim3((unsigned)(cdiv(n / piece + (E < n ? E : n), 8) * 8),
+                   (unsigned)((cdiv(b.width, BW) + cdiv(a.width, BW)) * cdiv(u_width<T>(rank), UW))),
+              dim3(256), C::LDS / 2, st, b, a, rank, seg, E, piece);
   return HMOE_OK;
 }
 template <typename T>
 int lora_grad(const GradSide& b, const GradSide& a, int rank, const int32_t* seg, int E, int64_t n, hipStream_t st) {
-  constexpr int NARROW = sizeof(T) == 2 ? 48 : 32;  // rank 16, 32
+  constexpr int NARROW = kNarrow<T>;
   const int64_t pieces = n / lora_piece(n) + (E < n ? E : n);
   if (pieces * (cdiv(b.width, 256) + cdiv(a.width, 256)) < device_cus())
     HMOE_TRY((lora_grad_tiles<T, NARROW, 64>(b, a, rank, seg, E, n, st)));
