@@ -165,13 +165,13 @@ __global__ void __launch_bounds__(64 * kFewShrinkWaves) k_lora_few_shrink(LoraFe
 // 16 MI columns of Y for all rows (16 NT at most); the waves split d, and the adapters of the rows.
 // RB > 0: one row, whose 16 RB values of U the workgroup forms itself, the rows of A going past x with its rows
 // of W: for a narrow A the reads of it (from L2) take less than the launch that U otherwise comes from.
-template <typename T, int MI, int NT, int RB>
-__global__ void __launch_bounds__(256) k_lora_few(LoraFew a) {
+template <typename T, int MI, int NT, int RB, int NW>
+__global__ void __launch_bounds__(64 * NW) k_lora_few(LoraFew a) {
   static_assert(RB == 0 || (MI == 1 && NT == 1), "one row");
   constexpr int UROW = HMOE_LORA_RANK * 4 + 16;  // bytes of a row of U at most, and a bank shift
-  constexpr int ACC = 4 * MI * NT * 64 * 16, ULDS = 16 * NT * UROW;
+  constexpr int ACC = NW * MI * NT * 64 * 16, ULDS = 16 * NT * UROW;
   __shared__ __attribute__((aligned(16))) char s_mem[ACC > ULDS ? ACC : ULDS];
-  __shared__ floatx4 s_a[RB > 0 ? 4 : 1][RB > 0 ? RB : 1][64];
+  __shared__ floatx4 s_a[RB > 0 ? NW : 1][RB > 0 ? RB : 1][64];
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6, lr = l & 15, lg = l >> 4;
   const int c0 = blockIdx.x * 16 * MI;
   const int ldu = u_width<T, 2>(a.rank), blocks = u_blocks(a.rank), urow = ldu * (int)sizeof(T) + 16;
@@ -179,7 +179,7 @@ __global__ void __launch_bounds__(256) k_lora_few(LoraFew a) {
   lds<char>* s_u = (lds<char>*)s_mem;
   if constexpr (RB == 0) {  // U, 16-byte pieces
     const int per = ldu * (int)sizeof(T) / 16;
-    for (int q = threadIdx.x; q < per * a.n; q += 256) {
+    for (int q = threadIdx.x; q < per * a.n; q += 64 * NW) {
       const int r = q / per, v = q - r * per;
       *reinterpret_cast<lds<i32x4>*>(s_u + r * urow + 16 * v) =
           *reinterpret_cast<const i32x4*>(static_cast<const char*>(a.U) + (int64_t)r * ldu * sizeof(T) + 16 * v);
@@ -227,7 +227,7 @@ __global__ void __launch_bounds__(256) k_lora_few(LoraFew a) {
     for (int t = 0; t < NT; ++t) acc[i][t] = floatx4{0.f, 0.f, 0.f, 0.f};
   const int groups = groups_of<T>(a.d);
   stream_groups<T, (RB > 0 ? 2 : (MI * NT > 1 ? 1 : 4))>(
-      W, wo, static_cast<const T*>(a.X), xo, a.d, groups * w / 4, groups * (w + 1) / 4,
+      W, wo, static_cast<const T*>(a.X), xo, a.d, groups * w / NW, groups * (w + 1) / NW,
       [&](const i32x4(&wv)[MI + RB], const i32x4(&xv)[NT]) {
 #pragma unroll
         for (int i = 0; i < MI + RB; ++i)
@@ -240,7 +240,9 @@ __global__ void __launch_bounds__(256) k_lora_few(LoraFew a) {
     __syncthreads();
     if (w < RB && lr == 0) {
       const int e = all >= 0 && all < a.E ? all : 0;
-      floatx4 u = (s_a[0][w][l] + s_a[1][w][l]) + (s_a[2][w][l] + s_a[3][w][l]);
+      floatx4 u = s_a[0][w][l];
+#pragma unroll
+      for (int q = 1; q < NW; ++q) u += s_a[q][w][l];
       u_store<T, 2>((T*)s_mem, 0, ldu, w, lg, a.rank, u * (a.scale ? a.scale[e] : 1.f));
     }
   }
@@ -252,7 +254,7 @@ __global__ void __launch_bounds__(256) k_lora_few(LoraFew a) {
     const int e = __builtin_amdgcn_readlane(all, __builtin_ctzll(left));
     const uint64_t with = __ballot(all == e) & left;
     left &= ~with;
-    if (turn % 4 != w) continue;
+    if (turn % NW != w) continue;
     const T* B[MI];
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
@@ -301,9 +303,11 @@ __global__ void __launch_bounds__(256) k_lora_few(LoraFew a) {
 #pragma unroll
     for (int t = 0; t < NT; ++t) s_acc[w][i][t][l] = acc[i][t];
   __syncthreads();
-  for (int q = w; q < MI * NT; q += 4) {
+  for (int q = w; q < MI * NT; q += NW) {
     const int i = q / NT, t = q % NT, c = c0 + 16 * i + 4 * lg;
-    floatx4 v = (s_acc[0][i][t][l] + s_acc[1][i][t][l]) + (s_acc[2][i][t][l] + s_acc[3][i][t][l]);
+    floatx4 v = s_acc[0][i][t][l];
+#pragma unroll
+    for (int p = 1; p < NW; ++p) v += s_acc[p][i][t][l];
     if (16 * t + lr >= a.n || c >= a.o) continue;
     quad<T> y;
 #pragma unroll
@@ -312,14 +316,14 @@ __global__ void __launch_bounds__(256) k_lora_few(LoraFew a) {
   }
 }
 
-template <typename T, int MI>
+template <typename T, int MI, int NW>
 int lora_few_mi(const LoraFew& a, hipStream_t st) {
-  const dim3 grid((unsigned)cdiv(a.o, 16 * MI)), block(256);
+  const dim3 grid((unsigned)cdiv(a.o, 16 * MI)), block(64 * NW);
   switch ((a.n + 15) / 16) {
-    case 1: HMOE_LAUNCH("lora few", (k_lora_few<T, MI, 1, 0>), grid, block, 0, st, a); break;
-    case 2: HMOE_LAUNCH("lora few", (k_lora_few<T, MI, 2, 0>), grid, block, 0, st, a); break;
-    case 3: HMOE_LAUNCH("lora few", (k_lora_few<T, MI, 3, 0>), grid, block, 0, st, a); break;
-    default: HMOE_LAUNCH("lora few", (k_lora_few<T, MI, 4, 0>), grid, block, 0, st, a); break;
+    case 1: HMOE_LAUNCH("lora few", (k_lora_few<T, MI, 1, 0, 4>), grid, dim3(256), 0, st, a); break;
+    case 2: HMOE_LAUNCH("lora few", (k_lora_few<T, MI, 2, 0, NW>), grid, block, 0, st, a); break;
+    case 3: HMOE_LAUNCH("lora few", (k_lora_few<T, MI, 3, 0, NW>), grid, block, 0, st, a); break;
+    default: HMOE_LAUNCH("lora few", (k_lora_few<T, MI, 4, 0, NW>), grid, block, 0, st, a); break;
   }
   return HMOE_OK;
 }
@@ -327,19 +331,27 @@ int lora_few_mi(const LoraFew& a, hipStream_t st) {
 template <typename T>
 int lora_few_t(const LoraFew& a, hipStream_t st) {
   const int slots = a.n < a.E ? a.n : a.E, blocks = u_blocks(a.rank);
+  // Eight waves to a workgroup rather than four where there is one on each CU at most, for more than 16 rows
+  // (bf16, 2048 -> 4096, 16 adapters: 48 rows 17.4 -> 15.2 us, 64 rows of rank 128 31 -> 24; 4 rows 10.2 ->
+  // 10.6; 64 rows, 8192 columns 24 -> 27), and for one row whose reduction gives each two groups (2048 -> 4096
+  // 6.7 -> 6.1 us, 1024 -> 1024 4.5 -> 4.7).
+  const bool narrow = cdiv(a.o, 16) <= device_cus();
   // One row: in one launch where reading A for every 16 columns (up to 20 MB from L2 per 16 of the rank,
   // 4 us) takes less than a second one.
   if (a.n == 1 && blocks <= 2 && (int64_t)a.o * a.d * sizeof(T) * blocks <= (20 << 20)) {
-    const dim3 grid((unsigned)cdiv(a.o, 16)), block(256);
-    if (blocks == 1) HMOE_LAUNCH("lora few", (k_lora_few<T, 1, 1, 1>), grid, block, 0, st, a);
-    else HMOE_LAUNCH("lora few", (k_lora_few<T, 1, 1, 2>), grid, block, 0, st, a);
+    const dim3 grid((unsigned)cdiv(a.o, 16));
+    const bool eight = narrow && groups_of<T>(a.d) >= 16;
+    if (blocks == 1 && eight) HMOE_LAUNCH("lora few", (k_lora_few<T, 1, 1, 1, 8>), grid, dim3(512), 0, st, a);
+    else if (blocks == 1) HMOE_LAUNCH("lora few", (k_lora_few<T, 1, 1, 1, 4>), grid, dim3(256), 0, st, a);
+    else if (eight) HMOE_LAUNCH("lora few", (k_lora_few<T, 1, 1, 2, 8>), grid, dim3(512), 0, st, a);
+    else HMOE_LAUNCH("lora few", (k_lora_few<T, 1, 1, 2, 4>), grid, dim3(256), 0, st, a);
     return HMOE_OK;
   }
-  HMOE_LAUNCH("lora few shrink", k_lora_few_shrink<T>, dim3((unsigned)(slots * blocks)), dim3(64 * kFewShrinkWaves), 0, st,
-              a);
+  HMOE_LAUNCH("lora few shrink", k_lora_few_shrink<T>, dim3((unsigned)(slots * blocks)), dim3(64 * kFewShrinkWaves), 0,
+              st, a);
   // wide outputs: two blocks of columns to a workgroup, which halves the reads of X
-  if (a.o >= 16 * 1024) return lora_few_mi<T, 2>(a, st);
-  return lora_few_mi<T, 1>(a, st);
+  if (a.o >= 16 * 1024) return lora_few_mi<T, 2, 4>(a, st);
+  return narrow && a.n > 16 ? lora_few_mi<T, 1, 8>(a, st) : lora_few_mi<T, 1, 4>(a, st);
 }
 
 // ------------------------------------------------------------------ rows in adapter order

@@ -165,6 +165,31 @@ def test_tilings(dtype, n, E, d, o, r):
         close(got[k], ref[k], k)
 
 
+@pytest.mark.parametrize("dtype,n,E,d,o,r", [
+    # a workgroup of eight waves or of four to 16 columns, few and many of them, groups short of the waves
+    ("bf16", 1, 3, 2040, 4096, 16), ("bf16", 1, 3, 2048, 4104, 16), ("f32", 1, 3, 1032, 72, 24), ("bf16", 1, 3, 4104, 88, 32),
+    ("bf16", 24, 30, 72, 4096, 24), ("bf16", 40, 7, 264, 6008, 16), ("f32", 64, 20, 136, 4104, 40),
+    ("bf16", 64, 20, 1032, 1000, 128)])
+def test_waves_of_a_workgroup(dtype, n, E, d, o, r):
+    p = adapters(E, d, o, r, dtype, True, n + o, scale=True)
+    X, ids = rows(n, d, dtype, n), ids_of(n, E, o)
+    if n == 1:
+        ids[0] = 1
+    close(hmoe.lora_few(p, X, torch.tensor(ids).cuda()), plain(p, X, ids)["Y"], "Y")
+
+
+@pytest.mark.parametrize("dtype,n,E,d,o,r", [
+    # gradients: ranks that take one chunk of U or several, tiles of 64 and of 256 columns, long adapters
+    ("bf16", 1200, 70, 520, 1032, 16), ("bf16", 1200, 70, 520, 1032, 104), ("f32", 1200, 70, 520, 264, 32),
+    ("f32", 900, 70, 264, 1032, 72), ("bf16", 6000, 2, 136, 264, 88)])
+def test_chunks_of_the_rank(dtype, n, E, d, o, r):
+    p = adapters(E, d, o, r, dtype, False, n + o)
+    X, dY, ids = rows(n, d, dtype, n), rows(n, o, dtype, n + 1), ids_of(n, E, n)
+    got, ref = grouped(p, X, ids, dY), plain(p, X, ids, dY)
+    for k in ("dA", "dB"):
+        close(got[k], ref[k], k)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_rows_without_adapters_and_adapters_without_rows(dtype):
     n, E, d, o, r = 600, 6, 72, 88, 16
