@@ -840,23 +840,24 @@ int lora_shrink(const T* X, int K, const T* A, int rank, const float* scale, con
   return HMOE_OK;
 }
 
-// Tiles for the type (gemm.hpp), quarter tiles where there are fewer of them than CUs.
+// Tiles for the type (gemm.hpp), quarter tiles where there are fewer of them than half of the CUs (bf16, rows of
+// 1024 into 1024: 4096 rows, 64 tiles, 37 us with whole tiles and 25 with quarter tiles; 8192 rows 36 and 43).
 template <typename T, bool W_KC>
 using LoraTile = typename std::conditional<W_KC, typename Pick<T>::C, typename Pick<T>::CK>::type;
 template <typename T, bool W_KC>
 bool lora_small(int64_t n, int cols) {
   using C = LoraTile<T, W_KC>;
-  return cdiv(n, C::BM) * cdiv(cols, C::BN) < device_cus();
+  return cdiv(n, C::BM) * cdiv(cols, C::BN) * 2 < device_cus();
 }
-// Splits of the reduction: for fewer quarter tiles than CUs, of two stages at least (777 x 64 fp32 outputs of 1000
-// products, 13 tiles: 36 us, 10 in eight splits with the launch that joins them).
+// Splits of the reduction, of three stages at least, up to four workgroups to a CU, where that makes three or
+// more of them worth the launch that joins them (4 us): 777 x 64 fp32 outputs of 1000 products, 13 tiles: 36 us,
+// 10 in eight splits; 4814 x 200 bf16 of 3528, 304 tiles: 60 us, 31 in three.
 template <typename T>
 int lora_gemm_splits(int64_t n, int cols, int Kd) {
   using Q = CfgQuarter<T>;
   const int64_t tiles = cdiv(n, Q::BM) * cdiv(cols, Q::BN);
-  if (tiles >= device_cus()) return 1;
-  const int64_t fill = device_cus() / tiles, stages = Kd / (2 * Q::BK), s = fill < stages ? fill : stages;
-  return s < 4 ? 1 : (s > 8 ? 8 : (int)s);
+  const int64_t fill = 4 * device_cus() / tiles, stages = Kd / (3 * Q::BK), s = fill < stages ? fill : stages;
+  return s < 3 ? 1 : (s > 8 ? 8 : (int)s);
 }
 template <typename T>
 size_t lora_gemm_part(int64_t n, int cols, int Kd) {

@@ -190,6 +190,17 @@ def test_chunks_of_the_rank(dtype, n, E, d, o, r):
         close(got[k], ref[k], k)
 
 
+@pytest.mark.parametrize("dtype,n,E,d,o,r", [
+    ("bf16", 8000, 5, 1032, 136, 16),  # whole tiles on half of the chip, gathering
+    ("bf16", 4700, 3, 200, 616, 8), ("f32", 4700, 3, 200, 616, 8)])  # reductions in three splits
+def test_half_filled_tilings(dtype, n, E, d, o, r):
+    p = adapters(E, d, o, r, dtype, True, n + o)
+    X, dY, ids = rows(n, d, dtype, n), rows(n, o, dtype, n + 1), ids_of(n, E, n)
+    got, ref = grouped(p, X, ids, dY), plain(p, X, ids, dY)
+    for k in ("Y", "dX", "dA", "dB"):
+        close(got[k], ref[k], k)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_rows_without_adapters_and_adapters_without_rows(dtype):
     n, E, d, o, r = 600, 6, 72, 88, 16
