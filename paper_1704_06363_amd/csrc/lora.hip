@@ -625,8 +625,12 @@ __global__ void __launch_bounds__(256) k_lora_transpose(const T* __restrict__ B,
 // Rows of one adapter that a workgroup sums over; adapters with more have several pieces, joined
 // in order by k_lora_grad_join.  A 64th of all rows, so that no workgroup has much more than the others (with
 // 1024 for 16384 rows the few long ones took 69 us for dB and 57 for dA) and 130 pieces at most are kept.
-inline int lora_piece(int64_t n) {
+// Smaller ones, of 64 at least, where they leave CUs idle (a step on 777 rows of 8 adapters of 64 and 1000 columns:
+// 54 us with 256 rows, 49 with 64).
+inline int lora_piece(int64_t n, int E, int d_in, int d_out) {
+  const int64_t tiles = cdiv(d_in, 64) + cdiv(d_out, 64);
   int rows = 256;
+  while (rows > 64 && (n / rows + (E < n ? E : n)) * tiles < 2 * device_cus()) rows /= 2;
   while (rows < (1 << 20) && (int64_t)rows * 64 < n) rows *= 2;
   return rows;
 }
@@ -886,10 +890,10 @@ int lora_gemm(const T* A, const T* W, const T* bias, const T* U, const T* B, int
 }
 
 template <typename T, int UW, int BW>
-int lora_grad_tiles(const GradSide& b, const GradSide& a, int rank, const int32_t* seg, int E, int64_t n, hipStream_t st) {
+int lora_grad_tiles(const GradSide& b, const GradSide& a, int rank, const int32_t* seg, int E, int64_t n, int piece,
+                    hipStream_t st) {
   using C = typename GradTile<T, UW, BW, false>::type;
   static_assert(C::LDS == GradTile<T, UW, BW, true>::type::LDS, "one launch for both");
-  const int piece = lora_piece(n);
   HMOE_LAUNCH("lora gradients", (k_lora_grad<T, UW, BW>),
               dim3((unsigned)(cdiv(n / piece + (E < n ? E : n), 8) * 8),
                    (unsigned)((cdiv(b.width, BW) + cdiv(a.width, BW)) * cdiv(u_width<T>(rank), UW))),
@@ -897,18 +901,19 @@ int lora_grad_tiles(const GradSide& b, const GradSide& a, int rank, const int32_
   return HMOE_OK;
 }
 template <typename T>
-int lora_grad(const GradSide& b, const GradSide& a, int rank, const int32_t* seg, int E, int64_t n, hipStream_t st) {
+int lora_grad(const GradSide& b, const GradSide& a, int rank, const int32_t* seg, int E, int64_t n, int piece,
+                    hipStream_t st) {
   constexpr int NARROW = kNarrow<T>;
-  const int64_t pieces = n / lora_piece(n) + (E < n ? E : n);
+  const int64_t pieces = n / piece + (E < n ? E : n);
   if (pieces * (cdiv(b.width, 256) + cdiv(a.width, 256)) < device_cus())
-    HMOE_TRY((lora_grad_tiles<T, NARROW, 64>(b, a, rank, seg, E, n, st)));
+    HMOE_TRY((lora_grad_tiles<T, NARROW, 64>(b, a, rank, seg, E, n, piece, st)));
   else if (u_width<T>(rank) <= NARROW)
-    HMOE_TRY((lora_grad_tiles<T, NARROW, 256>(b, a, rank, seg, E, n, st)));
+    HMOE_TRY((lora_grad_tiles<T, NARROW, 256>(b, a, rank, seg, E, n, piece, st)));
   else
-    HMOE_TRY((lora_grad_tiles<T, 2 * NARROW, 256>(b, a, rank, seg, E, n, st)));
+    HMOE_TRY((lora_grad_tiles<T, 2 * NARROW, 256>(b, a, rank, seg, E, n, piece, st)));
   HMOE_LAUNCH("lora gradient join", k_lora_grad_join,
               dim3((unsigned)(cdiv((int64_t)b.width * rank, 1024) + cdiv((int64_t)a.width * rank, 1024)), (unsigned)E),
-              dim3(256), 0, st, b, a, rank, seg, lora_piece(n));
+              dim3(256), 0, st, b, a, rank, seg, piece);
   return HMOE_OK;
 }
 
@@ -924,7 +929,7 @@ LoraSpace lora_carve(const hmoe_lora_t* p, int64_t n, Workspace& ws) {
   x.Bt = ws.take<char>((size_t)p->E * p->rank * p->d_out * s);
   x.At = ws.take<char>((size_t)p->E * p->rank * p->d_in * s);
   x.V = ws.take<char>((size_t)n * ldu * s);
-  const int64_t piece = lora_piece(n);
+  const int64_t piece = lora_piece(n, p->E, p->d_in, p->d_out);
   const size_t pieces = n > piece ? 2 * (n / piece) + 2 : 0;
   x.part_a = ws.take<float>(pieces * p->d_in * p->rank);
   x.part_b = ws.take<float>(pieces * p->d_out * p->rank);
@@ -972,7 +977,7 @@ int lora_backward_t(const hmoe_lora_t* p, int64_t n, const T* X, const int32_t* 
   }
   if (dA || dB) {
     const GradSide b = {dY, map, U, dB ? p->d_out : 0, dB, w.part_b}, a = {X, nullptr, w.V, dA ? p->d_in : 0, dA, w.part_a};
-    return lora_grad<T>(b, a, p->rank, offsets, p->E, n, st);
+    return lora_grad<T>(b, a, p->rank, offsets, p->E, n, lora_piece(n, p->E, p->d_in, p->d_out), st);
   }
   return HMOE_OK;
 }
