@@ -162,11 +162,15 @@ __global__ void __launch_bounds__(64 * kFewShrinkWaves) k_lora_few_shrink(LoraFe
   }
 }
 
+// Waves to a SIMD that the registers are kept to for wide outputs: what fits without spilling.  (48 rows, 50000
+// columns of 1024, 16 adapters of rank 32: 50 us, with two waves to a SIMD 61, with four and 16 spilled registers, a load of B at a time, 59.)
+constexpr int few_waves(int mi, int nt) { return mi == 1 ? 1 : (nt == 4 ? 2 : (nt == 3 ? 3 : 4)); }
+
 // 16 MI columns of Y for all rows (16 NT at most); the waves split d, and the adapters of the rows.
 // RB > 0: one row, whose 16 RB values of U the workgroup forms itself, the rows of A going past x with its rows
 // of W: for a narrow A the reads of it (from L2) take less than the launch that U otherwise comes from.
 template <typename T, int MI, int NT, int RB, int NW>
-__global__ void __launch_bounds__(64 * NW) k_lora_few(LoraFew a) {
+__global__ void __launch_bounds__(64 * NW, few_waves(MI, NT)) k_lora_few(LoraFew a) {
   static_assert(RB == 0 || (MI == 1 && NT == 1), "one row");
   constexpr int UROW = HMOE_LORA_RANK * 4 + 16;  // bytes of a row of U at most, and a bank shift
   constexpr int ACC = NW * MI * NT * 64 * 16, ULDS = 16 * NT * UROW;
@@ -249,52 +253,80 @@ __global__ void __launch_bounds__(64 * NW) k_lora_few(LoraFew a) {
   __syncthreads();
   // The adapters in the order of their first rows, one to a wave in turn, with sums of their own, which only
   // their rows take: another row's zeros times an infinite B would not be zeros.
-  uint64_t left = __ballot(l < a.n && all >= 0 && all < a.E);
-  for (int turn = 0; left != 0; ++turn) {
-    const int e = __builtin_amdgcn_readlane(all, __builtin_ctzll(left));
-    const uint64_t with = __ballot(all == e) & left;
-    left &= ~with;
-    if (turn % NW != w) continue;
-    const T* B[MI];
+  // Four loads of B go out together, of one adapter or of several (one at a time: 53 us for the 50).
+  constexpr int PER = rank_steps<T>(), BATCH = 4;
+  const int loads = (blocks + PER - 1) / PER;
+  uint64_t left = __ballot(l < a.n && all >= 0 && all < a.E), with = 0;
+  int turn = 0, e = -1, j = loads;  // what is loaded next: load j of adapter e
+  floatx4 own[MI][NT];
+  while (true) {
+    i32x4 raw[BATCH][MI];
+    int be[BATCH], bj[BATCH];
+    uint64_t bw[BATCH];
 #pragma unroll
-    for (int i = 0; i < MI; ++i) {
-      const int c = col[i] + (l >> 2);
-      B[i] = static_cast<const T*>(a.B) + ((int64_t)e * a.o + (c < a.o ? c : a.o - 1)) * a.rank;
+    for (int q = 0; q < BATCH; ++q) {
+      if (j == loads) {
+        j = 0;
+        e = -1;
+        while (left != 0 && e < 0) {
+          const int c = __builtin_amdgcn_readlane(all, __builtin_ctzll(left));
+          const uint64_t m = __ballot(all == c) & left;
+          left &= ~m;
+          if (turn++ % NW != uniform_int(w)) continue;
+          e = c;
+          with = m;
+        }
+      }
+      be[q] = e;
+      bj[q] = j;
+      bw[q] = with;
+      if (e < 0) {  // no more
+        j = loads;
+        continue;
+      }
+#pragma unroll
+      for (int i = 0; i < MI; ++i) {
+        const int c = col[i] + (l >> 2);
+        raw[q][i] = rank_load(static_cast<const T*>(a.B) + ((int64_t)e * a.o + (c < a.o ? c : a.o - 1)) * a.rank, j, a.rank);
+      }
+      ++j;
     }
-    floatx4 own[MI][NT];
+    if (be[0] < 0) break;
 #pragma unroll
-    for (int i = 0; i < MI; ++i)
+    for (int q = 0; q < BATCH; ++q) {
+      if (be[q] < 0) break;
+      if (bj[q] == 0) {
 #pragma unroll
-      for (int t = 0; t < NT; ++t) own[i][t] = floatx4{0.f, 0.f, 0.f, 0.f};
-    constexpr int PER = rank_steps<T>();
-    for (int j = 0; j * PER < blocks; ++j) {
-      i32x4 raw[MI];
+        for (int i = 0; i < MI; ++i)
 #pragma unroll
-      for (int i = 0; i < MI; ++i) raw[i] = rank_load(B[i], j, a.rank);
+          for (int t = 0; t < NT; ++t) own[i][t] = floatx4{0.f, 0.f, 0.f, 0.f};
+      }
 #pragma unroll
       for (int p = 0; p < PER; ++p) {
-        const int kb = j * PER + p;
+        const int kb = bj[q] * PER + p;
         if (kb >= blocks) break;
         i32x4 bv[MI];
 #pragma unroll
-        for (int i = 0; i < MI; ++i) bv[i] = rank_pick<T>(raw[i], kb, lr, lg, a.rank);
-        const int at = (sizeof(T) == 2 ? 64 * kb : 64 * kb) + 16 * lg;  // bytes of the row of U
+        for (int i = 0; i < MI; ++i) bv[i] = rank_pick<T>(raw[q][i], kb, lr, lg, a.rank);
+        const int at = 64 * kb + 16 * lg;  // bytes of the row of U
         const bool in = at < ldu * (int)sizeof(T);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-          if (((with >> (16 * t)) & 0xffff) == 0) continue;
+          if (((bw[q] >> (16 * t)) & 0xffff) == 0) continue;
           i32x4 uv = *reinterpret_cast<const lds<i32x4>*>(s_u + row[t] * urow + (in ? at : 0));
-          uv = in && mine[t] == e ? uv : i32x4{0, 0, 0, 0};
+          uv = in && mine[t] == be[q] ? uv : i32x4{0, 0, 0, 0};
 #pragma unroll
           for (int i = 0; i < MI; ++i) step_mfma<T>(bv[i], uv, own[i][t]);
         }
       }
+      if (bj[q] == loads - 1) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+            if (mine[t] == be[q]) acc[i][t] += own[i][t];
+      }
     }
-#pragma unroll
-    for (int i = 0; i < MI; ++i)
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-        if (mine[t] == e) acc[i][t] += own[i][t];
   }
   __syncthreads();
   floatx4(*s_acc)[MI][NT][64] = reinterpret_cast<floatx4(*)[MI][NT][64]>(s_mem);
