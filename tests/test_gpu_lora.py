@@ -128,6 +128,30 @@ def test_few_rows(dtype, n, E, d, o, r, bias):
     close(Y, plain(p, X, ids)["Y"], "Y")
 
 
+@pytest.mark.parametrize("dtype,n,E,d,o,r", [
+    # a wave's adapters take more loads than go out together, or fewer; wide outputs and narrow ones
+    ("bf16", 64, 64, 64, 16392, 128), ("bf16", 64, 80, 72, 16400, 40), ("bf16", 33, 64, 136, 72, 104),
+    ("bf16", 48, 16, 72, 16392, 72), ("bf16", 19, 30, 64, 16384, 8), ("f32", 50, 64, 72, 40, 72),
+    ("f32", 64, 100, 64, 16392, 24), ("f32", 17, 2, 64, 136, 48)])
+def test_loads_of_several_adapters(dtype, n, E, d, o, r):
+    p = adapters(E, d, o, r, dtype, True, n + r, scale=True)
+    X, ids = rows(n, d, dtype, n), np.random.default_rng(r).permutation(max(n, E))[:n].astype(np.int32) % E
+    ids[1] = -1
+    close(hmoe.lora_few(p, X, torch.tensor(ids).cuda()), plain(p, X, ids)["Y"], "Y")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,E", [(63, 1), (64, 1), (65, 1), (129, 2), (257, 1), (700, 3)])
+def test_pieces_of_small_problems(dtype, n, E):
+    """Adapters whose rows end at, before and past a piece of the smallest size."""
+    d, o, r = 72, 88, 16
+    p = adapters(E, d, o, r, dtype, False, n)
+    X, dY, ids = rows(n, d, dtype, n), rows(n, o, dtype, n + 1), np.sort(np.arange(n) % (E + 1) % E).astype(np.int32)
+    got, ref = grouped(p, X, ids, dY), plain(p, X, ids, dY)
+    for k in ("dA", "dB"):
+        close(got[k], ref[k], k)
+
+
 @pytest.mark.parametrize("dtype,n,E,d,o,r,bias", [
     ("f32", 1, 1, 8, 8, 8, True), ("bf16", 2, 3, 16, 8, 8, False), ("bf16", 300, 5, 72, 136, 24, True),
     ("f32", 777, 8, 64, 1000, 8, True), ("bf16", 1000, 300, 64, 104, 16, False), ("bf16", 2500, 3, 136, 72, 128, True),
