@@ -20,11 +20,10 @@ __device__ __forceinline__ void wave_lds_fence() {
 // (bitonic, each merge starting with the mirrored pair, so that every step keeps the larger value
 // in the lower lane), then the 16 largest of two rows are the larger ones of one row and the other
 // reversed, sorted again.  A step is a lane move and a median with +inf or -inf: about 50
-// instructions (130 in a full sort by selects of minima and maxima).
-__device__ __forceinline__ float max_of(float a, float b) {  // one instruction, any NaN passed over
-  return __builtin_amdgcn_fmed3f(a, b, INFINITY);
-}
+// instructions (130 in a full sort by selects of minima and maxima).  NaN counts as -inf: the median of two
+// NaN and +inf is +inf, which no lane holds.
 __device__ __forceinline__ float mth_lane_value(float x, int m, int l) {
+  x = fmaxf(x, -INFINITY);
   const auto step = [&](float y, int bit) {
     x = __builtin_amdgcn_fmed3f(x, y, (l & bit) ? -INFINITY : INFINITY);  // the smaller : the larger
   };
@@ -44,14 +43,14 @@ __device__ __forceinline__ float mth_lane_value(float x, int m, int l) {
   xor1();
   // rows 0 and 2 take the best of rows 0, 1 and 2, 3
   unsigned y = __float_as_uint(dpp<0x140>(x));
-  x = max_of(x, __uint_as_float(__builtin_amdgcn_permlane16_swap(y, y, false, false)[1]));
+  x = fmaxf(x, __uint_as_float(__builtin_amdgcn_permlane16_swap(y, y, false, false)[1]));
   xor8();
   xor4();
   xor2();
   xor1();
   // row 0 the best of all
   y = __float_as_uint(dpp<0x140>(x));
-  x = max_of(x, __uint_as_float(__builtin_amdgcn_permlane32_swap(y, y, false, false)[1]));
+  x = fmaxf(x, __uint_as_float(__builtin_amdgcn_permlane32_swap(y, y, false, false)[1]));
   xor8();
   xor4();
   xor2();

@@ -241,7 +241,7 @@ __global__ void __launch_bounds__(256) k_token_logprob(LogprobArgs a) {
 #pragma unroll
       for (int z = 1; z < N; ++z) {
         f[u][z] = to_f32(e[z]);
-        cm[u] = max_of(cm[u], f[u][z]);
+        cm[u] = fmaxf(cm[u], f[u][z]);
       }
       cm[u] = ANC ? base[u] + cm[u] : cm[u];
     }

@@ -197,7 +197,7 @@ __global__ void __launch_bounds__(64 * kTopmWaves, 6)
   };
   const auto tile = [&](int t) { return present(t < nt ? arow[(int64_t)t * n] : floatx4{NAN, NAN, NAN, NAN}, t); };
   const auto top_of = [](float x, const floatx4& q) {
-    return max_of(max_of(max_of(max_of(x, q[0]), q[1]), q[2]), q[3]);
+    return fmaxf(fmaxf(fmaxf(fmaxf(x, q[0]), q[1]), q[2]), q[3]);
   };
   floatx4 q[kTopmRegTiles];
 #pragma unroll
@@ -301,7 +301,7 @@ __global__ void __launch_bounds__(64 * kTopmWaves, 6)
 #pragma unroll
       for (int z = 0; z < EPV; ++z) {
         f[u][z] = c0[u] < V ? a + to_f32(e[z]) : NAN;  // absent: never listed
-        best = max_of(best, f[u][z]);
+        best = fmaxf(best, f[u][z]);
       }
     }
     const float t1 = mth_lane_value(best, m, l);
