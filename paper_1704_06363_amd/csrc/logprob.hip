@@ -226,8 +226,8 @@ __global__ void __launch_bounds__(256) k_token_logprob(LogprobArgs a) {
   };
   if (b0 < end) load(b0);
   for (int b = b0; b < end; b += step) {
-    // stored values, the anchors that are added to them, and each vector's largest entry
-    float f[U][N], base[U], cm[U];
+    // the entries, as fp32 sums with their anchors, and each vector's largest
+    float f[U][N], cm[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const bool in = b + 64 * u + l < end;
@@ -236,14 +236,12 @@ __global__ void __launch_bounds__(256) k_token_logprob(LogprobArgs a) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) q[i] = in ? q[i] : kNone;
       const T* e = reinterpret_cast<const T*>(&q);
-      base[u] = ANC && in ? an[u] : 0.f;
-      f[u][0] = cm[u] = to_f32(e[0]);
+      const float base = ANC && in ? an[u] : 0.f;
 #pragma unroll
-      for (int z = 1; z < N; ++z) {
-        f[u][z] = to_f32(e[z]);
-        cm[u] = fmaxf(cm[u], f[u][z]);
+      for (int z = 0; z < N; ++z) {
+        f[u][z] = ANC ? base + to_f32(e[z]) : to_f32(e[z]);
+        cm[u] = z == 0 ? f[u][0] : fmaxf(cm[u], f[u][z]);
       }
-      cm[u] = ANC ? base[u] + cm[u] : cm[u];
     }
     if (b + step < end) load(b + step);
     float mx = r.M;
@@ -252,16 +250,14 @@ __global__ void __launch_bounds__(256) k_token_logprob(LogprobArgs a) {
     r.raise(mx, c2);
     float S = 0.f, Tn = 0.f;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const float ref = ANC ? mx - base[u] : mx;
+    for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int z = 0; z < N; ++z) {
-        const float d = f[u][z] - ref;
+        const float d = f[u][z] - mx;
         const float e = __builtin_amdgcn_exp2f(d * c2);
         S += e;
         Tn = fmaf(e, fmaxf(d, -FLT_MAX), Tn);
       }
-    }
     r.S += S;
     r.T += Tn;
     if constexpr (TOP) {
@@ -277,9 +273,6 @@ __global__ void __launch_bounds__(256) k_token_logprob(LogprobArgs a) {
       for (int u = 0; u < U; ++u) {
         const float below = top.below();
         if (__ballot(cm[u] > below) == 0) continue;
-        if constexpr (ANC)
-#pragma unroll
-          for (int z = 0; z < N; ++z) f[u][z] += base[u];  // the entries, as fp32 sums
         // the lanes' entries that may enter, one of each lane at a time
         const int v = b + 64 * u + l;
         uint32_t bits = 0;

@@ -1,10 +1,14 @@
-"""Token log-probabilities of rows that the usual ones do not show: blocks of NaN.
+"""Token log-probabilities of rows that the usual ones do not show: blocks of NaN, anchored logits of a large
+size.
 
 Tolerances as in test_gpu_logprob.py, whose plain forms these tests use."""
+import numpy as np
 import pytest
 import torch
 
-from tests.test_gpu_logprob import check, rows, tokens
+from paper_1704_06363_amd import hmoe
+from tests.parity import np64
+from tests.test_gpu_logprob import DT, check, check_grad, rows, tokens
 
 pytestmark = pytest.mark.gpu
 
@@ -29,3 +33,19 @@ def blocks_of_nan(n, V, dtype, seed):
 def test_blocks_of_nan_rank_last(dtype, n, V, m):
     """A row in several pieces, in one of four waves, in one of one wave."""
     check(blocks_of_nan(n, V, dtype, V + m), tokens(n, V, m), m, 1.0)
+
+
+@pytest.mark.parametrize("dtype,n,V,size", [("bf16", 12, 1000, 1e3), ("f32", 12, 1000, 1e4), ("bf16", 6, 30000, 1e4),
+                                            ("f32", 600, 24000, 3e3), ("bf16", 1100, 520, 1e4)])
+def test_anchored_logits_of_any_size(dtype, n, V, size):
+    """A logit is anchor + stored value rounded to fp32, at 10^4 to 5e-4: the sums and the gradient take that number."""
+    rs = np.random.default_rng(V)
+    nb, tiles = -(-V // hmoe.ANCHOR_COLS), hmoe.anchor_shape(n, V)[0]
+    a = np.full((n, tiles * 4), -3.0e38, np.float32)
+    a[:, :nb] = size * rs.choice([1.0, 1.0003, 0.9998], (n, 1)) + rs.standard_normal((n, nb))
+    anchor = torch.tensor(a.reshape(n, tiles, 4).transpose(1, 0, 2).copy()).cuda()
+    x = torch.tensor(-np.abs(rs.standard_normal((n, V)) * 3)).to(DT[dtype]).cuda()
+    full = (np.repeat(a[:, :nb], hmoe.ANCHOR_COLS, 1)[:, :V] + np64(x).astype(np.float32)).astype(np.float64)
+    t = tokens(n, V, 1)
+    f, lp, ent = check(x, t, 6, 1.0, anchor=anchor, full=full)
+    check_grad(x, t, 1.0, f, lp, ent, 2, anchor=anchor)
