@@ -49,7 +49,8 @@ int hmoe_token_logprob(const void* logits, int64_t ld, const float* anchor, hmoe
 /* The gradient of  sum_i g_logp[i] logp[i] + g_entropy[i] entropy[i]  with respect to the logits:
  *   dlogits[i][v] = scale * (g_logp ([v = t] - p_v) - g_entropy p_v (ln p_v + entropy))
  * with p_v = exp(scale (logit_v - stat[0]) - stat[1]).  Rows without a token take nothing from g_logp;
- * masked entries and rows of nothing else get 0.
+ * rows of masked entries alone get 0, and so do masked entries of other rows -- but for the row's own token, whose
+ * entry gets scale * g_logp there, as the formula with p = 0 has it.
  *   stat and entropy are the forward's.  g_logp, g_entropy float[n], either may be NULL (zeros); entropy
  *   is needed with g_entropy, token with g_logp.
  *   dlogits [n][vocab] in dtype dt, rows ld_out >= vocab elements apart; it may be logits itself (without

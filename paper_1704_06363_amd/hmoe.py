@@ -640,7 +640,8 @@ def token_logprob(logits, token=None, m: int = 0, scale: float = 1.0, anchor=Non
 def token_logprob_backward(logits, token, stat, entropy=None, g_logp=None, g_entropy=None, scale: float = 1.0,
                            anchor=None, out=None):
     """The gradient with respect to the logits [n, V] of sum(g_logp * logp) + sum(g_entropy * entropy),
-    from the forward's stat and (with g_entropy) entropy.  out: a buffer, which may be logits itself."""
+    from the forward's stat and (with g_entropy) entropy.  Entries of -inf get 0, but the row's token among them
+    scale * g_logp.  out: a buffer, which may be logits itself."""
     n, V = logits.shape
     f32 = torch.float32
     dt = _dt(logits)

@@ -1,5 +1,5 @@
 """Token log-probabilities of rows that the usual ones do not show: blocks of NaN, anchored logits of a large
-size.
+size, tokens that are masked.
 
 Tolerances as in test_gpu_logprob.py, whose plain forms these tests use."""
 import numpy as np
@@ -8,7 +8,7 @@ import torch
 
 from paper_1704_06363_amd import hmoe
 from tests.parity import np64
-from tests.test_gpu_logprob import DT, check, check_grad, rows, tokens
+from tests.test_gpu_logprob import DT, INF, check, check_grad, rows, tokens
 
 pytestmark = pytest.mark.gpu
 
@@ -49,3 +49,24 @@ def test_anchored_logits_of_any_size(dtype, n, V, size):
     t = tokens(n, V, 1)
     f, lp, ent = check(x, t, 6, 1.0, anchor=anchor, full=full)
     check_grad(x, t, 1.0, f, lp, ent, 2, anchor=anchor)
+
+
+@pytest.mark.parametrize("dtype,n,V", [("bf16", 6, 100), ("f32", 3, 9000)])
+def test_a_masked_token(dtype, n, V):
+    """Its log-probability is -inf, and its own entry of the gradient scale * g_logp as the formula has it: the one
+    masked entry that is not 0."""
+    x, t = rows(n, V, 0, dtype, 1).clone(), tokens(n, V, 2)
+    at = t.long()[:, None]
+    x.scatter_(1, at, -INF)
+    x[:, V // 2::3] = -INF
+    x[:, 0] = 1.0
+    t[t == 0] = V // 2
+    f, lp, ent = check(x, t, 4, 1.5)
+    assert (np64(f["logp"]) == -INF).all()
+    check_grad(x, t, 1.5, f, lp, ent, 3)
+    g = torch.randn(n, device="cuda")
+    d = hmoe.token_logprob_backward(x, t, f["stat"], f["entropy"], g, g, scale=1.5)
+    own = d.gather(1, t.long()[:, None])[:, 0]
+    assert torch.equal(own, (1.5 * g).to(x.dtype))
+    masked = (x == -INF).scatter_(1, t.long()[:, None], False)
+    assert bool((d[masked] == 0).all())
