@@ -32,7 +32,7 @@ extern "C" {
  *   logits [n][vocab] in dtype dt, rows ld elements apart (ld >= vocab), any vocab >= 1, aligned to
  *     their element.  With anchor (float, HMOE_ANCHOR_*; then ld = vocab, a multiple of 8, and both
  *     16-byte aligned) a logit is anchor + stored value, formed in fp32, as hmoe_moe_forward keeps them.
- *   scale > 0 (an inverse temperature), finite.  token int32[n] or NULL (logp is then not written).
+ *   0 < scale <= 2^127 (an inverse temperature).  token int32[n] or NULL (logp is then not written).
  *   logp, entropy, lse float[n], stat float[n][2], top_idx int32[n][m], top_logp float[n][m]: each may be
  *     NULL (top_idx and top_logp if m = 0, top_logp always).  0 <= m <= min(16, vocab).
  * A logit of -inf is a masked entry: probability 0, and nothing in the entropy.  A row of nothing

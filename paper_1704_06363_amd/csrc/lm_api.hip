@@ -1,7 +1,5 @@
 // lm_api.hip -- the extern "C" entry points of include/hmoe_lm.h: argument validation, workspace
 // checks and dispatch to the launchers.  Host code only.
-#include <math.h>
-
 #include "checks.hpp"
 #include "lm_launch.hpp"
 
@@ -17,7 +15,8 @@ static int check_logits(const void* logits, int64_t ld, const float* anchor, hmo
   HMOE_TRY(check_n(n));
   if (vocab < 1) return fail(HMOE_EINVAL, "vocab = %d is not positive", vocab);
   if (ld < vocab) return fail(HMOE_EINVAL, "ld = %lld is less than vocab = %d", (long long)ld, vocab);
-  if (!(scale > 0.f) || isinf(scale)) return fail(HMOE_EINVAL, "scale = %g is not positive and finite", (double)scale);
+  // the kernels take scale log2 e, which has to be finite too
+  if (!(scale > 0.f) || scale > 0x1p127f) return fail(HMOE_EINVAL, "scale = %g outside (0, 2^127]", (double)scale);
   if (n == 0) return HMOE_OK;
   HMOE_TRY(check_ptr("logits", logits, anchor != nullptr));
   if (reinterpret_cast<uintptr_t>(logits) % dtype_size(dt)) return fail(HMOE_ESHAPE, "logits are not aligned to their type");

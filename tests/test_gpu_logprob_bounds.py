@@ -1,5 +1,5 @@
 """Token log-probabilities of rows that the usual ones do not show: blocks of NaN, anchored logits of a large
-size, tokens that are masked.
+size, tokens that are masked, the largest scale.
 
 Tolerances as in test_gpu_logprob.py, whose plain forms these tests use."""
 import numpy as np
@@ -70,3 +70,10 @@ def test_a_masked_token(dtype, n, V):
     assert torch.equal(own, (1.5 * g).to(x.dtype))
     masked = (x == -INF).scatter_(1, t.long()[:, None], False)
     assert bool((d[masked] == 0).all())
+
+
+@pytest.mark.parametrize("dtype,n,V", [("bf16", 5, 700), ("f32", 3, 30000)])
+def test_the_largest_scale(dtype, n, V):
+    """Multiples of 2^-6: every entry but the largest has probability 0."""
+    x, t = rows(n, V, 0, dtype, 1, ties=True) / 64, tokens(n, V, 2)
+    check(x, t, 5, 2.0 ** 127)
