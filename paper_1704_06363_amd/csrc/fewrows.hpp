@@ -138,17 +138,22 @@ __device__ __forceinline__ void stream_groups(const T* const (&wb)[MI], const ui
 
 // An fp32 value as M bf16 numbers that add up to it, each an operand of its own MFMA: two are good to 2^-16 of
 // the value, three hold all of its bits.  All but the last are cut off rather than rounded, so that no
-// finite value becomes infinite.  (fp32 data: the value itself.)
+// finite value becomes infinite.  None is 0 unless the value is, as far as bf16 goes (from 2^-86 on): 0
+// times an infinite factor would make NaN of a product that is infinite.  In its place stands 2^-126, or 2^-40 of
+// smaller values, which no sum notices.  (fp32 data: the value itself.)
 template <typename T, int M>
 struct Parts {
   static constexpr int N = sizeof(T) == 2 ? M : 1;
   T part[N];
   __device__ __forceinline__ explicit Parts(float v) {
+    const float least = copysignf(fminf(fabsf(v) * 0x1p-40f, 0x1p-126f), v);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const float hi = i + 1 < N ? __uint_as_float(__float_as_uint(v) & 0xffff0000u) : v;
       part[i] = from_f32<T>(hi);
-      v = fabsf(v) == INFINITY ? 0.f : v - hi;
+      if (fabsf(v) == INFINITY) continue;  // all of them
+      v = v - hi;
+      v = v == 0.f ? least : v;
     }
   }
 };
