@@ -137,23 +137,22 @@ __device__ __forceinline__ void stream_groups(const T* const (&wb)[MI], const ui
 }
 
 // An fp32 value as M bf16 numbers that add up to it, each an operand of its own MFMA: two are good to 2^-16 of
-// the value, three hold all of its bits.  All but the last are cut off rather than rounded, so that no
-// finite value becomes infinite.  None is 0 unless the value is, as far as bf16 goes (from 2^-86 on): 0
-// times an infinite factor would make NaN of a product that is infinite.  In its place stands 2^-126, or 2^-40 of
-// smaller values, which no sum notices.  (fp32 data: the value itself.)
+// the value, the first two of three as well, three hold all of its bits.  All but the last are cut off rather than
+// rounded, so that no finite value becomes infinite.  None is 0 unless the value is, because an infinite factor
+// would make NaN of it: a value of one number is halved, and a third number without anything to hold is 2^-126, or
+// 2^-40 of smaller values, which no sum notices.  (fp32 data: the value itself.)
 template <typename T, int M>
 struct Parts {
   static constexpr int N = sizeof(T) == 2 ? M : 1;
   T part[N];
   __device__ __forceinline__ explicit Parts(float v) {
-    const float least = copysignf(fminf(fabsf(v) * 0x1p-40f, 0x1p-126f), v);
+    const float half = 0.5f * v, least = copysignf(fminf(fabsf(v) * 0x1p-40f, 0x1p-126f), v);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const float hi = i + 1 < N ? __uint_as_float(__float_as_uint(v) & 0xffff0000u) : v;
-      part[i] = from_f32<T>(hi);
-      if (fabsf(v) == INFINITY) continue;  // all of them
-      v = v - hi;
-      v = v == 0.f ? least : v;
+      const bool all = hi == v;  // infinities too
+      part[i] = from_f32<T>(i == 0 && i + 1 < N && all ? half : hi);
+      v = all ? (i == 0 ? half : least) : v - hi;
     }
   }
 };

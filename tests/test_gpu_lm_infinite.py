@@ -108,3 +108,26 @@ def plain(p, X, ids, dY):
                 out["dX"][i] += v @ A[e]
                 out["dA"][e], out["dB"][e] = v.T @ x[i], dy[i].T @ u
     return out
+
+
+def test_sums_of_integers_are_exact():
+    """Nothing of how a value is taken apart shows in a product: of integers Y is exact, zeros too."""
+    K, d, h, o, n = 4, 264, 520, 264, 40
+    g = torch.Generator().manual_seed(4)
+    few = lambda *s: (torch.randint(-1, 2, s, generator=g) * (torch.rand(s, generator=g) < 0.1)).bfloat16().cuda()
+    p = params(K, d, h, o, "bf16", "relu", False, 3)
+    p["W1"].copy_(few(K, h, d)), p["W2"].copy_(few(K, o, h))
+    X = torch.randint(-1, 2, (n, d), generator=g).bfloat16().cuda()
+    f = hmoe.moe_few(p, X)
+    e, x, W1, W2 = f["expert"][:, 0].cpu().numpy(), np64(X), np64(p["W1"]), np64(p["W2"])
+    ref = np.stack([W2[e[i]] @ np.maximum(W1[e[i]] @ x[i], 0) for i in range(n)])
+    assert (ref == 0).any() and np.array_equal(np64(f["Y"]), np64(torch.tensor(ref).bfloat16()))
+    E, r = 3, 24
+    for m in (1, n):
+        q = {"W": few(o, d), "b": None, "A": few(E, r, d), "B": few(E, o, r), "scale": None}
+        ids = np.arange(m).astype(np.int32) % E
+        ref = plain(dict(q, b=torch.zeros(o)), X[:m], ids, None)["Y"]
+        want = np64(torch.tensor(ref).bfloat16())
+        assert (ref == 0).any() and np.array_equal(np64(hmoe.lora_few(q, X[:m], torch.tensor(ids).cuda())), want)
+        off, perm = order(ids, E)
+        assert np.array_equal(np64(hmoe.lora_forward(q, X[:m][perm.long()].contiguous(), off, perm)["Y"]), want)
