@@ -20,6 +20,7 @@
 
 #include "lanes.hpp"
 #include "lm_launch.hpp"
+#include "slices.hpp"
 
 namespace hmoe {
 
@@ -454,18 +455,10 @@ int logprob_pieces(int64_t n, int V, hmoe_dtype_t dt) {
   return (int)(p < 1 ? 1 : (p > 64 ? 64 : p));
 }
 
-// Launches over slices of the rows: a launch holds fewer than 2^32 threads.
-template <typename F>
-int over_rows(int64_t n, int64_t blocks_per_row, F launch) {
-  const int64_t slice = cdiv(int64_t(1) << 22, blocks_per_row);
-  for (int64_t r = 0; r < n; r += slice) HMOE_TRY(launch(r, n - r < slice ? n - r : slice));
-  return HMOE_OK;
-}
-
 template <typename T, bool ANC, bool TOP>
 int logprob_t(LogprobArgs a, hipStream_t st) {
   const int64_t n = a.n;
-  return over_rows(n, a.pieces, [&](int64_t row0, int64_t rows) {
+  return over_slices(n, a.pieces, 256, [&](int64_t row0, int64_t rows) {
     a.row0 = row0;
     a.n_end = row0 + rows;
     const dim3 block(256);
@@ -483,7 +476,7 @@ int logprob_t(LogprobArgs a, hipStream_t st) {
 
 template <typename T, bool ANC>
 int logprob_grad_t(LogprobGrad a, hipStream_t st) {
-  return over_rows(a.n, a.chunks, [&](int64_t row0, int64_t rows) {
+  return over_slices(a.n, a.chunks, 256, [&](int64_t row0, int64_t rows) {
     a.row0 = row0;
     HMOE_LAUNCH("token logprob gradient", (k_logprob_grad<T, ANC>), dim3((unsigned)(rows * a.chunks)), dim3(256), 0, st,
                 a);

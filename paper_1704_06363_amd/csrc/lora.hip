@@ -12,6 +12,7 @@
 #include "gemm.hpp"
 #include "lm_launch.hpp"
 #include "primitives.hpp"
+#include "slices.hpp"
 
 namespace hmoe {
 
@@ -390,14 +391,15 @@ int lora_few_t(const LoraFew& a, hipStream_t st) {
 
 // U = s_e rows A_e^T for 16 MT rows of one adapter and 16 RT values of the rank: rows [n][K] (row map[p] for slot
 // p, if there is a map), A [E][rank][K].
-// The four waves split K.
+// The four waves split K.  blockIdx.x: the runs from run0 on.
 template <typename T, int RT, int MT>
 __global__ void __launch_bounds__(256) k_lora_shrink(const T* __restrict__ X, int K, const T* __restrict__ A, int rank,
                                                      const float* __restrict__ scale, const int32_t* __restrict__ seg,
-                                                     int E, const int32_t* __restrict__ map, T* __restrict__ U) {
+                                                     int E, const int32_t* __restrict__ map, T* __restrict__ U,
+                                                     int64_t run0) {
   __shared__ floatx4 s_acc[4][RT][MT][64];
   Run run;
-  if (!find_run(seg, E, 16 * MT, blockIdx.x, run)) return;
+  if (!find_run(seg, E, 16 * MT, run0 + blockIdx.x, run)) return;
   const int e = run.segment;
   const int64_t r0 = seg[e] + run.local * (16 * MT);
   const int rows = seg[e + 1] - r0 < 16 * MT ? (int)(seg[e + 1] - r0) : 16 * MT;
@@ -865,15 +867,17 @@ template <typename T>
 int lora_shrink(const T* X, int K, const T* A, int rank, const float* scale, const int32_t* seg, int E,
                 int64_t n, const int32_t* map, T* U, hipStream_t st) {
   const int blocks = u_blocks(rank);
-  const auto bound = [&](int rows) { return (unsigned)(n / rows + (E < n ? E : n)); };
-  if (blocks == 1)
-    HMOE_LAUNCH("lora shrink", (k_lora_shrink<T, 1, 1>), dim3(bound(16)), dim3(256), 0, st, X, K, A, rank, scale, seg, E, map, U);
-  else if (blocks == 2)
-    HMOE_LAUNCH("lora shrink", (k_lora_shrink<T, 2, 2>), dim3(bound(32)), dim3(256), 0, st, X, K, A, rank, scale, seg, E, map, U);
-  else
-    HMOE_LAUNCH("lora shrink", (k_lora_shrink<T, 4, 2>), dim3(bound(32), (unsigned)cdiv(blocks, 4)), dim3(256), 0, st, X, K,
-                A, rank, scale, seg, E, map, U);
-  return HMOE_OK;
+  const int rows = blocks == 1 ? 16 : 32;
+  return over_slices(n / rows + (E < n ? E : n), 1, 256, [&](int64_t run0, int64_t runs) {
+    const dim3 grid((unsigned)runs, (unsigned)cdiv(blocks, 4)), block(256);
+    if (blocks == 1)
+      HMOE_LAUNCH("lora shrink", (k_lora_shrink<T, 1, 1>), grid, block, 0, st, X, K, A, rank, scale, seg, E, map, U, run0);
+    else if (blocks == 2)
+      HMOE_LAUNCH("lora shrink", (k_lora_shrink<T, 2, 2>), grid, block, 0, st, X, K, A, rank, scale, seg, E, map, U, run0);
+    else
+      HMOE_LAUNCH("lora shrink", (k_lora_shrink<T, 4, 2>), grid, block, 0, st, X, K, A, rank, scale, seg, E, map, U, run0);
+    return (int)HMOE_OK;
+  });
 }
 
 // Tiles for the type (gemm.hpp), quarter tiles where there are fewer of them than half of the CUs (bf16, rows of

@@ -3,6 +3,7 @@
 
 #include "fewrows.hpp"
 #include "lm_launch.hpp"
+#include "slices.hpp"
 
 namespace hmoe {
 
@@ -333,7 +334,8 @@ __device__ __forceinline__ floatx4 load_through(const float* p) {
                  __uint_as_float((uint32_t)(hi >> 32))};
 }
 
-// LAYER 1: hid[q] = act(W1_e x + b1_e).   LAYER 2: Y, the combine included.
+// LAYER 1: hid[q] = act(W1_e x + b1_e).   LAYER 2: Y, the combine included.   For the slots from slot0 on, of `slots`
+// in all.
 // A workgroup has 16 outputs (GATED: and the 16 they are gated with) of one expert, or of a split of
 // its reduction; its four waves split that further and join in LDS.  In layer 2 with several parts to an
 // output the workgroup that is the last to store its part of 16 columns adds them up, in the order of the
@@ -343,13 +345,13 @@ __device__ __forceinline__ floatx4 load_through(const float* p) {
 // (2048 -> 1024); one sample with one of 16, U = 4 / 8 / 16: 6.9 / 6.5 / 5.3 us for the first
 // (2048 -> 4096), whose waves have 16 steps each.
 template <typename T, int LAYER, bool GATED, int UG>
-__global__ void __launch_bounds__(256) k_few_layer(FewArgs a, int tiles, int slots) {
+__global__ void __launch_bounds__(256) k_few_layer(FewArgs a, int tiles, int slots, int slot0) {
   constexpr int MI = LAYER == 1 && GATED ? 2 : 1;
   constexpr int NX = LAYER == 2 ? Halves<T>::N : 1;  // operands of an activation
   __shared__ int s_expert, s_count, s_rows[HMOE_FEW_ROWS];
   __shared__ floatx4 s_acc[4][MI][64];
   const int splits = LAYER == 1 ? 1 : a.splits;
-  const int slot = blockIdx.x / (tiles * splits), tile = blockIdx.x % tiles, split = blockIdx.x / tiles % splits;
+  const int slot = slot0 + blockIdx.x / (tiles * splits), tile = blockIdx.x % tiles, split = blockIdx.x / tiles % splits;
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6, lr = l & 15, lg = l >> 4;
   const int c0 = tile * 16 + 4 * lg;
   // the choices of one sample are groups of their own
@@ -481,12 +483,15 @@ template <typename T, int LAYER, bool GATED>
 int few_layer(const FewArgs& a, hipStream_t st) {
   const int slots = (int)few_slots(a.n, a.k, a.K), tiles = (int)cdiv(LAYER == 1 ? a.h : a.o, 16);
   const char* label = LAYER == 1 ? "few layer 1" : "few layer 2";
-  const dim3 grid((unsigned)(slots * tiles * (LAYER == 1 ? 1 : a.splits))), block(256);
-  if (LAYER == 1 && (int64_t)slots * tiles <= 2 * device_cus() && groups_of<T>(a.d) > 8)
-    HMOE_LAUNCH(label, (k_few_layer<T, LAYER, GATED, (GATED ? 2 : 4)>), grid, block, 0, st, a, tiles, slots);
-  else
-    HMOE_LAUNCH(label, (k_few_layer<T, LAYER, GATED, 1>), grid, block, 0, st, a, tiles, slots);
-  return HMOE_OK;
+  const int per = tiles * (LAYER == 1 ? 1 : a.splits);  // workgroups of a slot
+  return over_slices(slots, per, 256, [&](int64_t slot0, int64_t count) {
+    const dim3 grid((unsigned)(count * per)), block(256);
+    if (LAYER == 1 && (int64_t)slots * tiles <= 2 * device_cus() && groups_of<T>(a.d) > 8)
+      HMOE_LAUNCH(label, (k_few_layer<T, LAYER, GATED, (GATED ? 2 : 4)>), grid, block, 0, st, a, tiles, slots, (int)slot0);
+    else
+      HMOE_LAUNCH(label, (k_few_layer<T, LAYER, GATED, 1>), grid, block, 0, st, a, tiles, slots, (int)slot0);
+    return (int)HMOE_OK;
+  });
 }
 
 template <typename T>
