@@ -6,7 +6,7 @@
  * The conventions are hmoe.h's: device pointers, the caller's workspace, one stream, no
  * allocation, no state and no host synchronisation, argument errors before any launch
  * (hmoe_last_error), HMOE_F32 or HMOE_BF16 data with sums in fp32 or wider, calls that can be
- * captured into HIP graphs.
+ * captured into HIP graphs.  Workspaces are 16-byte aligned, too (HMOE_ESHAPE).
  */
 #ifndef HMOE_LM_H_
 #define HMOE_LM_H_

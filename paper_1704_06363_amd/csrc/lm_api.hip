@@ -7,6 +7,12 @@ using namespace hmoe;
 
 extern "C" {
 
+// The kernels take vectors and count workgroups in the workspace.
+static int check_lm_ws(size_t need, size_t have, const void* ws) {
+  HMOE_TRY(check_ws(need, have, ws));
+  return need > 0 ? check_ptr("workspace", ws) : HMOE_OK;
+}
+
 // ------------------------------------------------------------------ token log-probabilities
 
 static int check_logits(const void* logits, int64_t ld, const float* anchor, hmoe_dtype_t dt, int64_t n, int32_t vocab,
@@ -41,7 +47,7 @@ int hmoe_token_logprob(const void* logits, int64_t ld, const float* anchor, hmoe
   if (m < 0 || m > 16 || m > vocab) return fail(HMOE_EINVAL, "m = %d outside [0, min(16, vocab)]", m);
   if (n == 0) return HMOE_OK;
   if (m > 0) HMOE_TRY(check_ptr("top_idx", top_idx, false));
-  HMOE_TRY(check_ws(token_logprob_ws(n, vocab, m, dt), ws_bytes, ws));
+  HMOE_TRY(check_lm_ws(token_logprob_ws(n, vocab, m, dt), ws_bytes, ws));
   Workspace w(ws, ws_bytes);
   return launch_token_logprob(logits, ld, anchor, dt, n, vocab, scale, token, m, logp, entropy, lse, stat, top_idx,
                               top_logp, w, (hipStream_t)stream);
@@ -108,7 +114,7 @@ int hmoe_moe_few(const hmoe_few_params_t* p, int64_t n, const void* X, int32_t* 
   HMOE_TRY(check_ptr("expert", expert, false));
   HMOE_TRY(check_ptr("weight", weight, false));
   HMOE_TRY(check_ptr("Y", Y));
-  HMOE_TRY(check_ws(moe_few_ws(p, n), ws_bytes, ws));
+  HMOE_TRY(check_lm_ws(moe_few_ws(p, n), ws_bytes, ws));
   Workspace w(ws, ws_bytes);
   return launch_moe_few(p, n, X, expert, weight, Y, w, (hipStream_t)stream);
 }
@@ -157,7 +163,7 @@ int hmoe_lora_few(const hmoe_lora_t* p, int64_t n, const void* X, const int32_t*
   HMOE_TRY(check_ptr("X", X));
   HMOE_TRY(check_ptr("adapter", adapter, false));
   HMOE_TRY(check_ptr("Y", Y));
-  HMOE_TRY(check_ws(lora_few_ws(p, n), ws_bytes, ws));
+  HMOE_TRY(check_lm_ws(lora_few_ws(p, n), ws_bytes, ws));
   Workspace w(ws, ws_bytes);
   return launch_lora_few(p, n, X, adapter, Y, w, (hipStream_t)stream);
 }
@@ -186,7 +192,7 @@ int hmoe_lora_forward(const hmoe_lora_t* p, int64_t n, const void* X_sorted, con
   HMOE_TRY(check_ptr("offsets", offsets, false));
   HMOE_TRY(check_ptr("U", U));
   HMOE_TRY(check_ptr("Y", Y));
-  HMOE_TRY(check_ws(lora_ws(p, n), ws_bytes, ws));
+  HMOE_TRY(check_lm_ws(lora_ws(p, n), ws_bytes, ws));
   Workspace w(ws, ws_bytes);
   return launch_lora_forward(p, n, X_sorted, offsets, perm, U, Y, w, (hipStream_t)stream);
 }
@@ -206,7 +212,7 @@ int hmoe_lora_backward(const hmoe_lora_t* p, int64_t n, const void* X_sorted, co
     HMOE_TRY(check_ptr("U", U));
     HMOE_TRY(check_ptr("dY", dY));
     if (dX) HMOE_TRY(check_ptr("dX", dX));
-    HMOE_TRY(check_ws(lora_ws(p, n), ws_bytes, ws));
+    HMOE_TRY(check_lm_ws(lora_ws(p, n), ws_bytes, ws));
     Workspace w(ws, ws_bytes);
     return launch_lora_backward(p, n, X_sorted, offsets, perm, U, dY, dX, dA, dB, w, (hipStream_t)stream);
   }

@@ -1,10 +1,12 @@
 """Limits of the entry points of include/hmoe_lm.h (no GPU needed), and of what one launch holds."""
+import ctypes
 import os
 import shutil
 import subprocess
 
 import pytest
 
+from paper_1704_06363_amd import hmoe
 from tests.test_lm_abi import F, ROOT, lib, refused  # noqa: F401 (lib: the fixture)
 
 
@@ -43,3 +45,15 @@ def test_slices_hold_fewer_than_2_to_32_threads(slices, units, blocks, threads):
         at += count
     assert at == units
     assert (calls, third) == ((3, -7) if len(parts) >= 3 else (len(parts), 0))
+
+
+def test_workspaces_that_are_not_aligned(lib):  # noqa: F811
+    big = 1 << 40
+    refused(lib.hmoe_token_logprob(16, 100000, None, 1, 1, 100000, F(1.0), 16, 3, 16, 16, 16, 16, 16, 16, 24, big, None),
+            -3, "workspace")
+    few = hmoe.FewParams(8, 64, 128, 64, 2, 1, 0, 16, None, 16, None, 16, None)
+    refused(lib.hmoe_moe_few(ctypes.byref(few), 4, 16, 16, 16, 16, 20, big, None), -3, "workspace")
+    p = hmoe.Lora(8, 64, 128, 16, 1, 16, None, 16, 16, None)
+    refused(lib.hmoe_lora_few(ctypes.byref(p), 4, 16, 16, 16, 17, big, None), -3, "workspace")
+    refused(lib.hmoe_lora_forward(ctypes.byref(p), 400, 16, 16, None, 16, 16, 8, big, None), -3, "workspace")
+    refused(lib.hmoe_lora_backward(ctypes.byref(p), 400, 16, 16, None, 16, 16, 16, 16, 16, 8, big, None), -3, "workspace")
