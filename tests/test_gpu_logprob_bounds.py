@@ -77,3 +77,19 @@ def test_the_largest_scale(dtype, n, V):
     """Multiples of 2^-6: every entry but the largest has probability 0."""
     x, t = rows(n, V, 0, dtype, 1, ties=True) / 64, tokens(n, V, 2)
     check(x, t, 5, 2.0 ** 127)
+
+
+@pytest.mark.parametrize("scale", [1.0, 0.5])
+def test_gradients_of_tokens_that_are_nearly_certain(scale):
+    """Rows of two entries, p of the first 1 - e with e from 1e-2 to 1e-5: its gradient is 1 - p, and p carries
+    the rounding of S = 1 + e (2^-24), v_exp_f32's last place (2^-23) and that of its argument and of the difference
+    (2^-24 each, at most): 2.5 2^-23 of the gradient of logp."""
+    n = 4000
+    x = torch.zeros(n, 2, device="cuda")
+    x[:, 1] = -torch.linspace(4.6, 11.5, n, device="cuda") / scale
+    t = torch.zeros(n, dtype=torch.int32, device="cuda")
+    f = hmoe.token_logprob(x, t, scale=scale)
+    g = np64(hmoe.token_logprob_backward(x, t, f["stat"], None, torch.ones(n, device="cuda"), scale=scale))
+    e = np.exp(scale * np64(x)[:, 1])
+    ref = scale * (e / (1 + e))
+    assert np.abs(g[:, 0] - ref).max() <= scale * 2.5 * 2.0 ** -23
