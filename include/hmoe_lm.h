@@ -86,14 +86,15 @@ typedef struct {
   const void *W1, *b1, *W2, *b2;
 } hmoe_few_params_t;
 
-/* The whole layer for 1 <= n <= HMOE_FEW_ROWS samples, for serving: no sort, no padding, each
- * expert that is chosen read once.  For row i of X [n x d_in]:
+/* The whole layer for 1 <= n <= HMOE_FEW_ROWS samples, for serving: no sort, no padding, an
+ * expert's weights read once for every 16 samples that chose it.  For row i of X [n x d_in]:
  *   s_e = R_e . x + r_bias[e];  expert[i][0 .. top_k) = the top_k largest, in decreasing order, equal ones in
  *   increasing e (NaN ranks last);  weight[i][j] = softmax of those top_k scores;
  *   Y[i] = sum_j weight[i][j] (W2_e h + b2_e), e = expert[i][j].
  * A weight below 2^-126, the smallest normal float, is 0, and an expert of weight 0 is not evaluated: one
- * with a score of -inf (r_bias[e] = -inf: it is off) never is.  A row of nothing else has Y = 0.  Scores, sums, h and weights are held in fp32; for the second product
- * of bf16 data h is split into two bf16 numbers, so nothing but Y is rounded to bf16.
+ * with a score of -inf (r_bias[e] = -inf: it is off) never is.  A row of nothing else has Y = 0.
+ * Scores, sums, h and weights are held in fp32; the second product of bf16 data takes h as two bf16 numbers, good to
+ * 2^-16 of it, and Y is rounded to bf16 once.
  *   expert int32[n][top_k], weight float[n][top_k], Y [n x d_out] in dtype dt: out.
  * 1 <= top_k <= min(HMOE_FEW_EXPERTS, K).  Errors: HMOE_EINVAL (n, K, top_k or act out of range, NULL pointer),
  * HMOE_ESHAPE (width not a multiple of 8, misaligned pointer), HMOE_EDTYPE, HMOE_EWORKSPACE. */
@@ -121,7 +122,9 @@ typedef struct {
 } hmoe_lora_t;
 
 /* For serving: n <= HMOE_FEW_ROWS rows X [n x d_in] of any mix of requests, adapter int32[n] (an id outside
- * [0, E): none); Y [n x d_out] out.  W is read once, and so is each adapter that is used. */
+ * [0, E): none); Y [n x d_out] out.  W is read once, of each adapter that is used B once and A once for every 16 of
+ * its rows (and A by every workgroup, from the caches, where one row and a narrow A take one launch).  Y is rounded to
+ * the data type as it is: bf16 logits have no anchors here and are good to 2^-9 of their size. */
 size_t hmoe_lora_few_workspace(const hmoe_lora_t* p, int64_t n);
 int hmoe_lora_few(const hmoe_lora_t* p, int64_t n, const void* X, const int32_t* adapter, void* Y, void* ws,
                   size_t ws_bytes, void* stream);
@@ -129,7 +132,7 @@ int hmoe_lora_few(const hmoe_lora_t* p, int64_t n, const void* X, const int32_t*
 /* Many rows, in adapter order as hmoe_moe_dispatch leaves them: X_sorted [n x d_in], rows [offsets[a],
  * offsets[a + 1]) with adapter a and rows from offsets[E] on without one; offsets int32[E + 1] starts at 0.
  * perm int32[n] (slot -> sample, a permutation), or NULL: Y's rows are in slot order too.
- *   Y [n x d_out] out, sample order.
+ *   Y [n x d_out] out, sample order; rounded as above.
  *   U [n][hmoe_lora_saved_width] out, dtype dt: scale A x of every row with an adapter, for the
  *     backward, in fp32: with bf16 data as three bf16 numbers a value, in blocks of 16 values. */
 int32_t hmoe_lora_saved_width(int32_t rank, hmoe_dtype_t dt);

@@ -4,7 +4,8 @@ The shared decoder of the paper's Section 2 gets a low-rank adapter for every cl
 their own for the experts at a small part of the independent decoders' parameters.
 
   answer     features of a few samples -> gater and experts (moe_few) -> decoder with the cluster's
-             adapter (lora_few) -> the most probable tags, with log-probabilities and the entropy (token_logprob)
+             adapter (lora_few) -> the most probable tags, with log-probabilities and the entropy (token_logprob);
+             with bf16 parameters the logits between the two are plain bf16, good to 2^-9 of their size
   tune_step  one step of the adapters on samples with a tag each: rows by cluster (moe_dispatch), decoder with
              adapters (lora_forward), log-probabilities of the tags (token_logprob), their gradient back
              (token_logprob_backward, lora_backward), and the update (sgd_step)

@@ -367,7 +367,7 @@ int lora_few_t(const LoraFew& a, hipStream_t st) {
   // Eight waves to a workgroup rather than four where there is one on each CU at most, for more than 16 rows
   // (bf16, 2048 -> 4096, 16 adapters: 48 rows 17.4 -> 15.2 us, 64 rows of rank 128 31 -> 24; 4 rows 10.2 ->
   // 10.6; 64 rows, 8192 columns 24 -> 27), and for one row whose reduction gives each two groups (2048 -> 4096
-  // 6.7 -> 6.1 us, 1024 -> 1024 4.5 -> 4.7).
+  // 7.6 -> 7.1 us with W in the caches, 9.4 -> 9.7 from HBM; 1024 -> 1024, one group, 4.5 -> 4.7).
   const bool narrow = cdiv(a.o, 16) <= device_cus();
   // One row: in one launch where reading A for every 16 columns (up to 20 MB from L2 per 16 of the rank,
   // 4 us) takes less than a second one.
