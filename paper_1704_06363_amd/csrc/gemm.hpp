@@ -635,7 +635,7 @@ struct CfgP {
   static constexpr bool F32 = sizeof(T) == 4;
   static constexpr bool DMA = true, PIPE = true;
   static constexpr bool TRANS = true;  // accumulator element (i, j, r) at row 16 i + l % 16, col 16 j + 4 (l / 16) + r
-  static constexpr bool SPLIT = SPLIT_;
+  static constexpr bool SPLIT = SPLIT_, PAIR = false;
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
   static constexpr int WAVES_N = BN / WN, WAVES_M = BM / WM;
   static constexpr int WAVES = WAVES_M * WAVES_N;
@@ -655,6 +655,19 @@ typedef CfgP<float, 256, 256, 128, 64, false> CfgPipeF32;  // fp32, K-contiguous
 // at half height, with half the MFMA work of the padded 256-row tile.
 typedef CfgP<bf16, 128, 256, 64, 64, false> CfgPipeShort;
 typedef CfgP<bf16, 128, 256, 64, 64, true> CfgPipeShortKS;
+// Values of two fp16 numbers, v = hi + lo (PAIR).  Rows hold 32 values of K as 32 hi and then 32 lo, so that a
+// stage is 32 values of K and the fragments of its two MFMA steps are their hi and lo: three products, hi lo, lo hi
+// and hi hi, of what is read for two.  A K-strided operand is stored like that along its rows, too: of
+// the 64 K rows of a stage the first 32 are the hi of 32 rows of it, the others their lo.
+template <int BM_, int BN_, int WM_, int WN_, bool SPLIT_>
+struct CfgPair : CfgP<_Float16, BM_, BN_, WM_, WN_, SPLIT_> {
+  static constexpr bool PAIR = true;
+};
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+// Where value c of a row of pairs has its hi; its lo is kPairLo units behind.
+constexpr int kPairLo = 32;
+__host__ __device__ __forceinline__ int pair_at(int c) { return (c >> 5) * 64 + (c & 31); }
+
 template <class C>
 struct ShortTile {
   using type = void;
@@ -689,11 +702,12 @@ static __device__ const i32x4 kZeros = {0, 0, 0, 0};
 // Half panels of an operand of R tile rows, W per wave strip.
 //   K-contiguous: slot [R / 2 rows][64 K], 16-byte chunk c of slot row r at c ^ ((r ^ (r >> 2)) & 7).
 //   K-strided:    slot [64 K][R / 2 rows], chunk swizzle of ks_off<R / 2>.
-template <int R, int W, int THREADS, bool KC, bool SPLIT>
+template <int R, int W, int THREADS, bool KC, bool SPLIT, bool PAIR = false>
 struct HalfPanels {
   static constexpr int HR = R / 2;
   static constexpr int NQ = HR * 128 / (THREADS * 16);  // loads per wave and half
   static_assert(NQ * THREADS * 16 == HR * 128, "whole loads");
+  static_assert(KC || HR >= 128, "the chunk swizzle of a K-strided row spans 128 columns");
   uint32_t off[2][NQ];  // byte offset of this lane's 16 bytes from the stage's base
 
   // tile row of row q of half h
@@ -722,6 +736,8 @@ struct HalfPanels {
     } else {
       const int sw = ((k & 3) | ((k >> 1) & 4)) << 1;
       const int col = tile_row(h, ((piece % (HR / 8)) ^ sw) * 8);
+      if constexpr (PAIR)
+        return (uint32_t)(((k & 31) * ld + pair_at(col < rows_valid ? col : 0) + (k >> 5) * kPairLo) * 2);
       return (uint32_t)((k * ld + (col < rows_valid ? col : 0)) * 2);
     }
   }
@@ -837,8 +853,8 @@ struct HalfFrags {
 // step 685 -> 630, 5003 x 1000 and 50 experts 131 -> 119).
 template <class C, bool A_KC, bool B_KC, int A_SW = 0, bool REG_TAIL = false>
 struct PipeTile {
-  using OA = HalfPanels<C::BM, C::WM, C::THREADS, A_KC, false>;
-  using OB = HalfPanels<C::BN, C::WN, C::THREADS, B_KC, C::SPLIT>;
+  using OA = HalfPanels<C::BM, C::WM, C::THREADS, A_KC, false, C::PAIR>;
+  using OB = HalfPanels<C::BN, C::WN, C::THREADS, B_KC, C::SPLIT, C::PAIR>;
   static constexpr int AL = OA::NQ, BL = OB::NQ;
   static constexpr int HI = C::MI / 2, HJ = C::NJ / 2;
   static_assert(A_SW == 0 || (A_KC && A_SW % C::BK == 0), "slab-major A: K-contiguous, whole stages per slab");
@@ -898,8 +914,9 @@ struct PipeTile {
     k_len = __builtin_amdgcn_readfirstlane(k_len);
     nk = (REG_TAIL ? k_len : k_len + C::BK - 1) / C::BK;
     k_last = k_len - (REG_TAIL ? nk : nk - 1) * C::BK;
-    step_a = A_KC ? C::BK * 2 : C::BK * 2 * lda;
-    step_b = B_KC ? C::BK * 2 : C::BK * 2 * ldb;
+    constexpr int kRows = C::PAIR ? C::BK / 2 : C::BK;  // of a K-strided operand to a stage
+    step_a = A_KC ? C::BK * 2 : kRows * 2 * lda;
+    step_b = B_KC ? C::BK * 2 : kRows * 2 * ldb;
     oa.init(lda, a_rows);
     ob.init(ldb, b_rows);
     if constexpr (LONG) {
@@ -939,6 +956,19 @@ struct PipeTile {
   template <int QI, int QJ>
   __device__ __forceinline__ static void mfmas(const bf16x8 (&a)[HI][2], const bf16x8 (&b)[HJ][2],
                                                floatx4 (&acc)[C::MI][C::NJ]) {
+    if constexpr (C::PAIR) {
+#pragma unroll
+      for (int p = 0; p < 3; ++p)  // the small products first
+#pragma unroll
+        for (int i = 0; i < HI; ++i)
+#pragma unroll
+          for (int j = 0; j < HJ; ++j) {
+            floatx4& c = acc[QI * HI + i][QJ * HJ + j];
+            c = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, b[j][p == 0]),
+                                                       __builtin_bit_cast(f16x8, a[i][p == 1]), c, 0, 0, 0);
+          }
+      return;
+    }
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
 #pragma unroll

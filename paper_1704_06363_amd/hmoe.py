@@ -1,4 +1,4 @@
-"""Python binding of libhmoe.so (include/hmoe.h and include/hmoe_lm.h): argument marshalling only.
+"""Python binding of libhmoe.so (include/hmoe.h, hmoe_lm.h and hmoe_train.h): argument marshalling only.
 
 Tensors are torch tensors on the GPU; every function hands their device pointers, the
 current HIP stream and a workspace to the C ABI and returns the output tensors.  No step of
@@ -39,6 +39,13 @@ LM_SYMBOLS = (
     "hmoe_lora_backward",
 )
 
+# include/hmoe_train.h
+TRAIN_SYMBOLS = (
+    "hmoe_router_workspace", "hmoe_router_forward", "hmoe_router_backward",
+    "hmoe_join_forward", "hmoe_join_workspace", "hmoe_join_backward",
+    "hmoe_orthogonalise_workspace", "hmoe_orthogonalise", "hmoe_muon_workspace", "hmoe_muon_step",
+)
+
 
 class HmoeError(RuntimeError):
     pass
@@ -63,6 +70,17 @@ class Lora(ctypes.Structure):
     _fields_ = [("E", ctypes.c_int32), ("d_in", ctypes.c_int32), ("d_out", ctypes.c_int32), ("rank", ctypes.c_int32),
                 ("dt", ctypes.c_int), ("W", ctypes.c_void_p), ("b", ctypes.c_void_p), ("A", ctypes.c_void_p),
                 ("B", ctypes.c_void_p), ("scale", ctypes.c_void_p)]
+
+
+class Router(ctypes.Structure):
+    _fields_ = [("K", ctypes.c_int32), ("d", ctypes.c_int32), ("top_k", ctypes.c_int32), ("dt", ctypes.c_int),
+                ("renorm", ctypes.c_int32), ("R", ctypes.c_void_p), ("bias", ctypes.c_void_p)]
+
+
+class Join(ctypes.Structure):
+    _fields_ = [("d", ctypes.c_int32), ("k", ctypes.c_int32), ("dt", ctypes.c_int), ("norm_y", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("eps", ctypes.c_float), ("gamma_y", ctypes.c_void_p),
+                ("gamma_h", ctypes.c_void_p)]
 
 
 class Labels(ctypes.Structure):
@@ -135,8 +153,25 @@ def lib():
         L.hmoe_lora_few.argtypes = [_c.POINTER(Lora), _I64, _P, _P, _P, _P, _SZ, _P]
         L.hmoe_lora_forward.argtypes = [_c.POINTER(Lora), _I64, _P, _P, _P, _P, _P, _P, _SZ, _P]
         L.hmoe_lora_backward.argtypes = [_c.POINTER(Lora), _I64, _P, _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P]
+        L.hmoe_router_workspace.restype = _SZ
+        L.hmoe_router_workspace.argtypes = [_c.POINTER(Router), _I64]
+        L.hmoe_router_forward.argtypes = [_c.POINTER(Router), _I64, _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P]
+        L.hmoe_router_backward.argtypes = [_c.POINTER(Router), _I64, _P, _P, _P, _P, _P, _c.c_float, _c.c_float, _P, _P,
+                                           _P, _P, _SZ, _P]
+        L.hmoe_join_forward.argtypes = [_c.POINTER(Join), _I64, _P, _P, _P, _P, _P, _P]
+        L.hmoe_join_workspace.restype = _SZ
+        L.hmoe_join_workspace.argtypes = [_c.POINTER(Join), _I64]
+        L.hmoe_join_backward.argtypes = [_c.POINTER(Join), _I64, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P]
+        L.hmoe_orthogonalise_workspace.restype = _SZ
+        L.hmoe_orthogonalise_workspace.argtypes = [_I32, _I32, _I32, _c.c_int]
+        L.hmoe_orthogonalise.argtypes = [_P, _c.c_int, _I32, _I32, _I32, _I32, _P, _P, _P, _SZ, _P]
+        L.hmoe_muon_workspace.restype = _SZ
+        L.hmoe_muon_workspace.argtypes = [_I32, _I32, _I32]
+        L.hmoe_muon_step.argtypes = [_P, _P, _P, _P, _c.c_int, _I32, _I32, _I32, _c.c_float, _c.c_float, _c.c_float, _I32,
+                                     _c.c_float, _I32, _P, _P, _SZ, _P]
         for name in ("hmoe_token_logprob", "hmoe_token_logprob_backward", "hmoe_moe_few", "hmoe_lora_few",
-                     "hmoe_lora_forward", "hmoe_lora_backward"):
+                     "hmoe_lora_forward", "hmoe_lora_backward", "hmoe_router_forward", "hmoe_router_backward",
+                     "hmoe_join_forward", "hmoe_join_backward", "hmoe_orthogonalise", "hmoe_muon_step"):
             getattr(L, name).restype = _c.c_int
         for name in ("hmoe_kmeans_assign", "hmoe_kmeans_fit", "hmoe_kmeans_update",
                      "hmoe_moe_dispatch", "hmoe_moe_dispatch_noalloc", "hmoe_permute_rows", "hmoe_moe_forward",
@@ -825,7 +860,239 @@ def lora_backward(p, X_sorted, offsets, dY, U, perm=None, want_dX=True, want_ada
     return {"dX": dX, "dA": dA, "dB": dB}
 
 
+# ------------------------------------------------------------------ router of a batch
+
+ROUTER_EXPERTS, JOIN_ROWS = 8, 8  # include/hmoe_train.h: HMOE_ROUTER_EXPERTS, HMOE_JOIN_ROWS
+COEF = (3.4445, -4.7750, 2.0315)  # of hmoe_orthogonalise's iterations
+
+
+def _same_device(*tensors):
+    """The device that all of them (None aside) are on, a GPU; the library launches on the current one."""
+    dev = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise HmoeError("tensor is not on the GPU")
+        if dev is None:
+            dev = t.device
+        elif t.device != dev:
+            raise HmoeError(f"tensors on {dev} and {t.device}")
+    if dev.index != torch.cuda.current_device():
+        raise HmoeError(f"tensors on {dev}, which is not the current device")
+    return dev
+
+
+def make_router(p: dict, top_k: int = 1, renorm: bool = False) -> Router:
+    """p: the router's rows R [K, d], and bias [K] (fp32) or None."""
+    R, bias = p["R"], p.get("bias")
+    K, d = R.shape
+    prm = Router(K, d, top_k, _dt(R), 1 if renorm else 0, _arg(R, (K, d), R.dtype, "R"),
+                 _arg(bias, (K,), torch.float32, "bias"))
+    _same_device(R, bias)
+    return prm
+
+
+def _router(p, X, top_k, renorm):
+    prm = p if isinstance(p, Router) else make_router(p, top_k, renorm)
+    if _dt(X) != prm.dt:
+        raise HmoeError(f"X: dtype {X.dtype}, the router's expected")
+    return prm
+
+
+def router_workspace(p, n, top_k: int = 1) -> int:
+    """Of router_forward and router_backward."""
+    return lib().hmoe_router_workspace(ctypes.byref(p if isinstance(p, Router) else make_router(p, top_k)), n)
+
+
+def router_forward(p, X, top_k: int = 1, renorm: bool = False, out=None, ws=None):
+    """A learned router on a batch X [n, d] (include/hmoe_train.h): the top_k experts by R x + bias with their
+    weights, counts of choices and mean probabilities of the experts, and the balance and z losses.  p: a dict as in
+    make_router, or the Router made from one (whose top_k and renorm then count).  Returns expert int32 and weight
+    [n, top_k], scores [n, K], counts int32 and share [K], loss [2]."""
+    prm = _router(p, X, top_k, renorm)
+    n, k, K = X.shape[0], prm.top_k, prm.K
+    o = {} if out is None else out
+    dev, f32, i32 = X.device, torch.float32, torch.int32
+    x = _arg(X, (n, prm.d), X.dtype, "X")
+    expert, e = _out_arg(o, "expert", (n, k), i32, dev)
+    weight, wt = _out_arg(o, "weight", (n, k), f32, dev)
+    scores, s = _out_arg(o, "scores", (n, K), f32, dev)
+    counts, c = _out_arg(o, "counts", (K,), i32, dev)
+    share, sh = _out_arg(o, "share", (K,), f32, dev)
+    loss, lo = _out_arg(o, "loss", (2,), f32, dev)
+    _same_device(X, expert, weight, scores, counts, share, loss, ws)
+    ref = ctypes.byref(prm)
+    L = lib()
+    w, wb = _ws_arg(ws, lambda: L.hmoe_router_workspace(ref, n), dev)
+    rc = L.hmoe_router_forward(ref, n, x, e, wt, s, c, sh, lo, w, wb, _raw_stream(dev))
+    if rc:
+        _chk(rc, "router_forward")
+    return {"expert": expert, "weight": weight, "scores": scores, "counts": counts, "share": share, "loss": loss}
+
+
+def router_backward(p, X, f, g_weight=None, balance: float = 0.0, z: float = 0.0, renorm: bool = False, want_dX=True,
+                    want_router=True, out=None, ws=None):
+    """Gradients of sum(g_weight * weight) + balance loss[0] + z loss[1]: dX [n, d] in X's dtype, dR [K, d] and dbias
+    [K] (fp32).  f: what router_forward returned (its scores, expert and counts are used); renorm as there."""
+    expert = f["expert"]
+    k = expert.shape[1]
+    prm = _router(p, X, k, renorm)
+    n, K = X.shape[0], prm.K
+    o = {} if out is None else out
+    dev, f32, i32 = X.device, torch.float32, torch.int32
+    x, s = _arg(X, (n, prm.d), X.dtype, "X"), _arg(f["scores"], (n, K), f32, "scores")
+    e, c = _arg(expert, (n, prm.top_k), i32, "expert"), _arg(f["counts"], (K,), i32, "counts")
+    g = _arg(g_weight, (n, prm.top_k), f32, "g_weight")
+    dX = dR = db = gx = gr = gb = None
+    if want_dX:
+        dX, gx = _out_arg(o, "dX", (n, prm.d), X.dtype, dev)
+    if want_router:
+        dR, gr = _out_arg(o, "dR", (K, prm.d), f32, dev)
+        db, gb = _out_arg(o, "dbias", (K,), f32, dev)
+    _same_device(X, f["scores"], expert, f["counts"], g_weight, dX, dR, db, ws)
+    ref = ctypes.byref(prm)
+    L = lib()
+    w, wb = _ws_arg(ws, lambda: L.hmoe_router_workspace(ref, n), dev)
+    rc = L.hmoe_router_backward(ref, n, x, s, e, c, g, balance, z, gx, gr, gb, w, wb, _raw_stream(dev))
+    if rc:
+        _chk(rc, "router_backward")
+    return {"dX": dX, "dR": dR, "dbias": db}
+
+
+# ------------------------------------------------------------------ join with the residual stream
+
+def _join(t, y, gate, gamma_y, gamma_h, norm_y, scale, eps):
+    """(the parameters, y's and gate's pointers, whether y has one row a sample) for rows like t [n, d]."""
+    n, d = t.shape
+    dt = t.dtype
+    single = y is not None and y.dim() == 2
+    k = 0 if y is None else 1 if single else y.shape[1]
+    lead = (n,) if single else (n, k)
+    yp, gp = _arg(y, lead + (d,), dt, "y"), _arg(gate, lead, torch.float32, "gate")
+    return Join(d, k, _dt(t), 1 if norm_y else 0, scale, eps, _arg(gamma_y, (d,), dt, "gamma_y"),
+                _arg(gamma_h, (d,), dt, "gamma_h")), yp, gp, lead
+
+
+def join_forward(x, y=None, gate=None, gamma_y=None, gamma_h=None, norm_y: bool = True, scale: float = 1.0,
+                 eps: float = 1e-6, want_x=True, want_h=True, out=None):
+    """A layer's output joined with the residual stream, and the norm before the next layer:
+    x' = scale x + sum_j gate_j gamma_y N(y_j), h = gamma_h N(x') with N(t) = t / sqrt(mean t^2 + eps), or without
+    norm_y y_j itself.  x [n, d]; y [n, d], [n, k, d] (k rows a sample) or None; gate fp32 [n] or [n, k]; gains [d]
+    or None (ones).  Returns x (x') and h, None where not wanted; out["x"] may be x itself."""
+    n, d = x.shape
+    dev, dt = x.device, x.dtype
+    prm, yp, gp, _ = _join(x, y, gate, gamma_y, gamma_h, norm_y, scale, eps)
+    o = {} if out is None else out
+    new = h = np_ = hp = None
+    if want_x:
+        new, np_ = _out_arg(o, "x", (n, d), dt, dev)
+    if want_h:
+        h, hp = _out_arg(o, "h", (n, d), dt, dev)
+    xp = _arg(x, (n, d), dt, "x")
+    _same_device(x, y, gate, gamma_y, gamma_h, new, h)
+    rc = lib().hmoe_join_forward(ctypes.byref(prm), n, xp, yp, gp, np_, hp, _raw_stream(dev))
+    if rc:
+        _chk(rc, "join_forward")
+    return {"x": new, "h": h}
+
+
+def join_workspace(n, d, k, dtype) -> int:
+    """Of join_backward."""
+    return lib().hmoe_join_workspace(ctypes.byref(Join(d, k, _DT[dtype], 0, 1.0, 1.0, None, None)), n)
+
+
+def join_backward(x_out, y=None, gate=None, gamma_y=None, gamma_h=None, norm_y: bool = True, scale: float = 1.0,
+                  eps: float = 1e-6, dx_out=None, dh=None, want=("dx", "dy", "dgate", "dgamma_y", "dgamma_h"), out=None,
+                  ws=None):
+    """Gradients of join_forward from those of x' (dx_out) and h (dh), either of which may be None (zeros); x_out is
+    the forward's x'.  Returns dx [n, d], dy (y's shape), dgate (gate's), dgamma_y and dgamma_h [d] (fp32); those
+    that `want` does not name, of inputs that are None, or of h without dh, are None.  out["dx"] may be dx_out or dh,
+    out["dy"] may be y."""
+    n, d = x_out.shape
+    dev, dt, f32 = x_out.device, x_out.dtype, torch.float32
+    prm, yp, gp, lead = _join(x_out, y, gate, gamma_y, gamma_h, norm_y, scale, eps)
+    o = {} if out is None else out
+    r = dict.fromkeys(("dx", "dy", "dgate", "dgamma_y", "dgamma_h"))
+    p = dict(r)
+    shapes = {"dx": ((n, d), dt, True), "dy": (lead + (d,), dt, y is not None),
+              "dgate": (lead, f32, gate is not None and y is not None),
+              "dgamma_y": ((d,), f32, gamma_y is not None and y is not None),
+              "dgamma_h": ((d,), f32, gamma_h is not None and dh is not None)}
+    for key in want:
+        shape, kind, there = shapes[key]
+        if there:
+            r[key], p[key] = _out_arg(o, key, shape, kind, dev)
+    xp, dxo, dhp = _arg(x_out, (n, d), dt, "x_out"), _arg(dx_out, (n, d), dt, "dx_out"), _arg(dh, (n, d), dt, "dh")
+    _same_device(x_out, y, gate, gamma_y, gamma_h, dx_out, dh, ws, *r.values())
+    L = lib()
+    ref = ctypes.byref(prm)
+    w, wb = _ws_arg(ws, lambda: L.hmoe_join_workspace(ref, n), dev)
+    rc = L.hmoe_join_backward(ref, n, xp, yp, gp, dxo, dhp, p["dx"], p["dy"], p["dgate"], p["dgamma_y"], p["dgamma_h"], w,
+                              wb, _raw_stream(dev))
+    if rc:
+        _chk(rc, "join_backward")
+    return r
+
+
 # ------------------------------------------------------------------ parameter update
+
+def _matrices(t):
+    """(K, rows, cols) of one matrix or a stack of them."""
+    if t.dim() not in (2, 3):
+        raise HmoeError(f"shape {tuple(t.shape)}: a matrix or a stack of them expected")
+    return (1, *t.shape) if t.dim() == 2 else tuple(t.shape)
+
+
+def _coef(coef):
+    a, b, c = coef
+    return (ctypes.c_float * 3)(a, b, c)
+
+
+def orthogonalise_workspace(K, rows, cols, dtype) -> int:
+    return lib().hmoe_orthogonalise_workspace(K, rows, cols, _DT[dtype])
+
+
+def orthogonalise(G, steps: int = 5, coef=COEF, out=None, ws=None):
+    """`steps` Newton-Schulz iterations X <- a X + (b A + c A^2) X, A = X X^T, from X = G / |G| for each matrix of
+    G [K, rows, cols] or [rows, cols]: near its orthogonal factor with the default coefficients.  out may be G."""
+    K, rows, cols = _matrices(G)
+    dev, dt = G.device, _dt(G)
+    if out is None:
+        out = torch.empty_like(G)
+    g, o = _arg(G, tuple(G.shape), G.dtype, "G"), _arg(out, tuple(G.shape), G.dtype, "out")
+    _same_device(G, out, ws)
+    L = lib()
+    w, wb = _ws_arg(ws, lambda: L.hmoe_orthogonalise_workspace(K, rows, cols, dt), dev)
+    rc = L.hmoe_orthogonalise(g, dt, K, rows, cols, steps, _coef(coef), o, w, wb, _raw_stream(dev))
+    if rc:
+        _chk(rc, "orthogonalise")
+    return out
+
+
+def muon_workspace(K, rows, cols) -> int:
+    return lib().hmoe_muon_workspace(K, rows, cols)
+
+
+def muon_step(w, g, v=None, lr: float = 0.02, weight_decay: float = 0.0, momentum: float = 0.95, nesterov: bool = True,
+              scale: float = 1.0, steps: int = 5, coef=COEF, w_lo=None, ws=None):
+    """One step in place on fp32 weight matrices w [K, rows, cols] or [rows, cols] from their gradients g, beside
+    sgd_step: v = momentum v + g, w = (1 - lr weight_decay) w - lr scale NS(g + momentum v, or v without nesterov),
+    NS as in orthogonalise.  v is needed with momentum.  w_lo, if given, receives the updated weights in its dtype."""
+    K, rows, cols = _matrices(w)
+    shape, f32, dev = tuple(w.shape), torch.float32, w.device
+    wp, gp, vp = _arg(w, shape, f32, "w"), _arg(g, shape, f32, "g"), _arg(v, shape, f32, "v")
+    dt = 1 if w_lo is None else _dt(w_lo)
+    lo = None if w_lo is None else _arg(w_lo, shape, w_lo.dtype, "w_lo")
+    _same_device(w, g, v, w_lo, ws)
+    L = lib()
+    space, wb = _ws_arg(ws, lambda: L.hmoe_muon_workspace(K, rows, cols), dev)
+    rc = L.hmoe_muon_step(wp, gp, vp, lo, dt, K, rows, cols, lr, weight_decay, momentum, 1 if nesterov else 0, scale,
+                          steps, _coef(coef), space, wb, _raw_stream(dev))
+    if rc:
+        _chk(rc, "muon_step")
+    return w
+
 
 def sgd_step(w, g, lr: float, weight_decay: float = 0.0, momentum: float = 0.0, v=None, w_lo=None):
     """One SGD step in place on the fp32 master weights w (Section 4.2); v is the momentum
