@@ -93,6 +93,23 @@ def test_low_rank(rank):
     assert off(np64(hmoe.orthogonalise(G)), ref) <= tol(rank)
 
 
+@pytest.mark.parametrize("K,rows,cols", [(2, 72, 96), (1, 200, 1504), (3, 900, 136)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_numbers_of_steps(K, rows, cols, dtype):
+    """bf16: the last step, but where it is the first, takes fp16 numbers alone: eight roundings of 2^-11 of 1 or more
+    that no later step amplifies, relative to a result of norm sqrt(q) at most 8 2^-11 |X| |a| / sqrt(q) with |X| <= sqrt(q)
+    as the steps leave it, and the result's own 2^-8."""
+    G = rand(K, rows, cols, seed=9).to(dtype)
+    for steps in range(1, 8):
+        O = hmoe.orthogonalise(G, steps=steps)
+        for k in range(K):
+            ref = iterate64(np64(G[k]), steps)
+            most = tol(min(rows, cols), steps)
+            if dtype == torch.bfloat16:
+                most += 2.0 ** -8 + (8 * 2.0 ** -11 * COEF[0] if steps > 1 else 0)
+            assert off(np64(O[k]), ref) <= most, (steps, k)
+
+
 def test_sizes_of_entries():
     """The norm is taken in 64 bits: matrices of very small and very large entries have the same result."""
     G = rand(64, 96)
