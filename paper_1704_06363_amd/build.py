@@ -17,7 +17,7 @@ SRC = os.path.join(PKG, "csrc")
 OUT = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libhmoe.so")
 SOURCES = ["api.hip", "dispatch.hip", "join.hip", "kmeans.hip", "lm_api.hip", "logprob.hip", "lora.hip", "metrics.hip",
-           "moe.hip", "moe_few.hip", "optim.hip", "ortho.hip", "pca.hip", "router.hip", "train_api.hip"]
+           "moe.hip", "moe_few.hip", "optim.hip", "ortho.hip", "ortho_small.hip", "pca.hip", "router.hip", "train_api.hip"]
 ARCH = "gfx950"
 
 # Packed fp32 instructions are kept out of the generated code (hipcc's host pass warns that it

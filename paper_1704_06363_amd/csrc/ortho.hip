@@ -16,43 +16,13 @@
 // so that entries up to 8, 16 and 256 fit and the smallest lo, 2^-25, is 2^-38 of X -- 2^-25 of the mean entry of
 // a matrix of 8192 x 8192.
 #include "gemm.hpp"
-#include "primitives.hpp"
+#include "ortho.hpp"
 #include "slices.hpp"
-#include "train_launch.hpp"
 
 namespace hmoe {
 
 namespace {
 
-typedef _Float16 f16;
-typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
-
-constexpr float kScaleX = 0x1p13f, kScaleA = 0x1p12f, kScaleQ = 0x1p8f;
-
-// The problem as the iterations see it.
-struct Ortho {
-  int K, rows, cols;
-  int r, l;    // r <= l, X [r][l]
-  int rp, lp;  // rounded up to 32
-  bool tall;   // rows > cols: X is U^T
-  int blocks;  // of a matrix's sum of squares
-  __host__ __device__ int64_t x_size() const { return (int64_t)rp * 2 * lp; }  // of a matrix, in fp16 numbers
-  __host__ __device__ int64_t a_size() const { return (int64_t)r * 2 * rp; }
-};
-Ortho ortho_of(int K, int rows, int cols) {
-  Ortho o;
-  o.K = K;
-  o.rows = rows;
-  o.cols = cols;
-  o.tall = rows > cols;
-  o.r = o.tall ? cols : rows;
-  o.l = o.tall ? rows : cols;
-  o.rp = (o.r + 31) / 32 * 32;
-  o.lp = (o.l + 31) / 32 * 32;
-  const int64_t want = cdiv((int64_t)rows * cols, 256 * 32), most = cdiv(4 * (int64_t)device_cus(), K);
-  o.blocks = (int)(want < most ? want : most);
-  return o;
-}
 struct OrthoSpace {
   f16 *X[2], *A[3];
   double* part;   // [K][blocks]
@@ -69,25 +39,6 @@ OrthoSpace ortho_carve(const Ortho& o, size_t pieces, Workspace& ws) {
 
 // ------------------------------------------------------------------ the start
 
-// Four entries of U from `at` on.
-__device__ __forceinline__ floatx4 ortho_u(const OrthoStep& s, int64_t at) {
-  if (s.G) {
-    if (s.dt == HMOE_BF16) {
-      const bf16x4 v = *reinterpret_cast<const bf16x4*>(static_cast<const bf16*>(s.G) + at);
-      return floatx4{(float)v[0], (float)v[1], (float)v[2], (float)v[3]};
-    }
-    return *reinterpret_cast<const floatx4*>(static_cast<const float*>(s.G) + at);
-  }
-  const floatx4 g = *reinterpret_cast<const floatx4*>(s.g + at);
-  if (!s.v) return g;
-  const floatx4 v = *reinterpret_cast<const floatx4*>(s.v + at);
-  if (!s.nesterov) return v;
-  floatx4 u;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) u[e] = fmaf(s.momentum, v[e], g[e]);
-  return u;
-}
-
 // v = momentum v + g, and the sums of squares of U, in fp64 (entries of 1e-30 and of 1e30 have squares there), of
 // blockIdx.x's part of matrix m0 + blockIdx.y.
 __global__ void __launch_bounds__(256) k_ortho_start(OrthoStep s, Ortho o, int m0, double* __restrict__ part) {
@@ -96,13 +47,7 @@ __global__ void __launch_bounds__(256) k_ortho_start(OrthoStep s, Ortho o, int m
   const int64_t size = (int64_t)o.rows * o.cols, base = m * size;
   double sum = 0.0;
   for (int64_t q = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; q < size; q += (int64_t)gridDim.x * 1024) {
-    if (!s.G && s.v) {
-      const floatx4 g = *reinterpret_cast<const floatx4*>(s.g + base + q);
-      floatx4 v = *reinterpret_cast<const floatx4*>(s.v + base + q);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = fmaf(s.momentum, v[e], g[e]);
-      *reinterpret_cast<floatx4*>(s.v + base + q) = v;
-    }
+    ortho_momentum(s, base + q);
     const floatx4 u = ortho_u(s, base + q);
 #pragma unroll
     for (int e = 0; e < 4; ++e) sum = fma((double)u[e], (double)u[e], sum);
@@ -111,12 +56,6 @@ __global__ void __launch_bounds__(256) k_ortho_start(OrthoStep s, Ortho o, int m
   if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = sum;
   __syncthreads();
   if (threadIdx.x == 0) part[(int64_t)m * o.blocks + blockIdx.x] = (sh[0] + sh[1]) + (sh[2] + sh[3]);
-}
-
-__device__ __forceinline__ void pair_of(float v, f16& hi, f16& lo) {
-  hi = (f16)v;
-  // of what fp16 holds no more, as an infinity; a lo of NaN beside it would be NaN too
-  lo = (f16)(v - (float)hi);
 }
 
 // X = U / |U| in pairs, 64 x 64 entries to a workgroup, zeros where X is padded.
@@ -193,27 +132,6 @@ __device__ __forceinline__ void get4(const f16* row, int c, float (&v)[4]) {
   if constexpr (PAIR) lo = *reinterpret_cast<const f16x4*>(row + pair_at(c) + kPairLo);
 #pragma unroll
   for (int e = 0; e < 4; ++e) v[e] = (float)hi[e] + (float)lo[e];
-}
-
-// 4 x 4 values of the lanes 4 q .. 4 q + 3 transposed: lane 4 q + s gets element s of each.
-__device__ __forceinline__ void quad_transpose(float (&v)[4]) {
-  const int s = threadIdx.x & 3;
-  // lanes a distance of 1 apart trade their odd and even elements, then those 2 apart halves
-  float x[4];
-#pragma unroll
-  for (int p = 0; p < 2; ++p) {
-    const float give = (s & 1) ? v[2 * p] : v[2 * p + 1];
-    const float got = dpp<0xB1>(give);
-    x[2 * p] = (s & 1) ? got : v[2 * p];
-    x[2 * p + 1] = (s & 1) ? v[2 * p + 1] : got;
-  }
-#pragma unroll
-  for (int p = 0; p < 2; ++p) {
-    const float give = (s & 2) ? x[p] : x[p + 2];
-    const float got = dpp<0x4E>(give);
-    v[p] = (s & 2) ? got : x[p];
-    v[p + 2] = (s & 2) ? x[p + 2] : got;
-  }
 }
 
 // Tile `b` of those on and above the diagonal, column by column.
@@ -303,39 +221,11 @@ __device__ __forceinline__ void product_out(const Ortho& o, const Product& p, co
     if (row >= o.r || col >= o.l) return;
     const int64_t base = (int64_t)t.m * o.rows * o.cols;
     if (!o.tall) {  // l = cols, a multiple of 8
-      const int64_t at = base + (int64_t)row * o.cols + col;
-      if (s.G) {
-        if (s.dt == HMOE_BF16)
-          *reinterpret_cast<bf16x4*>(static_cast<bf16*>(s.O) + at) = bf16x4{(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3]};
-        else
-          *reinterpret_cast<floatx4*>(static_cast<float*>(s.O) + at) = floatx4{v[0], v[1], v[2], v[3]};
-        return;
-      }
-      floatx4 w = *reinterpret_cast<const floatx4*>(s.w + at);
+      ortho_put4(s, base + (int64_t)row * o.cols + col, v);
+    } else {  // X^T: the lanes of a row hold consecutive entries
 #pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] = fmaf(-s.rate, v[e], s.keep * w[e]);
-      *reinterpret_cast<floatx4*>(s.w + at) = w;
-      if (!s.w_lo) return;
-      if (s.dt == HMOE_BF16)
-        *reinterpret_cast<bf16x4*>(static_cast<bf16*>(s.w_lo) + at) = bf16x4{(bf16)w[0], (bf16)w[1], (bf16)w[2], (bf16)w[3]};
-      else
-        *reinterpret_cast<floatx4*>(static_cast<float*>(s.w_lo) + at) = w;
-      return;
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {  // X^T: the lanes of a row hold consecutive entries
-      if (col + e >= o.l) continue;
-      const int64_t at = base + (int64_t)(col + e) * o.cols + row;
-      if (s.G) {
-        if (s.dt == HMOE_BF16) static_cast<bf16*>(s.O)[at] = (bf16)v[e];
-        else static_cast<float*>(s.O)[at] = v[e];
-        continue;
-      }
-      const float w = fmaf(-s.rate, v[e], s.keep * s.w[at]);
-      s.w[at] = w;
-      if (!s.w_lo) continue;
-      if (s.dt == HMOE_BF16) static_cast<bf16*>(s.w_lo)[at] = (bf16)w;
-      else static_cast<float*>(s.w_lo)[at] = w;
+      for (int e = 0; e < 4; ++e)
+        if (col + e < o.l) ortho_put(s, base + (int64_t)(col + e) * o.cols + row, v[e]);
     }
   }
 }
@@ -532,9 +422,17 @@ struct Iterations {
 
 }  // namespace
 
+int launch_ortho_start(const OrthoStep& s, const Ortho& o, double* part, hipStream_t st) {
+  return over_slices(o.K, o.blocks, 256, [&](int64_t m0, int64_t count) {
+    HMOE_LAUNCH("ortho start", k_ortho_start, dim3(o.blocks, (unsigned)count), dim3(256), 0, st, s, o, (int)m0, part);
+    return (int)HMOE_OK;
+  });
+}
+
 size_t ortho_ws(int32_t K, int32_t rows, int32_t cols) {
   Workspace w(nullptr, 0);
   const Ortho o = ortho_of(K, rows, cols);
+  if (small_ortho_ws(o) > 0) return small_ortho_ws(o);
   ortho_carve(o, part_size(o), w);
   return w.off;
 }
@@ -542,11 +440,9 @@ size_t ortho_ws(int32_t K, int32_t rows, int32_t cols) {
 int launch_ortho(const OrthoStep& s, int32_t K, int32_t rows, int32_t cols, int32_t steps, const float* coef,
                  Workspace& ws, hipStream_t st) {
   const Ortho o = ortho_of(K, rows, cols);
+  if (small_ortho_ws(o) > 0) return launch_small_ortho(s, o, steps, coef, ws, st);
   const OrthoSpace w = ortho_carve(o, part_size(o), ws);
-  HMOE_TRY(over_slices(K, o.blocks, 256, [&](int64_t m0, int64_t count) {
-    HMOE_LAUNCH("ortho start", k_ortho_start, dim3(o.blocks, (unsigned)count), dim3(256), 0, st, s, o, (int)m0, w.part);
-    return (int)HMOE_OK;
-  }));
+  HMOE_TRY(launch_ortho_start(s, o, w.part, st));
   const bool low = s.G && s.dt == HMOE_BF16, single_first = low && steps == 1;
   const int64_t parts = cdiv(o.rp, 64) * cdiv(o.lp, 64);
   HMOE_TRY(over_slices(K, parts, 256, [&](int64_t m0, int64_t count) {

@@ -42,7 +42,10 @@ def rand(*shape, seed=0):
 
 
 SHAPES = [(1, 1, 8), (3, 8, 8), (2, 5, 40), (2, 33, 32), (1, 64, 64), (2, 100, 328), (1, 129, 128), (2, 130, 264),
-          (1, 257, 200), (3, 1000, 64), (1, 40, 3000), (1, 300, 304), (1, 520, 1032), (1, 777, 512), (40, 64, 128)]
+          (1, 257, 200), (3, 1000, 64), (1, 40, 3000), (1, 300, 304), (1, 520, 1032), (1, 777, 512), (40, 64, 128),
+          # short sides of up to 32, 64 and 128, one workgroup's columns and several's
+          (9, 16, 16), (2, 31, 136), (3, 17, 704), (2, 32, 776), (1, 30, 5000), (2, 5000, 24), (1, 9, 49160), (2, 64, 384),
+          (3, 60, 392), (1, 3000, 56), (1, 64, 6152), (2, 128, 128), (2, 120, 136), (1, 128, 2056), (2, 900, 128), (1, 65, 1024)]
 
 
 @pytest.mark.parametrize("K,rows,cols", SHAPES)
