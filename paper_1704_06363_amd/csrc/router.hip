@@ -5,9 +5,9 @@
 //
 // Bound by HBM: X is read for the scores and for dR, and dX written; the scores (K values a row) lie
 // between.  The products are narrow (K columns, or a reduction over K).  ds is fp32 and keeps its accuracy on
-// the matrix cores: with bf16 data a value is kept as three bf16 numbers that add up to it, in blocks of 16
-// experts -- 16 values, their remainders, and the remainders of those.  The two steps of a block's first 32
-// against 16 experts of R taken twice give dX to 2^-16, rounded to bf16 once; dR takes all three.
+// the matrix cores: with bf16 data a value is kept as three bf16 numbers that add up to it, a row's in three planes,
+// [values, their remainders, the remainders of those][experts, padded to 16].  The first two against R taken twice
+// give dX to 2^-16, rounded to bf16 once; dR takes all three.
 #include "fewrows.hpp"
 #include "gemm.hpp"
 #include "primitives.hpp"
@@ -26,7 +26,8 @@ __host__ __device__ inline int ds_width(int K) {
 
 // ------------------------------------------------------------------ scores
 
-// scores [n][K] = X R^T + bias on the ring engine's narrow tiles.
+// scores [n][K] = X R^T + bias on the ring engine's narrow tiles; of several pieces of the reduction (gridDim.y) each
+// its part in a plane of `scores`, without the bias.
 template <class C>
 __global__ void __launch_bounds__(C::THREADS)
     k_router_scores(const typename C::type* __restrict__ X, const typename C::type* __restrict__ R,
@@ -37,35 +38,60 @@ __global__ void __launch_bounds__(C::THREADS)
   const int64_t m0 = (int64_t)(blockIdx.x / nt) * C::BM;
   const int n0 = (int)(blockIdx.x % nt) * C::BN;
   const int rows = n - m0 < C::BM ? (int)(n - m0) : C::BM, cols = K - n0 < C::BN ? K - n0 : C::BN;
+  const int units = (d + 63) / 64, s = blockIdx.y, pieces = gridDim.y;
+  const int k0 = (int)((int64_t)units * s / pieces) * 64, to = (int)((int64_t)units * (s + 1) / pieces) * 64;
   floatx4 acc[C::MI][C::NJ];
-  gemm_tile<C, true, true>(X + m0 * d, d, rows, R + (int64_t)n0 * d, d, cols, d, smem, acc);
+  gemm_tile<C, true, true>(X + m0 * d + k0, d, rows, R + (int64_t)n0 * d + k0, d, cols, (to < d ? to : d) - k0, smem, acc);
+  static_assert(C::TRANS, "four consecutive scores to a lane");
   const Frag<C> f;
+  float* out = scores + ((int64_t)s * n + m0) * K + n0;
+  const bool vec = K % 4 == 0;
 #pragma unroll
-  for (int i = 0; i < C::MI; ++i)
+  for (int j = 0; j < C::NJ; ++j) {
+    const int col = f.col(j, 0);
+    float b[4];
 #pragma unroll
-    for (int j = 0; j < C::NJ; ++j)
+    for (int r = 0; r < 4; ++r) b[r] = bias && pieces == 1 && col + r < cols ? bias[n0 + col + r] : 0.f;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int row = f.row(i, r), col = f.col(j, r);
-        if (row < rows && col < cols) scores[(m0 + row) * K + n0 + col] = acc[i][j][r] + (bias ? bias[n0 + col] : 0.f);
+    for (int i = 0; i < C::MI; ++i) {
+      const int row = f.row(i, 0);
+      if (row >= rows || col >= cols) continue;
+      float* to = out + (int64_t)row * K + col;
+      if (vec) {
+        *reinterpret_cast<floatx4*>(to) = acc[i][j] + floatx4{b[0], b[1], b[2], b[3]};
+      } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (col + r < cols) to[r] = acc[i][j][r] + b[r];
       }
+    }
+  }
 }
 
 // ------------------------------------------------------------------ choices
 
-// The largest of a key over L lanes, and sums, in each of them.
-template <int L>
-__device__ __forceinline__ uint64_t lanes_max(uint64_t k) {
-  const auto step = [&](uint64_t o) { k = o > k ? o : k; };
-  step(lane_xor<1>(k));
-  step(lane_xor<2>(k));
-  step(lane_xor<4>(k));
-  step(lane_xor<8>(k));
+// `op` over L lanes, and sums, in each of them.
+template <int L, class Op>
+__device__ __forceinline__ uint32_t lanes_reduce(uint32_t k, Op op) {
   if constexpr (L > 16) {
-    step(lane_xor<16>(k));
-    step(lane_xor<32>(k));
+    k = op(k, lane_xor<32>(k));
+    k = op(k, lane_xor<16>(k));
   }
-  return k;
+  const auto turned = [&](auto ctrl) {  // within the rows of 16 lanes, whose values repeat with the distance then
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)k, decltype(ctrl)::value, 0xf, 0xf, true);
+  };
+  k = op(k, turned(std::integral_constant<int, 0x128>{}));
+  k = op(k, turned(std::integral_constant<int, 0x124>{}));
+  k = op(k, turned(std::integral_constant<int, 0x122>{}));
+  return op(k, turned(std::integral_constant<int, 0x121>{}));
+}
+template <int L>
+__device__ __forceinline__ uint32_t lanes_max(uint32_t k) {
+  return lanes_reduce<L>(k, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+}
+template <int L>
+__device__ __forceinline__ uint32_t lanes_min(uint32_t k) {
+  return lanes_reduce<L>(k, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
 }
 template <int L>
 __device__ __forceinline__ float lanes_sum(float v) {
@@ -76,30 +102,36 @@ __device__ __forceinline__ float lanes_sum(float v) {
 __device__ __forceinline__ float row_exp(float s, float mx) { return s == -INFINITY ? 0.f : expf(s - mx); }
 
 // A workgroup's sums over its row groups of L lanes: acc[p] of expert p L + lane.
-template <int L, int P, typename V>
+template <int L, int P, int THREADS, typename V>
 __device__ __forceinline__ void experts_out(const V (&acc)[P], V* sh, int K, V* __restrict__ to) {
-  constexpr int G = 256 / L, KP = P * L;
+  constexpr int G = THREADS / L, KP = P * L;
   const int g = threadIdx.x / L, lane = threadIdx.x % L;
 #pragma unroll
   for (int p = 0; p < P; ++p) sh[g * KP + p * L + lane] = acc[p];
   __syncthreads();
-  for (int e = threadIdx.x; e < K; e += 256) {
+  for (int e = threadIdx.x; e < K; e += THREADS) {
     V v = sh[e];
+#pragma unroll 4
     for (int i = 1; i < G; ++i) v += sh[i * KP + e];
     to[e] = v;
   }
   __syncthreads();
 }
 
-// L lanes to a row, P scores to a lane.  A workgroup's counts, probabilities' sums and sum of squared lse go to
+// Threads of the kernels that take a row at a time, with P scores to each of L lanes: as many as registers allow.
+template <int P>
+constexpr int kRowThreads = P <= 4 ? 1024 : P <= 8 ? 512 : 256;
+
+// L lanes to a row, P scores to a lane.  With `planes` the scores are their sum and the bias, and are written, too.
+// A workgroup's counts, probabilities' sums and sum of squared lse go to
 // its row of the parts.
 template <int L, int P>
-__global__ void __launch_bounds__(256)
-    k_router_choose(const float* __restrict__ scores, int64_t n, int K, int top, int renorm, int32_t* __restrict__ expert,
-                    float* __restrict__ weight, float* __restrict__ share_part, int32_t* __restrict__ count_part,
-                    double* __restrict__ z_part) {
-  constexpr int G = 256 / L;
-  __shared__ double s_z[4];
+__global__ void __launch_bounds__(kRowThreads<P>)
+    k_router_choose(float* __restrict__ scores, const float* __restrict__ planes, int pieces, const float* __restrict__ bias,
+                    int64_t n, int K, int top, int renorm, int32_t* __restrict__ expert, float* __restrict__ weight,
+                    float* __restrict__ share_part, int32_t* __restrict__ count_part, double* __restrict__ z_part) {
+  constexpr int THREADS = kRowThreads<P>, G = THREADS / L;
+  __shared__ double s_z[THREADS / 64];
   extern __shared__ __attribute__((aligned(16))) char smem_raw[];
   const int lane = threadIdx.x % L;
   float share[P];
@@ -111,30 +143,45 @@ __global__ void __launch_bounds__(256)
     const int64_t row = first + threadIdx.x / L;
     const bool live = row < n;
     float s[P];
+    if (planes) {
 #pragma unroll
-    for (int p = 0; p < P; ++p) s[p] = live && p * L + lane < K ? scores[row * K + p * L + lane] : -INFINITY;
-    uint64_t taken = 0;
+      for (int p = 0; p < P; ++p) {
+        const bool in = live && p * L + lane < K;
+        s[p] = in ? 0.f : -INFINITY;
+        if (!in) continue;
+        const float* from = planes + row * K + p * L + lane;
+#pragma unroll 4
+        for (int z = 0; z < pieces; ++z) s[p] += from[(int64_t)z * n * K];
+        if (bias) s[p] += bias[p * L + lane];
+        scores[row * K + p * L + lane] = s[p];
+      }
+    } else {
+#pragma unroll
+      for (int p = 0; p < P; ++p) s[p] = live && p * L + lane < K ? scores[row * K + p * L + lane] : -INFINITY;
+    }
+    uint32_t key[P];  // 0: no entry, or taken; 1: NaN
+#pragma unroll
+    for (int p = 0; p < P; ++p) key[p] = p * L + lane < K ? sortable(s[p]) + 1 : 0;
     float chosen[HMOE_ROUTER_EXPERTS];
     int index[HMOE_ROUTER_EXPERTS];
 #pragma unroll
     for (int j = 0; j < HMOE_ROUTER_EXPERTS; ++j) {
       if (j >= top) break;
-      uint64_t best = 0;
+      uint32_t best = key[0], at = ~0u;
+#pragma unroll
+      for (int p = 1; p < P; ++p) best = key[p] > best ? key[p] : best;
+      best = lanes_max<L>(best);
+#pragma unroll
+      for (int p = P - 1; p >= 0; --p) at = key[p] == best ? p * L + lane : at;
+      at = lanes_min<L>(at);
+      index[j] = (int)at;
+      const uint32_t u = best - 1;
+      chosen[j] = u == 0 ? NAN : __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u);
 #pragma unroll
       for (int p = 0; p < P; ++p) {
-        const uint64_t k = p * L + lane < K && !((taken >> p) & 1) ? rank_key(s[p], p * L + lane) : 0;
-        best = k > best ? k : best;
-      }
-      best = lanes_max<L>(best);
-      const int e = (int)key_index(best);
-      index[j] = e;
-      chosen[j] = (uint32_t)(best >> 32) == 0 ? NAN : key_value(best);
-      if (e % L == lane) {
-        taken |= uint64_t(1) << (e / L);
-        if (live && chosen[j] > -INFINITY) {
-#pragma unroll
-          for (int p = 0; p < P; ++p) count[p] += p == e / L;
-        }
+        const bool mine = at == (uint32_t)(p * L + lane);
+        key[p] = mine ? 0 : key[p];
+        count[p] += mine && live && chosen[j] > -INFINITY;
       }
     }
     const float mx = chosen[0];  // NaN only where all are
@@ -172,12 +219,15 @@ __global__ void __launch_bounds__(256)
       for (int p = 0; p < P; ++p) share[p] = fmaf(p_e[p], inv, share[p]);
     }
   }
-  experts_out<L, P>(share, reinterpret_cast<float*>(smem_raw), K, share_part + (int64_t)blockIdx.x * K);
-  experts_out<L, P>(count, reinterpret_cast<int32_t*>(smem_raw), K, count_part + (int64_t)blockIdx.x * K);
+  experts_out<L, P, THREADS>(share, reinterpret_cast<float*>(smem_raw), K, share_part + (int64_t)blockIdx.x * K);
+  experts_out<L, P, THREADS>(count, reinterpret_cast<int32_t*>(smem_raw), K, count_part + (int64_t)blockIdx.x * K);
   z = wave_sum(z);
   if ((threadIdx.x & 63) == 0) s_z[threadIdx.x >> 6] = z;
   __syncthreads();
-  if (threadIdx.x == 0) z_part[blockIdx.x] = (s_z[0] + s_z[1]) + (s_z[2] + s_z[3]);
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < THREADS / 64; ++i) z += s_z[i];
+    z_part[blockIdx.x] = z;
+  }
 }
 
 // The parts added in order: a wave to 64 experts at a time, and the losses.  One workgroup.
@@ -232,14 +282,42 @@ __global__ void __launch_bounds__(1024)
 
 // ------------------------------------------------------------------ the scores' gradient
 
-// ds in parts (ds_width) and a workgroup's sums of it.
+// Rt [d][copies][padded K] = R [K][d], zeros past K.
+template <typename T>
+struct Transposed {
+  const T* R;
+  T* Rt;
+  int d, copies;  // copies 0: not wanted
+};
+// 64 columns of 16 experts to a workgroup.
+template <typename T, int THREADS>
+__device__ __forceinline__ void router_transpose(const Transposed<T>& t, int K, int block) {
+  __shared__ T s[16][65];
+  const int kp = padded(K), d = t.d, c0 = block / (kp / 16) * 64, e0 = block % (kp / 16) * 16;
+  for (int q = threadIdx.x; q < 16 * 64; q += THREADS) {
+    const int e = q / 64, c = q % 64;
+    s[e][c] = e0 + e < K && c0 + c < d ? t.R[(int64_t)(e0 + e) * d + c0 + c] : from_f32<T>(0.f);
+  }
+  __syncthreads();
+  for (int q = threadIdx.x; q < 16 * 64; q += THREADS) {
+    const int c = q / 16, e = q % 16;
+    if (c0 + c < d)
+      for (int i = 0; i < t.copies; ++i) t.Rt[((int64_t)(c0 + c) * t.copies + i) * kp + e0 + e] = s[e][c];
+  }
+}
+
+// ds in parts (ds_width) and a workgroup's sums of it; workgroups past `blocks` transpose R.
 template <typename T, int L, int P>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(kRowThreads<P>)
     k_router_ds(const float* __restrict__ scores, const int32_t* __restrict__ expert, const int32_t* __restrict__ counts,
                 const float* __restrict__ g_weight, int64_t n, int K, int top, int renorm, double balance, float z2,
-                T* __restrict__ ds, float* __restrict__ bias_part) {
-  constexpr int G = 256 / L;
+                T* __restrict__ ds, float* __restrict__ bias_part, int blocks, Transposed<T> t) {
+  constexpr int THREADS = kRowThreads<P>, G = THREADS / L;
   extern __shared__ __attribute__((aligned(16))) char smem_raw[];
+  if ((int)blockIdx.x >= blocks) {
+    router_transpose<T, THREADS>(t, K, blockIdx.x - blocks);
+    return;
+  }
   const int lane = threadIdx.x % L, ld = ds_width<T>(K), kp = padded(K);
   float q[P], sum[P];
 #pragma unroll
@@ -247,7 +325,7 @@ __global__ void __launch_bounds__(256)
     q[p] = p * L + lane < K ? (float)(balance * counts[p * L + lane]) : 0.f;
     sum[p] = 0.f;
   }
-  for (int64_t first = (int64_t)blockIdx.x * G; first < n; first += (int64_t)gridDim.x * G) {
+  for (int64_t first = (int64_t)blockIdx.x * G; first < n; first += (int64_t)blocks * G) {
     const int64_t row = first + threadIdx.x / L;
     const bool live = row < n;
     float s[P], mx = -INFINITY;
@@ -256,14 +334,9 @@ __global__ void __launch_bounds__(256)
       s[p] = live && p * L + lane < K ? scores[row * K + p * L + lane] : -INFINITY;
       mx = fmaxf(mx, s[p]);
     }
-    mx = fmaxf(mx, __uint_as_float(lane_xor<1>(__float_as_uint(mx))));
-    mx = fmaxf(mx, __uint_as_float(lane_xor<2>(__float_as_uint(mx))));
-    mx = fmaxf(mx, __uint_as_float(lane_xor<4>(__float_as_uint(mx))));
-    mx = fmaxf(mx, __uint_as_float(lane_xor<8>(__float_as_uint(mx))));
-    if constexpr (L > 16) {
-      mx = fmaxf(mx, __uint_as_float(lane_xor<16>(__float_as_uint(mx))));
-      mx = fmaxf(mx, __uint_as_float(lane_xor<32>(__float_as_uint(mx))));
-    }
+    mx = __uint_as_float(lanes_reduce<L>(__float_as_uint(mx), [](uint32_t a, uint32_t b) {
+      return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+    }));
     float pe[P], g[P], on[P], tot = 0.f;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
@@ -317,32 +390,16 @@ __global__ void __launch_bounds__(256)
       if (live && e < kp) {
         if constexpr (sizeof(T) == 2) {
           const Parts<T, kParts> parts(v);
-          T* to = ds + row * ld + e / 16 * (16 * kParts) + e % 16;
+          T* to = ds + row * ld + e;
 #pragma unroll
-          for (int i = 0; i < kParts; ++i) to[16 * i] = parts.part[i];
+          for (int i = 0; i < kParts; ++i) to[i * kp] = parts.part[i];
         } else {
           ds[row * ld + e] = v;
         }
       }
     }
   }
-  experts_out<L, P>(sum, reinterpret_cast<float*>(smem_raw), K, bias_part + (int64_t)blockIdx.x * K);
-}
-
-// Rt [d][padded K] = R [K][d], zeros past K.
-template <typename T>
-__global__ void __launch_bounds__(256) k_router_transpose(const T* __restrict__ R, int K, int d, T* __restrict__ Rt) {
-  __shared__ T s[16][65];
-  const int c0 = blockIdx.x * 64, e0 = blockIdx.y * 16, kp = padded(K);
-  for (int q = threadIdx.x; q < 16 * 64; q += 256) {
-    const int e = q / 64, c = q % 64;
-    s[e][c] = e0 + e < K && c0 + c < d ? R[(int64_t)(e0 + e) * d + c0 + c] : from_f32<T>(0.f);
-  }
-  __syncthreads();
-  for (int q = threadIdx.x; q < 16 * 64; q += 256) {
-    const int c = q / 16, e = q % 16;
-    if (c0 + c < d) Rt[(int64_t)(c0 + c) * kp + e0 + e] = s[e][c];
-  }
+  experts_out<L, P, THREADS>(sum, reinterpret_cast<float*>(smem_raw), K, bias_part + (int64_t)blockIdx.x * K);
 }
 
 // ------------------------------------------------------------------ the products
@@ -365,7 +422,7 @@ __global__ void __launch_bounds__(256) k_router_dx(const T* __restrict__ ds, con
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int64_t row = m0 + 16 * i + lr < n ? m0 + 16 * i + lr : n - 1;
-    a[i] = ds + row * ld + (sizeof(T) == 2 ? 8 : 4) * lg;
+    a[i] = ds + row * ld + (sizeof(T) == 2 ? (lg >> 1) * kp + 8 * (lg & 1) : 4 * lg);
     const int col = c0 + 16 * i + lr < d ? c0 + 16 * i + lr : d - 1;
     b[i] = Rt + (int64_t)col * kp + (sizeof(T) == 2 ? 8 * (lg & 1) : 4 * lg);
   }
@@ -373,7 +430,7 @@ __global__ void __launch_bounds__(256) k_router_dx(const T* __restrict__ ds, con
     i32x4 av[4], bv[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      av[i] = *reinterpret_cast<const i32x4*>(a[i] + kb * (sizeof(T) == 2 ? 16 * kParts : 16));
+      av[i] = *reinterpret_cast<const i32x4*>(a[i] + kb * 16);
       bv[i] = *reinterpret_cast<const i32x4*>(b[i] + kb * 16);
     }
 #pragma unroll
@@ -384,23 +441,52 @@ __global__ void __launch_bounds__(256) k_router_dx(const T* __restrict__ ds, con
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int64_t row = m0 + 16 * i + lr;
-    if (row >= n) continue;
+    if constexpr (sizeof(T) == 2) {
+      // lanes 16 apart trade halves of two column blocks, and hold eight columns in a row each
+      typedef unsigned int u2v __attribute__((ext_vector_type(2)));
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int col = c0 + 16 * j + 4 * lg;
-      if (col >= d) continue;
-      typedef T quad __attribute__((ext_vector_type(4)));
-      quad v;
+      for (int p = 0; p < 2; ++p) {
+        bf16x4 va, vb;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) v[r] = from_f32<T>(acc[i][j][r]);
-      *reinterpret_cast<quad*>(dX + row * d + col) = v;
+        for (int r = 0; r < 4; ++r) {
+          va[r] = (bf16)acc[i][2 * p][r];
+          vb[r] = (bf16)acc[i][2 * p + 1][r];
+        }
+        const u2v x = __builtin_bit_cast(u2v, va), y = __builtin_bit_cast(u2v, vb);
+        const u2v s0 = __builtin_amdgcn_permlane16_swap(x[0], y[0], false, false);
+        const u2v s1 = __builtin_amdgcn_permlane16_swap(x[1], y[1], false, false);
+        const int col = c0 + 32 * p + 16 * (lg & 1) + 8 * (lg >> 1);
+        if (row < n && col < d)
+          *reinterpret_cast<i32x4*>(dX + row * d + col) = i32x4{(int)s0[0], (int)s1[0], (int)s0[1], (int)s1[1]};
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int col = c0 + 16 * j + 4 * lg;
+        if (row < n && col < d) *reinterpret_cast<floatx4*>(dX + row * d + col) = acc[i][j];
+      }
     }
   }
 }
 
-// part[piece][K][d] = ds^T X over the piece's rows: 16 or 32 experts of bf16, 32 of fp32 and 256 columns to a workgroup.
+// dX = ds R on the engine's tiles, the reduction over the first two planes: for more experts than the narrow form holds.
+template <class C>
+__global__ void __launch_bounds__(C::THREADS)
+    k_router_dx_wide(const bf16* __restrict__ ds, const bf16* __restrict__ Rt, int64_t n, int K, int d, bf16* __restrict__ dX) {
+  extern __shared__ __attribute__((aligned(16))) char smem_raw[];
+  lds<char>* smem = (lds<char>*)smem_raw;
+  const int ld = ds_width<bf16>(K), k = 2 * padded(K);
+  const TileCoord tc = tile_plain<C>(n, d, k);
+  if (!tc.valid) return;
+  floatx4 acc[C::MI][C::NJ];
+  gemm_tile<C, true, true>(ds + tc.m0 * ld, ld, tc.m_rows, Rt + (int64_t)tc.n0 * k, k, tc.n_cols, k, smem, acc);
+  store_out<C, bf16>(tc, acc, smem, dX, d, [](int, int, int, float v) { return v; }, RowId{tc.m0}, NoVec{});
+}
+
+// part[piece][K][d] = ds^T X over the piece's rows: bf16: all of up to 16 or 32 experts, fp32: 32 experts, and 256
+// columns to a workgroup.
 template <typename T, int UW>
-__global__ void __launch_bounds__(256) k_router_dr(const T* __restrict__ ds, const T* __restrict__ X, int64_t n, int K,
+__global__ void __launch_bounds__(256, 2) k_router_dr(const T* __restrict__ ds, const T* __restrict__ X, int64_t n, int K,
                                                    int d, int piece, float* __restrict__ part) {
   using C = Cfg<T, UW, 256, UW, 64>;
   extern __shared__ __attribute__((aligned(16))) char smem_raw[];
@@ -414,35 +500,50 @@ __global__ void __launch_bounds__(256) k_router_dr(const T* __restrict__ ds, con
   gemm_tile<C, false, false>(ds + p0 * ld + u0, ld, uv, X + p0 * d + c0, d, cv, rows, smem, acc);
   const Frag<C> f;
   float* to = part + (int64_t)blockIdx.y * K * d;
+  constexpr int B = sizeof(T) == 2 ? C::MI / kParts : C::MI;  // blocks of 16 experts; bf16: and the planes behind them
 #pragma unroll
-  for (int i = 0; i < C::MI; ++i)
+  for (int i = 0; i < B; ++i)
 #pragma unroll
     for (int j = 0; j < C::NJ; ++j)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int col = c0 + f.col(j, r);
-        if constexpr (sizeof(T) == 2) {
-          if (i % 3 != 0) continue;
-          const int e = u0 / 3 + 16 * (i / 3) + 4 * f.lg + r;
-          if (e < K && col < d) to[(int64_t)e * d + col] = (acc[i + 2][j][r] + acc[i + 1][j][r]) + acc[i][j][r];
-        } else {
-          const int e = u0 + f.row(i, r);
-          if (e < K && col < d) to[(int64_t)e * d + col] = acc[i][j][r];
-        }
+        const int e = (sizeof(T) == 2 ? 0 : u0) + f.row(i, r), col = c0 + f.col(j, r);
+        float v = acc[i][j][r];
+        if constexpr (sizeof(T) == 2) v = (acc[i + 2 * B][j][r] + acc[i + B][j][r]) + v;
+        if (e < K && col < d) to[(int64_t)e * d + col] = v;
       }
 }
 
-// dR and dbias: their parts added in order.
-__global__ void __launch_bounds__(256) k_router_join(const float* __restrict__ part, int pieces, int64_t size,
-                                                     float* __restrict__ dR, const float* __restrict__ bias_part, int blocks,
+// part[piece][planes and experts][d] = ds^T X for more experts, on the engine's tiles; gridDim.y pieces of the rows.
+template <class C>
+__global__ void __launch_bounds__(C::THREADS) k_router_dr_wide(const bf16* __restrict__ ds, const bf16* __restrict__ X,
+                                                               int64_t n, int K, int d, int piece, float* __restrict__ part) {
+  extern __shared__ __attribute__((aligned(16))) char smem_raw[];
+  lds<char>* smem = (lds<char>*)smem_raw;
+  const int ld = ds_width<bf16>(K);
+  const int64_t p0 = (int64_t)blockIdx.y * piece;
+  const int rows = n - p0 < piece ? (int)(n - p0) : piece;
+  const TileCoord tc = tile_plain<C>(ld, d, rows);
+  if (!tc.valid) return;
+  floatx4 acc[C::MI][C::NJ];
+  gemm_tile<C, false, false, false, true>(ds + p0 * ld + tc.m0, ld, tc.m_rows, X + p0 * d + tc.n0, d, tc.n_cols, rows, smem, acc);
+  store_out<C, float>(tc, acc, smem, part + (int64_t)blockIdx.y * ld * d, d, [](int, int, int, float v) { return v; },
+                      RowId{tc.m0}, NoVec{});
+}
+
+// dR and dbias: their parts added in order.  part[piece][plane], `plane` values apart, of which `size` are dR's.
+__global__ void __launch_bounds__(256) k_router_join(const float* __restrict__ part, int pieces, int planes,
+                                                     int64_t plane, int64_t size, float* __restrict__ dR, const float* __restrict__ bias_part, int blocks,
                                                      int K, float* __restrict__ dbias) {
   const int64_t groups = dR ? cdiv(size, 1024) : 0;
   if ((int64_t)blockIdx.x < groups) {
     const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
     if (i >= size) return;
     floatx4 v = {0.f, 0.f, 0.f, 0.f};
+    for (int z = planes - 1; z >= 0; --z) {  // the remainders first
 #pragma unroll 8
-    for (int q = 0; q < pieces; ++q) v += *reinterpret_cast<const floatx4*>(part + q * size + i);
+      for (int q = 0; q < pieces; ++q) v += *reinterpret_cast<const floatx4*>(part + (q * planes + z) * plane + i);
+    }
     *reinterpret_cast<floatx4*>(dR + i) = v;
     return;
   }
@@ -465,34 +566,54 @@ template <class F>
 int router_lanes(int K, F run) {
   using std::integral_constant;
   if (K <= 16) return run(integral_constant<int, 16>{}, integral_constant<int, 1>{});
+  if (K <= 32) return run(integral_constant<int, 16>{}, integral_constant<int, 2>{});
   if (K <= 64) return run(integral_constant<int, 16>{}, integral_constant<int, 4>{});
+  if (K <= 128) return run(integral_constant<int, 16>{}, integral_constant<int, 8>{});
   if (K <= 256) return run(integral_constant<int, 64>{}, integral_constant<int, 4>{});
   if (K <= 1024) return run(integral_constant<int, 64>{}, integral_constant<int, 16>{});
   return run(integral_constant<int, 64>{}, integral_constant<int, 64>{});
 }
 int router_blocks(int64_t n, int K) {
-  const int64_t rows = K <= 64 ? 16 : 4, all = cdiv(n, rows), most = 2 * device_cus();
+  int rows = 1;
+  router_lanes(K, [&](auto l, auto per) {
+    rows = kRowThreads<decltype(per)::value> / decltype(l)::value;
+    return (int)HMOE_OK;
+  });
+  const int64_t all = cdiv(n, rows), most = device_cus();
   return (int)(all < most ? all : most);
 }
-
-template <typename T>
-constexpr int kWide = sizeof(T) == 2 ? 96 : 32;  // columns of ds to a workgroup of k_router_dr
-template <typename T>
-int router_tiles(int K, int d) {
-  const int uw = sizeof(T) == 2 && K <= 16 ? 48 : kWide<T>;
-  return (ds_width<T>(K) + uw - 1) / uw * ((d + 255) / 256);
+// Pieces of the scores' reduction, of 256 products at least, where rows are few.
+int router_pieces(int64_t n, int K, int d) {
+  if (n == 0) return 1;
+  const int64_t tiles = cdiv(n, 64) * cdiv(K, 64), fit = 2 * device_cus() / tiles, most = d / 256;
+  const int64_t pieces = fit < most ? fit : most;
+  return (int)(pieces < 2 ? 1 : pieces > 16 ? 16 : pieces);
 }
-// Rows to a piece of dR's reduction.
+
+// Columns of ds to a workgroup of k_router_dr; bf16 data of more experts takes k_router_dr_wide.
+template <typename T>
+int router_columns(int K) {
+  return sizeof(T) == 4 ? 32 : K <= 16 ? 48 : 96;
+}
+template <typename T>
+bool router_wide(int K) {
+  return sizeof(T) == 2 && K > 32;
+}
+using WideDR = CfgPipeKS;
+// Rows to a piece of dR's reduction: whole stages, as many pieces as there are CUs (twice of them where two
+// workgroups share one) for the tiles.
 template <typename T>
 int router_piece(int64_t n, int K, int d) {
-  int rows = 64;
-  const int64_t tiles = router_tiles<T>(K, d);
-  while (rows < (1 << 20) && cdiv(n, rows) * tiles > 2 * device_cus()) rows *= 2;
-  return rows;
+  const int width = ds_width<T>(K);
+  const bool wide = router_wide<T>(K);
+  const int64_t tiles = wide ? cdiv(width, WideDR::BM) * cdiv(d, WideDR::BN) : cdiv(width, router_columns<T>(K)) * cdiv(d, 256);
+  const int64_t most = (wide ? 1 : 2) * device_cus() / tiles, pieces = most < 1 ? 1 : most;
+  const int64_t rows = cdiv(cdiv(n, pieces), 64) * 64, least = wide ? 256 : 64;
+  return (int)(rows < least ? least : rows);
 }
 
 struct RouterSpace {
-  float *share, *bias, *part;
+  float *planes, *share, *bias, *part;
   int32_t* count;
   double* z;
   void *ds, *Rt;
@@ -505,17 +626,19 @@ RouterSpace router_carve(const hmoe_router_t* p, int64_t n, Workspace& ws) {
   s.bias = s.share;  // of the other direction
   s.count = ws.take<int32_t>(parts);
   s.z = ws.take<double>(router_blocks(n, p->K));
+  const int pieces = router_pieces(n, p->K, p->d);
+  s.planes = pieces > 1 ? ws.take<float>((size_t)pieces * n * p->K) : nullptr;
   s.ds = ws.take<T>((size_t)n * ds_width<T>(p->K));
-  s.Rt = ws.take<T>((size_t)p->d * padded(p->K));
-  s.part = ws.take<float>((size_t)cdiv(n, router_piece<T>(n, p->K, p->d)) * p->K * p->d);
+  s.Rt = ws.take<T>((size_t)p->d * padded(p->K) * (router_wide<T>(p->K) ? 2 : 1));
+  s.part = ws.take<float>((size_t)cdiv(n, router_piece<T>(n, p->K, p->d)) * (router_wide<T>(p->K) ? ds_width<T>(p->K) : p->K) * p->d);
   return s;
 }
 
 template <class C>
-int router_scores(const hmoe_router_t* p, int64_t n, const void* X, float* scores, hipStream_t st) {
+int router_scores(const hmoe_router_t* p, int64_t n, const void* X, float* scores, int pieces, hipStream_t st) {
   using T = typename C::type;
-  HMOE_LAUNCH("router scores", k_router_scores<C>, dim3((unsigned)(cdiv(n, C::BM) * cdiv(p->K, C::BN))), dim3(C::THREADS),
-              C::LDS, st, (const T*)X, (const T*)p->R, p->bias, n, p->K, p->d, scores);
+  HMOE_LAUNCH("router scores", k_router_scores<C>, dim3((unsigned)(cdiv(n, C::BM) * cdiv(p->K, C::BN)), pieces),
+              dim3(C::THREADS), C::LDS, st, (const T*)X, (const T*)p->R, p->bias, n, p->K, p->d, scores);
   return HMOE_OK;
 }
 
@@ -525,11 +648,14 @@ int router_forward_t(const hmoe_router_t* p, int64_t n, const void* X, int32_t* 
   const RouterSpace w = router_carve<T>(p, n, ws);
   const int blocks = n > 0 ? router_blocks(n, p->K) : 0;
   if (n > 0) {
-    HMOE_TRY((router_scores<CfgD<T, 128, 64, 32, 64, 3>>(p, n, X, scores, st)));
+    const int pieces = router_pieces(n, p->K, p->d);
+    if (pieces > 1) HMOE_TRY((router_scores<CfgD<T, 64, 64, 32, 32, 5>>(p, n, X, w.planes, pieces, st)));
+    else if (p->K > 64) HMOE_TRY((router_scores<CfgD<T, 128, 128, 32, 64, 4>>(p, n, X, scores, 1, st)));
+    else HMOE_TRY((router_scores<CfgD<T, 128, 64, 32, 64, 3>>(p, n, X, scores, 1, st)));
     HMOE_TRY(router_lanes(p->K, [&](auto l, auto per) {
       constexpr int L = decltype(l)::value, P = decltype(per)::value;
-      HMOE_LAUNCH("router choose", (k_router_choose<L, P>), dim3(blocks), dim3(256), 256 / L * P * L * 4, st, scores, n,
-                  p->K, p->top_k, p->renorm != 0, expert, weight, w.share, w.count, w.z);
+      HMOE_LAUNCH("router choose", (k_router_choose<L, P>), dim3(blocks), dim3(kRowThreads<P>), kRowThreads<P> * P * 4, st, scores,
+                  pieces > 1 ? w.planes : nullptr, pieces, p->bias, n, p->K, p->top_k, p->renorm != 0, expert, weight, w.share, w.count, w.z);
       return (int)HMOE_OK;
     }));
   }
@@ -547,32 +673,55 @@ int router_backward_t(const hmoe_router_t* p, int64_t n, const void* X, const fl
   const double even = (double)balance * K / ((double)n * n * p->top_k);
   const float z2 = (float)(2.0 * z / (double)n);
   T* ds = (T*)w.ds;
+  constexpr bool BF = sizeof(T) == 2;
+  const bool wide = router_wide<T>(K), engine = wide && n > 256;
+  const Transposed<T> t = {(const T*)p->R, (T*)w.Rt, d, dX ? (engine ? 2 : 1) : 0};
+  const int turning = dX ? (int)cdiv(d, 64) * (padded(K) / 16) : 0;
   HMOE_TRY(router_lanes(K, [&](auto l, auto per) {
     constexpr int L = decltype(l)::value, P = decltype(per)::value;
-    HMOE_LAUNCH("router score gradient", (k_router_ds<T, L, P>), dim3(blocks), dim3(256), 256 / L * P * L * 4, st, scores,
-                expert, counts, g_weight, n, K, p->top_k, p->renorm != 0, even, z2, ds, w.bias);
+    HMOE_LAUNCH("router score gradient", (k_router_ds<T, L, P>), dim3(blocks + turning), dim3(kRowThreads<P>), kRowThreads<P> * P * 4, st, scores,
+                expert, counts, g_weight, n, K, p->top_k, p->renorm != 0, even, z2, ds, w.bias, blocks, t);
     return (int)HMOE_OK;
   }));
   if (dX) {
-    HMOE_LAUNCH("router transpose", k_router_transpose<T>, dim3((unsigned)cdiv(d, 64), padded(K) / 16), dim3(256), 0, st,
-                (const T*)p->R, K, d, (T*)w.Rt);
-    HMOE_LAUNCH("router dX", k_router_dx<T>, dim3((unsigned)(cdiv(n, 64) * cdiv(d, 256))), dim3(256), 0, st, ds,
-                (const T*)w.Rt, n, K, d, (T*)dX);
+    if constexpr (BF) {
+      using C = CfgPipe;
+      if (engine)
+        HMOE_LAUNCH("router dX", k_router_dx_wide<C>, dim3((unsigned)(cdiv(n, C::BM) * cdiv(d, C::BN))), dim3(C::THREADS),
+                    C::LDS, st, ds, (const T*)w.Rt, n, K, d, (T*)dX);
+    }
+    if (!engine)
+      HMOE_LAUNCH("router dX", k_router_dx<T>, dim3((unsigned)(cdiv(n, 64) * cdiv(d, 256))), dim3(256), 0, st, ds,
+                  (const T*)w.Rt, n, K, d, (T*)dX);
   }
   const int piece = router_piece<T>(n, K, d), pieces = (int)cdiv(n, piece);
   if (dR) {
-    const dim3 grid(router_tiles<T>(K, d), pieces);
-    if (sizeof(T) == 2 && K <= 16)
-      HMOE_LAUNCH("router dR", (k_router_dr<T, 48>), grid, dim3(256), (Cfg<T, 48, 256, 48, 64>::LDS), st, ds, (const T*)X,
-                  n, K, d, piece, w.part);
-    else
-      HMOE_LAUNCH("router dR", (k_router_dr<T, kWide<T>>), grid, dim3(256), (Cfg<T, kWide<T>, 256, kWide<T>, 64>::LDS), st,
-                  ds, (const T*)X, n, K, d, piece, w.part);
+    const int uw = router_columns<T>(K);
+    const dim3 grid((unsigned)(cdiv(ds_width<T>(K), uw) * cdiv(d, 256)), pieces);
+    const auto narrow = [&](auto columns) {
+      constexpr int UW = decltype(columns)::value;
+      HMOE_LAUNCH("router dR", (k_router_dr<T, UW>), grid, dim3(256), (Cfg<T, UW, 256, UW, 64>::LDS), st, ds, (const T*)X, n,
+                  K, d, piece, w.part);
+      return (int)HMOE_OK;
+    };
+    if constexpr (BF) {
+      using C = WideDR;
+      if (wide)
+        HMOE_LAUNCH("router dR", k_router_dr_wide<C>, dim3((unsigned)(cdiv(ds_width<T>(K), C::BM) * cdiv(d, C::BN)), pieces),
+                    dim3(C::THREADS), C::LDS, st, ds, (const T*)X, n, K, d, piece, w.part);
+      else if (K <= 16)
+        HMOE_TRY(narrow(std::integral_constant<int, 48>{}));
+      else
+        HMOE_TRY(narrow(std::integral_constant<int, 96>{}));
+    } else {
+      HMOE_TRY(narrow(std::integral_constant<int, 32>{}));
+    }
   }
   if (dR || dbias) {
     const int64_t size = (int64_t)K * d;
     HMOE_LAUNCH("router join", k_router_join, dim3((unsigned)((dR ? cdiv(size, 1024) : 0) + (dbias ? cdiv(K, 64) : 0))),
-                dim3(256), 0, st, w.part, pieces, size, dR, w.bias, blocks, K, dbias);
+                dim3(256), 0, st, w.part, pieces, wide ? kParts : 1, wide ? (int64_t)padded(K) * d : size, size, dR, w.bias,
+                blocks, K, dbias);
   }
   return HMOE_OK;
 }
