@@ -122,51 +122,36 @@ __device__ __forceinline__ void experts_out(const V (&acc)[P], V* sh, int K, V* 
 template <int P>
 constexpr int kRowThreads = P <= 4 ? 1024 : P <= 8 ? 512 : 256;
 
-// L lanes to a row, P scores to a lane.  With `planes` the scores are their sum and the bias, and are written, too.
-// A workgroup's counts, probabilities' sums and sum of squared lse go to
-// its row of the parts.
-template <int L, int P>
-__global__ void __launch_bounds__(kRowThreads<P>)
-    k_router_choose(float* __restrict__ scores, const float* __restrict__ planes, int pieces, const float* __restrict__ bias,
-                    int64_t n, int K, int top, int renorm, int32_t* __restrict__ expert, float* __restrict__ weight,
-                    float* __restrict__ share_part, int32_t* __restrict__ count_part, double* __restrict__ z_part) {
-  constexpr int THREADS = kRowThreads<P>, G = THREADS / L;
-  __shared__ double s_z[THREADS / 64];
-  extern __shared__ __attribute__((aligned(16))) char smem_raw[];
-  const int lane = threadIdx.x % L;
+// What becomes of rows of scores, L lanes to a row and P scores to a lane: expert p L + lane.
+struct Choices {
+  int64_t n;
+  int K, top, renorm;
+  int32_t* expert;
+  float* weight;
+  float* share_part;     // [workgroup][K]: a workgroup's sums of probabilities,
+  int32_t* count_part;   // counts,
+  double* z_part;        // [workgroup] and sums of squared lse
+};
+template <int L, int P, int THREADS>
+struct Chooser {
   float share[P];
   int32_t count[P];
+  double z;
+  __device__ __forceinline__ Chooser() : z(0.0) {
 #pragma unroll
-  for (int p = 0; p < P; ++p) share[p] = 0.f, count[p] = 0;
-  double z = 0.0;
-  for (int64_t first = (int64_t)blockIdx.x * G; first < n; first += (int64_t)gridDim.x * G) {
-    const int64_t row = first + threadIdx.x / L;
-    const bool live = row < n;
-    float s[P];
-    if (planes) {
-#pragma unroll
-      for (int p = 0; p < P; ++p) {
-        const bool in = live && p * L + lane < K;
-        s[p] = in ? 0.f : -INFINITY;
-        if (!in) continue;
-        const float* from = planes + row * K + p * L + lane;
-#pragma unroll 4
-        for (int z = 0; z < pieces; ++z) s[p] += from[(int64_t)z * n * K];
-        if (bias) s[p] += bias[p * L + lane];
-        scores[row * K + p * L + lane] = s[p];
-      }
-    } else {
-#pragma unroll
-      for (int p = 0; p < P; ++p) s[p] = live && p * L + lane < K ? scores[row * K + p * L + lane] : -INFINITY;
-    }
+    for (int p = 0; p < P; ++p) share[p] = 0.f, count[p] = 0;
+  }
+  // Row `row` if `live`; entered by whole waves.
+  __device__ __forceinline__ void take(const Choices& c, int64_t row, bool live, const float (&s)[P]) {
+    const int lane = threadIdx.x % L;
     uint32_t key[P];  // 0: no entry, or taken; 1: NaN
 #pragma unroll
-    for (int p = 0; p < P; ++p) key[p] = p * L + lane < K ? sortable(s[p]) + 1 : 0;
+    for (int p = 0; p < P; ++p) key[p] = p * L + lane < c.K ? sortable(s[p]) + 1 : 0;
     float chosen[HMOE_ROUTER_EXPERTS];
     int index[HMOE_ROUTER_EXPERTS];
 #pragma unroll
     for (int j = 0; j < HMOE_ROUTER_EXPERTS; ++j) {
-      if (j >= top) break;
+      if (j >= c.top) break;
       uint32_t best = key[0], at = ~0u;
 #pragma unroll
       for (int p = 1; p < P; ++p) best = key[p] > best ? key[p] : best;
@@ -194,19 +179,19 @@ __global__ void __launch_bounds__(kRowThreads<P>)
     tot = lanes_sum<L>(tot);
     const bool none = tot == 0.f;  // nothing but -inf
     float of = tot;  // the weights' sum
-    if (renorm) {
+    if (c.renorm) {
       of = tot != tot ? tot : 0.f;
 #pragma unroll
       for (int j = 0; j < HMOE_ROUTER_EXPERTS; ++j)
-        if (j < top) of += expf(chosen[j] - mx);
+        if (j < c.top) of += expf(chosen[j] - mx);
     }
-    if (!live) continue;
+    if (!live) return;
     if (lane == 0) {
 #pragma unroll
       for (int j = 0; j < HMOE_ROUTER_EXPERTS; ++j)
-        if (j < top) {
-          expert[row * top + j] = index[j];
-          weight[row * top + j] = none ? 0.f : expf(chosen[j] - mx) / of;
+        if (j < c.top) {
+          c.expert[row * c.top + j] = index[j];
+          c.weight[row * c.top + j] = none ? 0.f : expf(chosen[j] - mx) / of;
         }
       if (!none) {
         const float lse = mx + logf(tot);
@@ -219,64 +204,149 @@ __global__ void __launch_bounds__(kRowThreads<P>)
       for (int p = 0; p < P; ++p) share[p] = fmaf(p_e[p], inv, share[p]);
     }
   }
-  experts_out<L, P, THREADS>(share, reinterpret_cast<float*>(smem_raw), K, share_part + (int64_t)blockIdx.x * K);
-  experts_out<L, P, THREADS>(count, reinterpret_cast<int32_t*>(smem_raw), K, count_part + (int64_t)blockIdx.x * K);
-  z = wave_sum(z);
-  if ((threadIdx.x & 63) == 0) s_z[threadIdx.x >> 6] = z;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int i = 1; i < THREADS / 64; ++i) z += s_z[i];
-    z_part[blockIdx.x] = z;
+  // The workgroup's sums; `sh` holds THREADS P values.
+  __device__ __forceinline__ void leave(const Choices& c, char* sh) {
+    __shared__ double s_z[THREADS / 64];
+    experts_out<L, P, THREADS>(share, reinterpret_cast<float*>(sh), c.K, c.share_part + (int64_t)blockIdx.x * c.K);
+    experts_out<L, P, THREADS>(count, reinterpret_cast<int32_t*>(sh), c.K, c.count_part + (int64_t)blockIdx.x * c.K);
+    z = wave_sum(z);
+    if ((threadIdx.x & 63) == 0) s_z[threadIdx.x >> 6] = z;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      for (int i = 1; i < THREADS / 64; ++i) z += s_z[i];
+      c.z_part[blockIdx.x] = z;
+    }
   }
+};
+
+// With `planes` the scores are their sum and the bias, and are written, too.
+template <int L, int P>
+__global__ void __launch_bounds__(kRowThreads<P>)
+    k_router_choose(float* __restrict__ scores, const float* __restrict__ planes, int pieces, const float* __restrict__ bias,
+                    Choices c) {
+  constexpr int THREADS = kRowThreads<P>, G = THREADS / L;
+  extern __shared__ __attribute__((aligned(16))) char smem_raw[];
+  const int lane = threadIdx.x % L, K = c.K;
+  Chooser<L, P, THREADS> choose;
+  for (int64_t first = (int64_t)blockIdx.x * G; first < c.n; first += (int64_t)gridDim.x * G) {
+    const int64_t row = first + threadIdx.x / L;
+    const bool live = row < c.n;
+    float s[P];
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int e = p * L + lane;
+      s[p] = -INFINITY;
+      if (!live || e >= K) continue;
+      if (!planes) {
+        s[p] = scores[row * K + e];
+        continue;
+      }
+      s[p] = 0.f;
+#pragma unroll 4
+      for (int z = 0; z < pieces; ++z) s[p] += planes[((int64_t)z * c.n + row) * K + e];
+      if (bias) s[p] += bias[e];
+      scores[row * K + e] = s[p];
+    }
+    choose.take(c, row, live, s);
+  }
+  choose.leave(c, smem_raw);
 }
 
-// The parts added in order: a wave to 64 experts at a time, and the losses.  One workgroup.
+// Scores and choices of up to 16 P experts in one: a tile of scores goes through LDS to 16 lanes a row.  (65536 rows of
+// 16 experts, d = 2048: 62 and 12 us apart.)
+template <class C>
+constexpr int scored_lds() {
+  constexpr int rows = C::BM * (C::BN + 4) * 4;
+  return rows > C::LDS ? rows : C::LDS;
+}
+template <class C, int P>
+__global__ void __launch_bounds__(C::THREADS)
+    k_router_score_choose(const typename C::type* __restrict__ X, const typename C::type* __restrict__ R,
+                          const float* __restrict__ bias, int d, float* __restrict__ scores, Choices c) {
+  constexpr int L = 16, G = C::THREADS / L, LD = C::BN + 4;
+  static_assert(L * P <= C::BN, "scores of the tile");
+  extern __shared__ __attribute__((aligned(16))) char smem_raw[];
+  lds<char>* smem = (lds<char>*)smem_raw;
+  lds<float>* tile = (lds<float>*)smem_raw;
+  const int lane = threadIdx.x % L, K = c.K;
+  const Frag<C> f;
+  Chooser<L, P, C::THREADS> choose;
+  for (int64_t m0 = (int64_t)blockIdx.x * C::BM; m0 < c.n; m0 += (int64_t)gridDim.x * C::BM) {
+    const int rows = c.n - m0 < C::BM ? (int)(c.n - m0) : C::BM;
+    floatx4 acc[C::MI][C::NJ];
+    gemm_tile<C, true, true>(X + m0 * d, d, rows, R, d, K, d, smem, acc);
+#pragma unroll
+    for (int j = 0; j < C::NJ; ++j) {
+      const int col = f.col(j, 0);
+      floatx4 b;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) b[r] = bias && col + r < K ? bias[col + r] : 0.f;
+#pragma unroll
+      for (int i = 0; i < C::MI; ++i) *reinterpret_cast<lds<floatx4>*>(tile + f.row(i, 0) * LD + col) = acc[i][j] + b;
+    }
+    __syncthreads();
+    for (int r = threadIdx.x / L; r < C::BM; r += G) {
+      float s[P];
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        const int e = p * L + lane;
+        s[p] = e < K ? tile[r * LD + e] : -INFINITY;
+        if (r < rows && e < K) scores[(m0 + r) * K + e] = s[p];
+      }
+      choose.take(c, m0 + r, r < rows, s);
+    }
+    __syncthreads();  // before the next tile's loads
+  }
+  choose.leave(c, smem_raw);
+}
+
+// The parts added in order, and the losses, by one workgroup: `cols` experts at a time (a power of two up to 1024), the
+// workgroups' parts dealt to 1024 / cols threads each.
 __global__ void __launch_bounds__(1024)
     k_router_finish(const float* __restrict__ share_part, const int32_t* __restrict__ count_part,
-                    const double* __restrict__ z_part, int blocks, int64_t n, int K, int top, int32_t* __restrict__ counts,
-                    float* __restrict__ share, float* __restrict__ loss) {
-  __shared__ double s_sum[16][64];
-  __shared__ int32_t s_cnt[16][64];
-  __shared__ double s_dot;
+                    const double* __restrict__ z_part, int blocks, int64_t n, int K, int top, int cols,
+                    int32_t* __restrict__ counts, float* __restrict__ share, float* __restrict__ loss) {
+  __shared__ double s_sum[1024];
+  __shared__ int32_t s_cnt[1024];
+  __shared__ double s_dot[16], s_z[16];
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
-  if (threadIdx.x == 0) s_dot = 0.0;
-  for (int e0 = 0; e0 < K; e0 += 64) {
-    const int e = e0 + l;
+  const int col = threadIdx.x & (cols - 1), slice = threadIdx.x / cols, slices = 1024 / cols;
+  double dot = 0.0, z = 0.0;
+  for (int b = threadIdx.x; b < blocks; b += 1024) z += z_part[b];
+  for (int e0 = 0; e0 < K; e0 += cols) {
+    const int e = e0 + col;
     double p = 0.0;
     int32_t c = 0;
     if (e < K) {
 #pragma unroll 8
-      for (int b = w; b < blocks; b += 16) {
+      for (int b = slice; b < blocks; b += slices) {
         p += share_part[(int64_t)b * K + e];
         c += count_part[(int64_t)b * K + e];
       }
     }
     __syncthreads();
-    s_sum[w][l] = p;
-    s_cnt[w][l] = c;
+    s_sum[threadIdx.x] = p;
+    s_cnt[threadIdx.x] = c;
     __syncthreads();
-    if (w == 0) {
-      for (int i = 1; i < 16; ++i) {
-        p += s_sum[i][l];
-        c += s_cnt[i][l];
+    if (slice == 0 && e < K) {
+      for (int i = 1; i < slices; ++i) {
+        p += s_sum[i * cols + col];
+        c += s_cnt[i * cols + col];
       }
       const float mean = n > 0 ? (float)(p / (double)n) : 0.f;
-      if (e < K) {
-        counts[e] = c;
-        share[e] = mean;
-      }
-      const double dot = wave_sum(e < K ? (double)c * (double)mean : 0.0);
-      if (l == 0) s_dot += dot;
+      counts[e] = c;
+      share[e] = mean;
+      dot = fma((double)c, (double)mean, dot);
     }
   }
-  if (w == 0) {
-    double z = 0.0;
-    for (int b = l; b < blocks; b += 64) z += z_part[b];
-    z = wave_sum(z);
-    if (l == 0) {
-      loss[0] = n > 0 ? (float)(s_dot * K / ((double)n * top)) : 0.f;
-      loss[1] = n > 0 ? (float)(z / (double)n) : 0.f;
-    }
+  dot = wave_sum(dot);
+  z = wave_sum(z);
+  if (l == 0) s_dot[w] = dot, s_z[w] = z;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < 16; ++i) dot += s_dot[i], z += s_z[i];
+    loss[0] = n > 0 ? (float)(dot * K / ((double)n * top)) : 0.f;
+    loss[1] = n > 0 ? (float)(z / (double)n) : 0.f;
   }
 }
 
@@ -582,6 +652,18 @@ int router_blocks(int64_t n, int K) {
   const int64_t all = cdiv(n, rows), most = device_cus();
   return (int)(all < most ? all : most);
 }
+// Tiles of the scores; those of up to 64 and 128 experts choose, too.
+template <typename T>
+using ScoreNarrow = CfgD<T, 128, 64, 32, 64, 3>;
+template <typename T>
+using ScoreWide = CfgD<T, 128, 128, 32, 64, 4>;
+// Workgroups that score and choose: none where a tile to each leaves CUs idle and a row at a time is what takes long
+// (777 rows of 8 experts: 18 us in one, 10 and 8 apart).
+int scored_blocks(int64_t n, int K) {
+  const int64_t all = cdiv(n, 128), most = (K <= 64 ? 4 : 2) * device_cus();
+  if (K > 128 || all < device_cus() / 2) return 0;
+  return (int)(all < most ? all : most);
+}
 // Pieces of the scores' reduction, of 256 products at least, where rows are few.
 int router_pieces(int64_t n, int K, int d) {
   if (n == 0) return 1;
@@ -621,11 +703,12 @@ struct RouterSpace {
 template <typename T>
 RouterSpace router_carve(const hmoe_router_t* p, int64_t n, Workspace& ws) {
   RouterSpace s;
-  const size_t parts = (size_t)router_blocks(n, p->K) * p->K;
+  const int blocks = router_blocks(n, p->K), scored = scored_blocks(n, p->K);
+  const size_t most = blocks > scored ? blocks : scored, parts = most * p->K;
   s.share = ws.take<float>(parts);
   s.bias = s.share;  // of the other direction
   s.count = ws.take<int32_t>(parts);
-  s.z = ws.take<double>(router_blocks(n, p->K));
+  s.z = ws.take<double>(most);
   const int pieces = router_pieces(n, p->K, p->d);
   s.planes = pieces > 1 ? ws.take<float>((size_t)pieces * n * p->K) : nullptr;
   s.ds = ws.take<T>((size_t)n * ds_width<T>(p->K));
@@ -646,21 +729,41 @@ template <typename T>
 int router_forward_t(const hmoe_router_t* p, int64_t n, const void* X, int32_t* expert, float* weight, float* scores,
                      int32_t* counts, float* share, float* loss, Workspace& ws, hipStream_t st) {
   const RouterSpace w = router_carve<T>(p, n, ws);
-  const int blocks = n > 0 ? router_blocks(n, p->K) : 0;
+  int blocks = 0;
   if (n > 0) {
+    const Choices c = {n, p->K, p->top_k, p->renorm != 0, expert, weight, w.share, w.count, w.z};
     const int pieces = router_pieces(n, p->K, p->d);
-    if (pieces > 1) HMOE_TRY((router_scores<CfgD<T, 64, 64, 32, 32, 5>>(p, n, X, w.planes, pieces, st)));
-    else if (p->K > 64) HMOE_TRY((router_scores<CfgD<T, 128, 128, 32, 64, 4>>(p, n, X, scores, 1, st)));
-    else HMOE_TRY((router_scores<CfgD<T, 128, 64, 32, 64, 3>>(p, n, X, scores, 1, st)));
-    HMOE_TRY(router_lanes(p->K, [&](auto l, auto per) {
-      constexpr int L = decltype(l)::value, P = decltype(per)::value;
-      HMOE_LAUNCH("router choose", (k_router_choose<L, P>), dim3(blocks), dim3(kRowThreads<P>), kRowThreads<P> * P * 4, st, scores,
-                  pieces > 1 ? w.planes : nullptr, pieces, p->bias, n, p->K, p->top_k, p->renorm != 0, expert, weight, w.share, w.count, w.z);
+    const auto score_choose = [&](auto config, auto per) {
+      using C = decltype(config);
+      constexpr int P = decltype(per)::value;
+      blocks = scored_blocks(n, p->K);
+      HMOE_LAUNCH("router scores", (k_router_score_choose<C, P>), dim3(blocks), dim3(C::THREADS), scored_lds<C>(), st, (const T*)X,
+                  (const T*)p->R, p->bias, p->d, scores, c);
       return (int)HMOE_OK;
-    }));
+    };
+    using std::integral_constant;
+    if (scored_blocks(n, p->K) > 0) {
+      if (p->K <= 16) HMOE_TRY(score_choose(ScoreNarrow<T>{}, integral_constant<int, 1>{}));
+      else if (p->K <= 32) HMOE_TRY(score_choose(ScoreNarrow<T>{}, integral_constant<int, 2>{}));
+      else if (p->K <= 64) HMOE_TRY(score_choose(ScoreNarrow<T>{}, integral_constant<int, 4>{}));
+      else HMOE_TRY(score_choose(ScoreWide<T>{}, integral_constant<int, 8>{}));
+    } else {
+      if (pieces > 1) HMOE_TRY((router_scores<CfgD<T, 64, 64, 32, 32, 5>>(p, n, X, w.planes, pieces, st)));
+      else if (p->K <= 64) HMOE_TRY((router_scores<ScoreNarrow<T>>(p, n, X, scores, 1, st)));
+      else HMOE_TRY((router_scores<ScoreWide<T>>(p, n, X, scores, 1, st)));
+      blocks = router_blocks(n, p->K);
+      HMOE_TRY(router_lanes(p->K, [&](auto l, auto per) {
+        constexpr int L = decltype(l)::value, P = decltype(per)::value;
+        HMOE_LAUNCH("router choose", (k_router_choose<L, P>), dim3(blocks), dim3(kRowThreads<P>), kRowThreads<P> * P * 4, st,
+                    scores, pieces > 1 ? w.planes : nullptr, pieces, p->bias, c);
+        return (int)HMOE_OK;
+      }));
+    }
   }
+  int cols = 16;
+  while (cols < p->K && cols < 1024) cols *= 2;
   HMOE_LAUNCH("router finish", k_router_finish, dim3(1), dim3(1024), 0, st, w.share, w.count, w.z, blocks, n, p->K,
-              p->top_k, counts, share, loss);
+              p->top_k, cols, counts, share, loss);
   return HMOE_OK;
 }
 
