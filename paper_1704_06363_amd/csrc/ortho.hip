@@ -273,6 +273,115 @@ __global__ void __launch_bounds__(C::THREADS) k_ortho_product(Ortho o, Product p
   }
 }
 
+// The same for few tiles and short reductions, where a product is all latency: 64 x 64 tiles of four waves, and 256 values of
+// K of both operands at once in LDS, one trip to memory.  (152 x 152 of 152 on the 128 x 128 tiles, three
+// workgroups: 10 us, and 13 where the result adds A; 152 x 1356 of 152 28.)
+// A K-contiguous operand's row is 1 KB of LDS, chunk c of 16 bytes at c ^ (row & 15).  A K-strided one's 64 columns are 256
+// bytes of a row of X, hi and lo of 32 columns and of the next 32, chunk c at c ^ sw(k) (ks_off's swizzle).
+struct CfgMid {
+  using type = f16;
+  static constexpr bool TRANS = true, SPLIT = false, PAIR = true;
+  static constexpr int BM = 64, BN = 64, WM = 32, WN = 32, WAVES_N = 2, WAVES_M = 2, WAVES = 4, THREADS = 256, MI = 2, NJ = 2;
+  static constexpr int CK = 256;                  // K to a trip
+  static constexpr int LDS = 2 * 64 * CK * 4;     // 128 KB
+};
+__device__ __forceinline__ int mid_sw(int k) { return ((k & 3) | ((k >> 1) & 4)) << 1; }
+
+template <bool SYM, bool LAST>
+__global__ void __launch_bounds__(256) k_ortho_mid(Ortho o, Product p, OrthoStep s) {
+  using C = CfgMid;
+  extern __shared__ __attribute__((aligned(16))) char smem_raw[];
+  lds<char>* const sl = (lds<char>*)smem_raw;
+  lds<char>* const sr = sl + 64 * C::CK * 4;
+  const int b = blockIdx.x, q = b - p.full;
+  const ProductTile<C, SYM> t(o, p, q < 0 ? b : p.full + q / p.split);
+  const int steps = p.k / 32, piece = q < 0 ? 0 : q % p.split, pieces = q < 0 ? 1 : p.split;  // p.k: a multiple of 32
+  const int k_end = steps * (piece + 1) / pieces * 32;
+  const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const Frag<C> f;
+  floatx4 acc[2][2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+  // 16 rows to a wave; rows past the last take a valid row's bytes, chunks past the end of K the first's
+  const auto load_rows = [&](const f16* from, int r0, int k0, int len, lds<char>* to) {
+    const char* base = reinterpret_cast<const char*>(from) + (int64_t)k0 * 4;
+#pragma unroll 4
+    for (int i = 0; i < 16; ++i) {
+      const int row = 16 * w + i, at = r0 + row < o.r ? r0 + row : o.r - 1, c = l ^ (row & 15);
+      __builtin_amdgcn_global_load_lds((const void*)(base + (int64_t)at * 4 * p.k + (c * 4 < len ? c : 0) * 16),
+                                       (lds<void>*)(to + row * 1024), 16, 0, 0);
+    }
+  };
+  for (int k0 = steps * piece / pieces * 32; k0 < k_end; k0 += C::CK) {
+    const int len = k_end - k0 < C::CK ? k_end - k0 : C::CK;
+    load_rows(p.L + t.m * p.step, t.r0, k0, len, sl);
+    if constexpr (SYM) {
+      load_rows(p.R + t.m * p.step, t.c0, k0, len, sr);
+    } else {
+      const char* base = reinterpret_cast<const char*>(p.R + t.m * o.x_size()) + (int64_t)t.c0 * 4;
+      const int groups = (o.lp - t.c0) / 32 < 2 ? 1 : 2;  // of 32 columns
+#pragma unroll 4
+      for (int i = 0; i < 16; ++i) {
+        const int k = 64 * w + 4 * i + (l >> 4), c = (l & 15) ^ mid_sw(k);
+        const int64_t row = k0 + (k < len ? k : 0);
+        __builtin_amdgcn_global_load_lds((const void*)(base + row * 4 * o.lp + ((c >> 3) < groups ? c : c & 7) * 16),
+                                         (lds<void>*)(sr + (64 * w + 4 * i) * 256), 16, 0, 0);
+      }
+    }
+    wait_vmcnt<0>();
+    __syncthreads();
+    for (int ks = 0; ks < len / 32; ++ks) {
+      f16x8 a[2][2], bb[2][2];  // [fragment][hi, lo]
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+          const int row = f.wm * 32 + 16 * i + f.lr;
+          a[i][z] = *reinterpret_cast<const lds<f16x8>*>(sl + row * 1024 + (((8 * ks + 4 * z + f.lg) ^ (row & 15)) << 4));
+        }
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+          if constexpr (SYM) {
+            const int row = f.wn * 32 + 16 * j + f.lr;
+            bb[j][z] = *reinterpret_cast<const lds<f16x8>*>(sr + row * 1024 + (((8 * ks + 4 * z + f.lg) ^ (row & 15)) << 4));
+          } else {
+            typedef short s4 __attribute__((ext_vector_type(4)));
+            typedef short s8 __attribute__((ext_vector_type(8)));
+            const int k = 32 * ks + 8 * f.lg + (f.lr >> 2), c = f.wn * 8 + z * 4 + j * 2 + ((f.lr & 3) >> 1);
+            lds<char>* at = sr + k * 256 + ((c ^ mid_sw(k)) << 4) + (f.lr & 1) * 8;
+            const s4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds<s4>*)at);
+            const s4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds<s4>*)(at + 4 * 256));
+            bb[j][z] = __builtin_bit_cast(f16x8, s8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]});
+          }
+        }
+#pragma unroll
+      for (int z = 0; z < 3; ++z)  // the small products first
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bb[j][z == 0], a[i][z == 1], acc[i][j], 0, 0, 0);
+    }
+    __syncthreads();  // before the next trip's loads
+  }
+  if (q < 0) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) product_out<C, SYM, true, LAST>(o, p, s, t, f, i, j, acc[i][j]);
+  } else {
+    floatx4* to = p.part + (int64_t)q * 4 * 256 + threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) to[(i * 2 + j) * 256] = acc[i][j];
+  }
+}
+
 // The pieces of the tiles that are split added in order, and their results: blockIdx.y names the accumulators' row.
 template <class C, bool SYM, bool OUT_PAIR, bool LAST>
 __global__ void __launch_bounds__(C::THREADS) k_ortho_join(Ortho o, Product p, OrthoStep s) {
@@ -314,7 +423,7 @@ struct PickTile<false, false, false> { using C = CfgP<f16, 128, 256, 64, 64, tru
 // How the tiles of a product are dealt out.  Whole rounds of the CUs take a tile each; the tiles of the last round, if
 // two or more workgroups are there for each, share their reductions, four stages at least to a piece.
 struct Deal {
-  bool large;
+  bool large, mid;
   int per, full, split, rest;
   size_t part;  // floatx4 of the pieces
 };
@@ -333,7 +442,27 @@ Deal deal_on(const Ortho& o, int k, bool sym) {
   d.part = (size_t)d.rest * d.split * C::MI * C::NJ * C::THREADS;
   return d;
 }
+// For k_ortho_mid: all tiles split, or none; a piece for each of its trips if they fit on the chip at once.
+Deal deal_mid(const Ortho& o, int k, bool sym) {
+  using C = CfgMid;
+  Deal d = {};
+  d.mid = true;
+  const int64_t mt = cdiv(o.r, C::BM);
+  d.per = (int)(sym ? mt * (mt + 1) / 2 : mt * cdiv(o.lp, C::BN));
+  const int64_t tiles = (int64_t)d.per * o.K, fit = device_cus() / tiles, trips = cdiv(k, C::CK);
+  d.split = (int)(trips < fit ? trips : fit < 1 ? 1 : fit);
+  d.full = (int)(d.split > 1 ? 0 : tiles);
+  d.rest = (int)(d.split > 1 ? tiles : 0);
+  d.part = (size_t)d.rest * d.split * C::MI * C::NJ * C::THREADS;
+  return d;
+}
+// Whether a problem's products are few tiles and short reductions.
+bool is_mid(const Ortho& o) {
+  const int64_t mt = cdiv(o.r, 128);
+  return o.r <= 512 && mt * (mt + 1) / 2 * o.K < device_cus() / 4;
+}
 Deal deal(const Ortho& o, int k, bool sym) {
+  if (is_mid(o)) return deal_mid(o, k, sym);
   using L = PickTile<true, true, true>::C;
   const int64_t mt = cdiv(o.r, L::BM), tiles = (sym ? mt * (mt + 1) / 2 : mt * cdiv(o.lp, L::BN)) * o.K;
   // enough work for the large tiles: pieces of sixteen stages on every CU
@@ -341,6 +470,7 @@ Deal deal(const Ortho& o, int k, bool sym) {
   Deal d = large ? deal_on<L>(o, k, sym)
                  : sym ? deal_on<PickTile<true, false, true>::C>(o, k, sym) : deal_on<PickTile<true, false, false>::C>(o, k, sym);
   d.large = large;
+  d.mid = false;
   return d;
 }
 
@@ -359,6 +489,20 @@ int product_on(const Ortho& o, Product p, const Deal& d, const OrthoStep& s, hip
 template <bool PAIR, bool SYM, bool OUT_PAIR, bool LAST = false>
 int product(const Ortho& o, const Product& p, const OrthoStep& s, hipStream_t st) {
   const Deal d = deal(o, p.k, SYM);
+  if constexpr (PAIR && OUT_PAIR) {
+    if (d.mid) {
+      Product m = p;
+      m.per = d.per;
+      m.full = d.full;
+      m.split = d.split;
+      HMOE_LAUNCH(SYM ? "ortho square" : "ortho apply", (k_ortho_mid<SYM, LAST>), dim3((unsigned)(d.full + d.rest * d.split)),
+                  dim3(CfgMid::THREADS), CfgMid::LDS, st, o, m, s);
+      if (d.rest)
+        HMOE_LAUNCH("ortho join", (k_ortho_join<CfgMid, SYM, true, LAST>), dim3(d.rest, CfgMid::MI), dim3(CfgMid::THREADS), 0,
+                    st, o, m, s);
+      return HMOE_OK;
+    }
+  }
   if (d.large) return product_on<typename PickTile<PAIR, true, SYM>::C, SYM, OUT_PAIR, LAST>(o, p, d, s, st);
   return product_on<typename PickTile<PAIR, false, SYM>::C, SYM, OUT_PAIR, LAST>(o, p, d, s, st);
 }
@@ -443,7 +587,7 @@ int launch_ortho(const OrthoStep& s, int32_t K, int32_t rows, int32_t cols, int3
   if (small_ortho_ws(o) > 0) return launch_small_ortho(s, o, steps, coef, ws, st);
   const OrthoSpace w = ortho_carve(o, part_size(o), ws);
   HMOE_TRY(launch_ortho_start(s, o, w.part, st));
-  const bool low = s.G && s.dt == HMOE_BF16, single_first = low && steps == 1;
+  const bool low = s.G && s.dt == HMOE_BF16 && !is_mid(o), single_first = low && steps == 1;
   const int64_t parts = cdiv(o.rp, 64) * cdiv(o.lp, 64);
   HMOE_TRY(over_slices(K, parts, 256, [&](int64_t m0, int64_t count) {
     HMOE_LAUNCH("ortho split", k_ortho_split, dim3((unsigned)parts, (unsigned)count), dim3(256), 0, st, s, o, (int)m0,

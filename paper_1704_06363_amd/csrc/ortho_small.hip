@@ -243,13 +243,22 @@ __global__ void __launch_bounds__(512) k_ortho_small(Ortho o, OrthoStep s, Small
 #pragma unroll
         for (int t = 0; t < T; ++t) x[g][t] = mine[(g * T + t) * 512];
       if (owner) {
+        // all tiles of a chunk at a time, and several chunks: what these loads take is their latency
+        const floatx4* from = q.gram + ((int64_t)m * q.chunks * T * T + ti0 * T + tj) * 64 + l;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          const floatx4* from = q.gram + ((int64_t)m * q.chunks * T * T + ti(n) * T + tj) * 64 + l;
-          floatx4 v = from[0];
-#pragma unroll 4
-          for (int k = 1; k < q.chunks; ++k) v += from[(int64_t)k * T * T * 64];
-          af[n] = v;
+        for (int n = 0; n < NT; ++n) af[n] = floatx4{0.f, 0.f, 0.f, 0.f};
+        constexpr int AHEAD = NT >= 8 ? 4 : 8;
+        for (int k0 = 0; k0 < q.chunks; k0 += AHEAD) {
+          floatx4 v[AHEAD][NT];
+#pragma unroll
+          for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+              v[k][n] = k0 + k < q.chunks ? from[((int64_t)(k0 + k) * T * T + n * (8 / T) * T) * 64] : floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) af[n] += v[k][n];
         }
       }
       step();

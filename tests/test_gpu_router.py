@@ -97,7 +97,9 @@ def check_backward(g, f, X, p, top, renorm, gw, cb, cz, dtype):
 
 CASES = [(1, 1, 8, 1), (5, 3, 24, 2), (64, 16, 64, 1), (777, 8, 64, 1), (130, 17, 72, 4), (300, 64, 200, 8), (257, 65, 136, 3),
          (500, 128, 264, 4), (129, 200, 1000, 2), (100, 256, 64, 8), (70, 300, 520, 2), (33, 1025, 64, 8), (17, 4096, 40, 5),
-         (4000, 16, 1024, 2), (2000, 128, 520, 4)]
+         (4000, 16, 1024, 2), (2000, 128, 520, 4),
+         # scores and choices in one kernel; more tiles than workgroups
+         (16500, 12, 40, 2), (17001, 30, 24, 8), (20000, 64, 72, 3), (18003, 100, 136, 4), (140001, 5, 8, 1), (70001, 70, 8, 2)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
