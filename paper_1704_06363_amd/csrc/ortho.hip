@@ -46,11 +46,19 @@ __global__ void __launch_bounds__(256) k_ortho_start(OrthoStep s, Ortho o, int m
   const int m = m0 + blockIdx.y;
   const int64_t size = (int64_t)o.rows * o.cols, base = m * size;
   double sum = 0.0;
-  for (int64_t q = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; q < size; q += (int64_t)gridDim.x * 1024) {
-    ortho_momentum(s, base + q);
-    const floatx4 u = ortho_u(s, base + q);
+  const int64_t step = (int64_t)gridDim.x * 1024;
+  for (int64_t q = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; q < size; q += 4 * step) {
+    floatx4 u[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) sum = fma((double)u[e], (double)u[e], sum);
+    for (int i = 0; i < 4; ++i) {  // four in flight
+      const bool in = q + i * step < size;
+      if (in) ortho_momentum(s, base + q + i * step);
+      u[i] = in ? ortho_u(s, base + q + i * step) : floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum = fma((double)u[i][e], (double)u[i][e], sum);
   }
   sum = wave_sum(sum);
   if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = sum;
@@ -107,31 +115,33 @@ __global__ void __launch_bounds__(256) k_ortho_split(OrthoStep s, Ortho o, int m
 
 // ------------------------------------------------------------------ the products
 
-// Four values from column c (a multiple of 4) of a row, as pairs or as one fp16 number each.
-template <bool PAIR>
-__device__ __forceinline__ void put4(f16* row, int c, const float (&v)[4]) {
-  f16x4 hi, lo;
+// Four or eight (N) values from column c (a multiple of N) of a row, as pairs or as one fp16 number each.
+template <int N>
+using f16xN = _Float16 __attribute__((ext_vector_type(N)));
+template <bool PAIR, int N>
+__device__ __forceinline__ void put(f16* row, int c, const float* v) {
+  f16xN<N> hi, lo;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
+  for (int e = 0; e < N; ++e) {
     f16 h, l;
     pair_of(v[e], h, l);
     hi[e] = h;
     lo[e] = l;
   }
   if constexpr (PAIR) {
-    *reinterpret_cast<f16x4*>(row + pair_at(c)) = hi;
-    *reinterpret_cast<f16x4*>(row + pair_at(c) + kPairLo) = lo;
+    *reinterpret_cast<f16xN<N>*>(row + pair_at(c)) = hi;
+    *reinterpret_cast<f16xN<N>*>(row + pair_at(c) + kPairLo) = lo;
   } else {
-    *reinterpret_cast<f16x4*>(row + c) = hi;
+    *reinterpret_cast<f16xN<N>*>(row + c) = hi;
   }
 }
 template <bool PAIR>
-__device__ __forceinline__ void get4(const f16* row, int c, float (&v)[4]) {
-  const f16x4 hi = *reinterpret_cast<const f16x4*>(row + (PAIR ? pair_at(c) : c));
-  f16x4 lo = {0, 0, 0, 0};
-  if constexpr (PAIR) lo = *reinterpret_cast<const f16x4*>(row + pair_at(c) + kPairLo);
+__device__ __forceinline__ void get8(const f16* row, int c, float (&v)[8]) {
+  const f16x8 hi = *reinterpret_cast<const f16x8*>(row + (PAIR ? pair_at(c) : c));
+  f16x8 lo = {};
+  if constexpr (PAIR) lo = *reinterpret_cast<const f16x8*>(row + pair_at(c) + kPairLo);
 #pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = (float)hi[e] + (float)lo[e];
+  for (int e = 0; e < 8; ++e) v[e] = (float)hi[e] + (float)lo[e];
 }
 
 // Tile `b` of those on and above the diagonal, column by column.
@@ -185,56 +195,95 @@ struct ProductTile {
   }
 };
 
-// Accumulator (i, j) of a tile stored; LAST: where `s` says.
-template <class C, bool SYM, bool OUT_PAIR, bool LAST>
+// Accumulators (i, 2 h) and (i, 2 h + 1) of a tile stored; LAST: where `s` says.  Lanes 16 apart trade halves of the two
+// blocks of 16 columns, after which each holds eight consecutive columns: 16-byte vectors of hi and of lo.  FULL: the
+// tile has no rows or columns that do not exist, and nothing is behind a branch.
+template <class C, bool SYM, bool OUT_PAIR, bool LAST, bool FULL>
 __device__ __forceinline__ void product_out(const Ortho& o, const Product& p, const OrthoStep& s,
-                                            const ProductTile<C, SYM>& t, const Frag<C>& f, int i, int j, floatx4 acc) {
-  const int row = t.r0 + f.row(i, 0), col = t.c0 + f.col(j, 0);
+                                            const ProductTile<C, SYM>& t, const Frag<C>& f, int i, int h, floatx4 a0,
+                                            floatx4 a1) {
+  const int row = t.r0 + f.row(i, 0), col = t.c0 + f.block(2 * h) + 16 * (f.lg & 1) + 8 * (f.lg >> 1);
   const int width = SYM ? o.rp : o.lp, cols = SYM ? o.r : o.l;
   const int64_t size = SYM ? o.a_size() : o.x_size();
-  float v[4];
+  float v[8];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = acc[e] * p.alpha;
-  if (p.E && row < o.r && col < width) {
-    float x[4];
-    get4<C::PAIR>(p.E + t.m * size + row * stride<C::PAIR>(width), col, x);
+  for (int e = 0; e < 4; ++e) {
+    const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(a0[e]), __float_as_uint(a1[e]), false, false);
+    v[e] = __uint_as_float(x[0]) * p.alpha;
+    v[e + 4] = __uint_as_float(x[1]) * p.alpha;
+  }
+  if (p.E && (FULL || (row < o.r && col < width))) {
+    float x[8];
+    get8<C::PAIR>(p.E + t.m * size + row * stride<C::PAIR>(width), col, x);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = fmaf(p.beta, x[e], v[e]);
+    for (int e = 0; e < 8; ++e) v[e] = fmaf(p.beta, x[e], v[e]);
   }
   if constexpr (!LAST) {
     // the padding is zeros: rows and columns past the last take part in no product but with zeros
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
+    for (int e = 0; e < 8; ++e) {
       if constexpr (SYM) v[e] += row == col + e ? p.diag : 0.f;
-      v[e] = row < o.r && col + e < cols ? v[e] : 0.f;
+      if constexpr (!FULL) v[e] = row < o.r && col + e < cols ? v[e] : 0.f;
     }
     f16* out = p.out + t.m * size;
-    if (row < (SYM ? o.r : o.rp) && col < width) put4<OUT_PAIR>(out + row * stride<OUT_PAIR>(width), col, v);
+    if (FULL || (row < (SYM ? o.r : o.rp) && col < width)) put<OUT_PAIR, 8>(out + row * stride<OUT_PAIR>(width), col, v);
     if constexpr (SYM) {
       if (!t.mirror) return;
-      quad_transpose(v);  // now of column col + s, rows 4 q .. 4 q + 3 of the 16
-      const int tr = col + (f.lr & 3), tc = row - (f.lr & 3);
-      if (tr < o.r) put4<OUT_PAIR>(out + tr * stride<OUT_PAIR>(width), tc, v);
+#pragma unroll
+      for (int z = 0; z < 8; z += 4) {
+        float u[4] = {v[z], v[z + 1], v[z + 2], v[z + 3]};
+        quad_transpose(u);  // now of column col + z + lane % 4, rows 4 q .. 4 q + 3 of the 16
+        const int tr = col + z + (f.lr & 3), tc = row - (f.lr & 3);
+        if (FULL || tr < o.r) put<OUT_PAIR, 4>(out + tr * stride<OUT_PAIR>(width), tc, u);
+      }
     }
-    return;
   } else {
-    if (row >= o.r || col >= o.l) return;
+    if (!FULL && (row >= o.r || col >= o.l)) return;
     const int64_t base = (int64_t)t.m * o.rows * o.cols;
     if (!o.tall) {  // l = cols, a multiple of 8
-      ortho_put4(s, base + (int64_t)row * o.cols + col, v);
+#pragma unroll
+      for (int z = 0; z < 8; z += 4) {
+        const float u[4] = {v[z], v[z + 1], v[z + 2], v[z + 3]};
+        ortho_put4(s, base + (int64_t)row * o.cols + col + z, u);
+      }
     } else {  // X^T: the lanes of a row hold consecutive entries
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (col + e < o.l) ortho_put(s, base + (int64_t)(col + e) * o.cols + row, v[e]);
+      for (int e = 0; e < 8; ++e)
+        if (FULL || col + e < o.l) ortho_put(s, base + (int64_t)(col + e) * o.cols + row, v[e]);
     }
   }
+}
+// All accumulators of a tile, or (ROWS = 1) those of row i0 alone.
+template <class C, bool SYM, bool OUT_PAIR, bool LAST, int ROWS>
+__device__ __forceinline__ void product_rows(const Ortho& o, const Product& p, const OrthoStep& s,
+                                             const ProductTile<C, SYM>& t, int i0, const floatx4 (&acc)[ROWS][C::NJ]) {
+  const Frag<C> f;
+  const auto rows = [&](auto full) {
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i)
+#pragma unroll
+      for (int h = 0; h < C::NJ / 2; ++h)
+        product_out<C, SYM, OUT_PAIR, LAST, decltype(full)::value>(o, p, s, t, f, i0 + i, h, acc[i][2 * h], acc[i][2 * h + 1]);
+  };
+  if (t.r0 + C::BM <= o.r && t.c0 + C::BN <= (SYM ? o.r : o.l)) rows(std::true_type{});
+  else rows(std::false_type{});
+}
+
+// Workgroups go to the eight XCDs in turn, each with an L2 of its own: the b-th of n gets the place that gives each XCD a
+// run of its own.  (16 matrices of 2048 x 2048: tiles that share rows of A met in other L2s, and 415 us a square
+// instead of 358.)
+__device__ __forceinline__ int xcd_run(int b, int n) {
+  const int even = n / 8 * 8;
+  return b < even ? b % 8 * (even / 8) + b / 8 : b;
 }
 
 template <class C, bool SYM, bool OUT_PAIR, bool LAST>
 __global__ void __launch_bounds__(C::THREADS) k_ortho_product(Ortho o, Product p, OrthoStep s) {
   extern __shared__ __attribute__((aligned(16))) char smem_raw[];
   lds<char>* smem = (lds<char>*)smem_raw;
-  const int b = blockIdx.x, q = b - p.full;
+  const bool whole = (int)blockIdx.x < p.full;
+  const int b = whole ? xcd_run(blockIdx.x, p.full) : p.full + xcd_run(blockIdx.x - p.full, gridDim.x - p.full);
+  const int q = b - p.full;
   const ProductTile<C, SYM> t(o, p, q < 0 ? b : p.full + q / p.split);
   constexpr int kStage = C::PAIR ? C::BK / 2 : C::BK;  // of the reduction
   const int stages = (p.k + kStage - 1) / kStage, piece = q < 0 ? 0 : q % p.split, pieces = q < 0 ? 1 : p.split;
@@ -259,11 +308,7 @@ __global__ void __launch_bounds__(C::THREADS) k_ortho_product(Ortho o, Product p
     g.run(smem, acc);
   }
   if (q < 0) {
-    const Frag<C> f;
-#pragma unroll
-    for (int i = 0; i < C::MI; ++i)
-#pragma unroll
-      for (int j = 0; j < C::NJ; ++j) product_out<C, SYM, OUT_PAIR, LAST>(o, p, s, t, f, i, j, acc[i][j]);
+    product_rows<C, SYM, OUT_PAIR, LAST, C::MI>(o, p, s, t, 0, acc);
   } else {
     floatx4* to = p.part + (int64_t)q * C::MI * C::NJ * C::THREADS + threadIdx.x;
 #pragma unroll
@@ -369,10 +414,7 @@ __global__ void __launch_bounds__(256) k_ortho_mid(Ortho o, Product p, OrthoStep
     __syncthreads();  // before the next trip's loads
   }
   if (q < 0) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int j = 0; j < 2; ++j) product_out<C, SYM, true, LAST>(o, p, s, t, f, i, j, acc[i][j]);
+    product_rows<C, SYM, true, LAST, 2>(o, p, s, t, 0, acc);
   } else {
     floatx4* to = p.part + (int64_t)q * 4 * 256 + threadIdx.x;
 #pragma unroll
@@ -386,18 +428,16 @@ __global__ void __launch_bounds__(256) k_ortho_mid(Ortho o, Product p, OrthoStep
 template <class C, bool SYM, bool OUT_PAIR, bool LAST>
 __global__ void __launch_bounds__(C::THREADS) k_ortho_join(Ortho o, Product p, OrthoStep s) {
   const ProductTile<C, SYM> t(o, p, p.full + blockIdx.x);
-  const Frag<C> f;
   const int i = blockIdx.y;
   const floatx4* from = p.part + ((int64_t)blockIdx.x * p.split * C::MI + i) * C::NJ * C::THREADS + threadIdx.x;
-  floatx4 acc[C::NJ];
+  floatx4 acc[1][C::NJ];
 #pragma unroll
-  for (int j = 0; j < C::NJ; ++j) acc[j] = floatx4{0.f, 0.f, 0.f, 0.f};
+  for (int j = 0; j < C::NJ; ++j) acc[0][j] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
   for (int q = 0; q < p.split; ++q)
 #pragma unroll
-    for (int j = 0; j < C::NJ; ++j) acc[j] += from[((int64_t)q * C::MI * C::NJ + j) * C::THREADS];
-#pragma unroll
-  for (int j = 0; j < C::NJ; ++j) product_out<C, SYM, OUT_PAIR, LAST>(o, p, s, t, f, i, j, acc[j]);
+    for (int j = 0; j < C::NJ; ++j) acc[0][j] += from[((int64_t)q * C::MI * C::NJ + j) * C::THREADS];
+  product_rows<C, SYM, OUT_PAIR, LAST, 1>(o, p, s, t, i, acc);
 }
 
 // Tiles: 256 x 256 of eight waves, or 128 x 128 and 128 x 256 (the swizzle of a K-strided operand spans 256 columns).
