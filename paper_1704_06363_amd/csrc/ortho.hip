@@ -46,19 +46,25 @@ __global__ void __launch_bounds__(256) k_ortho_start(OrthoStep s, Ortho o, int m
   const int m = m0 + blockIdx.y;
   const int64_t size = (int64_t)o.rows * o.cols, base = m * size;
   double sum = 0.0;
-  const int64_t step = (int64_t)gridDim.x * 1024;
-  for (int64_t q = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; q < size; q += 4 * step) {
-    floatx4 u[4];
+  // a run of the matrix to a workgroup
+  const int64_t run = cdiv(cdiv(size, gridDim.x), 1024) * 1024, first = blockIdx.x * run;
+  const int64_t end = first + run < size ? first + run : size, step = 1024;
+  const auto add = [&](floatx4 u) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {  // four in flight
-      const bool in = q + i * step < size;
-      if (in) ortho_momentum(s, base + q + i * step);
-      u[i] = in ? ortho_u(s, base + q + i * step) : floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int e = 0; e < 4; ++e) sum = fma((double)u[e], (double)u[e], sum);
+  };
+  for (int64_t q = first + threadIdx.x * 4; q < end; q += 2 * step) {
+    const int64_t at = base + q, next = q + step < end ? at + step : at;
+    if (!s.G && s.v) {  // both pairs of loads before the first store
+      const floatx4 g0 = *reinterpret_cast<const floatx4*>(s.g + at), g1 = *reinterpret_cast<const floatx4*>(s.g + next);
+      const floatx4 v0 = *reinterpret_cast<const floatx4*>(s.v + at), v1 = *reinterpret_cast<const floatx4*>(s.v + next);
+      add(ortho_first_u(s, at, g0, v0));
+      if (next != at) add(ortho_first_u(s, next, g1, v1));
+    } else {
+      const floatx4 u0 = ortho_u(s, at), u1 = ortho_u(s, next);
+      add(u0);
+      if (next != at) add(u1);
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sum = fma((double)u[i][e], (double)u[i][e], sum);
   }
   sum = wave_sum(sum);
   if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = sum;
@@ -238,18 +244,19 @@ __device__ __forceinline__ void product_out(const Ortho& o, const Product& p, co
       }
     }
   } else {
-    if (!FULL && (row >= o.r || col >= o.l)) return;
+    // four entries in a row of the result: of a row of X, or (tall) of a column, which the quads turn; its rows are
+    // cols long, a multiple of 8
     const int64_t base = (int64_t)t.m * o.rows * o.cols;
-    if (!o.tall) {  // l = cols, a multiple of 8
 #pragma unroll
-      for (int z = 0; z < 8; z += 4) {
-        const float u[4] = {v[z], v[z + 1], v[z + 2], v[z + 3]};
-        ortho_put4(s, base + (int64_t)row * o.cols + col + z, u);
+    for (int z = 0; z < 8; z += 4) {
+      float u[4] = {v[z], v[z + 1], v[z + 2], v[z + 3]};
+      int r = row, c = col + z;
+      if (o.tall) {
+        quad_transpose(u);
+        r -= f.lr & 3;
+        c += f.lr & 3;
       }
-    } else {  // X^T: the lanes of a row hold consecutive entries
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (FULL || col + e < o.l) ortho_put(s, base + (int64_t)(col + e) * o.cols + row, v[e]);
+      if (FULL || (r < o.r && c < o.l)) ortho_put4(s, base + (o.tall ? (int64_t)c * o.cols + r : (int64_t)r * o.cols + c), u);
     }
   }
 }
@@ -318,17 +325,17 @@ __global__ void __launch_bounds__(C::THREADS) k_ortho_product(Ortho o, Product p
   }
 }
 
-// The same for few tiles and short reductions, where a product is all latency: 64 x 64 tiles of four waves, and 256 values of
-// K of both operands at once in LDS, one trip to memory.  (152 x 152 of 152 on the 128 x 128 tiles, three
+// The same for few tiles and short reductions, where a product is all latency: 64 x 64 tiles of four waves, and 128 values of
+// K of both operands to a trip to memory, two trips in flight.  (152 x 152 of 152 on the 128 x 128 tiles, three
 // workgroups: 10 us, and 13 where the result adds A; 152 x 1356 of 152 28.)
-// A K-contiguous operand's row is 1 KB of LDS, chunk c of 16 bytes at c ^ (row & 15).  A K-strided one's 64 columns are 256
+// A K-contiguous operand's row is 512 bytes of LDS, chunk c of 16 bytes at c ^ (row & 15).  A K-strided one's 64 columns are 256
 // bytes of a row of X, hi and lo of 32 columns and of the next 32, chunk c at c ^ sw(k) (ks_off's swizzle).
 struct CfgMid {
   using type = f16;
   static constexpr bool TRANS = true, SPLIT = false, PAIR = true;
   static constexpr int BM = 64, BN = 64, WM = 32, WN = 32, WAVES_N = 2, WAVES_M = 2, WAVES = 4, THREADS = 256, MI = 2, NJ = 2;
-  static constexpr int CK = 256;                  // K to a trip
-  static constexpr int LDS = 2 * 64 * CK * 4;     // 128 KB
+  static constexpr int CK = 128;                  // K to a trip
+  static constexpr int OPERAND = 64 * CK * 4, LDS = 4 * OPERAND;  // two of each: 128 KB
 };
 __device__ __forceinline__ int mid_sw(int k) { return ((k & 3) | ((k >> 1) & 4)) << 1; }
 
@@ -336,8 +343,7 @@ template <bool SYM, bool LAST>
 __global__ void __launch_bounds__(256) k_ortho_mid(Ortho o, Product p, OrthoStep s) {
   using C = CfgMid;
   extern __shared__ __attribute__((aligned(16))) char smem_raw[];
-  lds<char>* const sl = (lds<char>*)smem_raw;
-  lds<char>* const sr = sl + 64 * C::CK * 4;
+  lds<char>* const smem = (lds<char>*)smem_raw;
   const int b = blockIdx.x, q = b - p.full;
   const ProductTile<C, SYM> t(o, p, q < 0 ? b : p.full + q / p.split);
   const int steps = p.k / 32, piece = q < 0 ? 0 : q % p.split, pieces = q < 0 ? 1 : p.split;  // p.k: a multiple of 32
@@ -349,34 +355,51 @@ __global__ void __launch_bounds__(256) k_ortho_mid(Ortho o, Product p, OrthoStep
   for (int i = 0; i < 2; ++i)
 #pragma unroll
     for (int j = 0; j < 2; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-  // 16 rows to a wave; rows past the last take a valid row's bytes, chunks past the end of K the first's
+  // 16 rows to a wave, two to an instruction; rows past the last take a valid row's bytes, chunks past the end of K the
+  // first's
+  constexpr int LOADS = 16;  // of a wave and trip
   const auto load_rows = [&](const f16* from, int r0, int k0, int len, lds<char>* to) {
     const char* base = reinterpret_cast<const char*>(from) + (int64_t)k0 * 4;
-#pragma unroll 4
-    for (int i = 0; i < 16; ++i) {
-      const int row = 16 * w + i, at = r0 + row < o.r ? r0 + row : o.r - 1, c = l ^ (row & 15);
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+      const int row = 16 * w + i + (l >> 5), at = r0 + row < o.r ? r0 + row : o.r - 1, c = (l & 31) ^ (row & 15);
       __builtin_amdgcn_global_load_lds((const void*)(base + (int64_t)at * 4 * p.k + (c * 4 < len ? c : 0) * 16),
-                                       (lds<void>*)(to + row * 1024), 16, 0, 0);
+                                       (lds<void>*)(to + (16 * w + i) * 512), 16, 0, 0);
     }
   };
-  for (int k0 = steps * piece / pieces * 32; k0 < k_end; k0 += C::CK) {
-    const int len = k_end - k0 < C::CK ? k_end - k0 : C::CK;
-    load_rows(p.L + t.m * p.step, t.r0, k0, len, sl);
+  const int k_begin = steps * piece / pieces * 32;
+  const auto length = [&](int k0) { return k_end - k0 < C::CK ? k_end - k0 : C::CK; };
+  const auto load = [&](int k0, int buffer) {
+    lds<char>* const to = smem + buffer * 2 * C::OPERAND;
+    const int len = length(k0);
+    load_rows(p.L + t.m * p.step, t.r0, k0, len, to);
     if constexpr (SYM) {
-      load_rows(p.R + t.m * p.step, t.c0, k0, len, sr);
+      load_rows(p.R + t.m * p.step, t.c0, k0, len, to + C::OPERAND);
     } else {
       const char* base = reinterpret_cast<const char*>(p.R + t.m * o.x_size()) + (int64_t)t.c0 * 4;
       const int groups = (o.lp - t.c0) / 32 < 2 ? 1 : 2;  // of 32 columns
-#pragma unroll 4
-      for (int i = 0; i < 16; ++i) {
-        const int k = 64 * w + 4 * i + (l >> 4), c = (l & 15) ^ mid_sw(k);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int k = 32 * w + 4 * i + (l >> 4), c = (l & 15) ^ mid_sw(k);
         const int64_t row = k0 + (k < len ? k : 0);
         __builtin_amdgcn_global_load_lds((const void*)(base + row * 4 * o.lp + ((c >> 3) < groups ? c : c & 7) * 16),
-                                         (lds<void>*)(sr + (64 * w + 4 * i) * 256), 16, 0, 0);
+                                         (lds<void>*)(to + C::OPERAND + (32 * w + 4 * i) * 256), 16, 0, 0);
       }
     }
-    wait_vmcnt<0>();
+  };
+  load(k_begin, 0);
+  int buffer = 0;
+  for (int k0 = k_begin; k0 < k_end; k0 += C::CK, buffer ^= 1) {
+    const int len = length(k0);
+    if (k0 + C::CK < k_end) {
+      load(k0 + C::CK, buffer ^ 1);
+      wait_vmcnt<LOADS>();
+    } else {
+      wait_vmcnt<0>();
+    }
     __syncthreads();
+    lds<char>* const sl = smem + buffer * 2 * C::OPERAND;
+    lds<char>* const sr = sl + C::OPERAND;
     for (int ks = 0; ks < len / 32; ++ks) {
       f16x8 a[2][2], bb[2][2];  // [fragment][hi, lo]
 #pragma unroll
@@ -384,7 +407,7 @@ __global__ void __launch_bounds__(256) k_ortho_mid(Ortho o, Product p, OrthoStep
 #pragma unroll
         for (int z = 0; z < 2; ++z) {
           const int row = f.wm * 32 + 16 * i + f.lr;
-          a[i][z] = *reinterpret_cast<const lds<f16x8>*>(sl + row * 1024 + (((8 * ks + 4 * z + f.lg) ^ (row & 15)) << 4));
+          a[i][z] = *reinterpret_cast<const lds<f16x8>*>(sl + row * 512 + (((8 * ks + 4 * z + f.lg) ^ (row & 15)) << 4));
         }
 #pragma unroll
       for (int j = 0; j < 2; ++j)
@@ -392,7 +415,7 @@ __global__ void __launch_bounds__(256) k_ortho_mid(Ortho o, Product p, OrthoStep
         for (int z = 0; z < 2; ++z) {
           if constexpr (SYM) {
             const int row = f.wn * 32 + 16 * j + f.lr;
-            bb[j][z] = *reinterpret_cast<const lds<f16x8>*>(sr + row * 1024 + (((8 * ks + 4 * z + f.lg) ^ (row & 15)) << 4));
+            bb[j][z] = *reinterpret_cast<const lds<f16x8>*>(sr + row * 512 + (((8 * ks + 4 * z + f.lg) ^ (row & 15)) << 4));
           } else {
             typedef short s4 __attribute__((ext_vector_type(4)));
             typedef short s8 __attribute__((ext_vector_type(8)));
@@ -411,7 +434,7 @@ __global__ void __launch_bounds__(256) k_ortho_mid(Ortho o, Product p, OrthoStep
           for (int j = 0; j < 2; ++j)
             acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bb[j][z == 0], a[i][z == 1], acc[i][j], 0, 0, 0);
     }
-    __syncthreads();  // before the next trip's loads
+    __syncthreads();  // before the loads of the trip after the next
   }
   if (q < 0) {
     product_rows<C, SYM, true, LAST, 2>(o, p, s, t, 0, acc);
@@ -475,21 +498,26 @@ Deal deal_on(const Ortho& o, int k, bool sym) {
   const int64_t tiles = (int64_t)d.per * o.K;
   const int64_t slots = (int64_t)device_cus() * (C::LDS <= 64 * 1024 ? 2 : 1);
   const int64_t rest = tiles % slots, fit = rest > 0 ? slots / rest : 1, most = k / 32 / 4;
-  const int64_t split = fit < most ? fit : most;
-  d.split = (int)(split < 2 ? 1 : split > 64 ? 64 : split);
+  int64_t split = fit < most ? fit : most;
+  split = split < 2 ? 1 : split > 64 ? 64 : split;
+  // what sharing saves of a tile's stages against the launch that joins the pieces (16 matrices of 562 x 562: 20 us for the
+  // halves and 12 to join them, 22 whole)
+  constexpr float stage = C::BM * C::BN == 256 * 256 ? 2.3f : C::BN == 256 ? 1.1f : 0.6f;  // us
+  if ((1.f - 1.f / split) * (k / 32) * stage < 12.f) split = 1;
+  d.split = (int)split;
   d.full = (int)(d.split > 1 ? tiles - rest : tiles);
   d.rest = (int)(d.split > 1 ? rest : 0);
   d.part = (size_t)d.rest * d.split * C::MI * C::NJ * C::THREADS;
   return d;
 }
-// For k_ortho_mid: all tiles split, or none; a piece for each of its trips if they fit on the chip at once.
+// For k_ortho_mid: all tiles split, or none; a piece for every two trips if they fit on the chip at once.
 Deal deal_mid(const Ortho& o, int k, bool sym) {
   using C = CfgMid;
   Deal d = {};
   d.mid = true;
   const int64_t mt = cdiv(o.r, C::BM);
   d.per = (int)(sym ? mt * (mt + 1) / 2 : mt * cdiv(o.lp, C::BN));
-  const int64_t tiles = (int64_t)d.per * o.K, fit = device_cus() / tiles, trips = cdiv(k, C::CK);
+  const int64_t tiles = (int64_t)d.per * o.K, fit = device_cus() / tiles, trips = cdiv(k, 2 * C::CK);
   d.split = (int)(trips < fit ? trips : fit < 1 ? 1 : fit);
   d.full = (int)(d.split > 1 ? 0 : tiles);
   d.rest = (int)(d.split > 1 ? tiles : 0);
@@ -501,8 +529,12 @@ bool is_mid(const Ortho& o) {
   const int64_t mt = cdiv(o.r, 128);
   return o.r <= 512 && mt * (mt + 1) / 2 * o.K < device_cus() / 4;
 }
-Deal deal(const Ortho& o, int k, bool sym) {
-  if (is_mid(o)) return deal_mid(o, k, sym);
+// pairs: k_ortho_mid can be taken -- for symmetric products of larger matrices, too, whose tiles all run at once (1024 x
+// 1024 in pieces of 128 x 128 tiles: 14 us, and 7 to join them).
+Deal deal(const Ortho& o, int k, bool sym, bool pairs) {
+  if (pairs && is_mid(o)) return deal_mid(o, k, sym);
+  const int64_t m64 = cdiv(o.r, 64);
+  if (pairs && sym && k == o.rp && m64 * (m64 + 1) / 2 * o.K <= device_cus()) return deal_mid(o, k, sym);
   using L = PickTile<true, true, true>::C;
   const int64_t mt = cdiv(o.r, L::BM), tiles = (sym ? mt * (mt + 1) / 2 : mt * cdiv(o.lp, L::BN)) * o.K;
   // enough work for the large tiles: pieces of sixteen stages on every CU
@@ -528,7 +560,7 @@ int product_on(const Ortho& o, Product p, const Deal& d, const OrthoStep& s, hip
 // Factors and results as pairs, or (fp16 numbers alone) as said.
 template <bool PAIR, bool SYM, bool OUT_PAIR, bool LAST = false>
 int product(const Ortho& o, const Product& p, const OrthoStep& s, hipStream_t st) {
-  const Deal d = deal(o, p.k, SYM);
+  const Deal d = deal(o, p.k, SYM, PAIR && OUT_PAIR);
   if constexpr (PAIR && OUT_PAIR) {
     if (d.mid) {
       Product m = p;
@@ -549,7 +581,9 @@ int product(const Ortho& o, const Product& p, const OrthoStep& s, hipStream_t st
 
 size_t part_size(const Ortho& o) {
   size_t most = 0;
-  for (const Deal& d : {deal(o, o.lp, true), deal(o, o.rp, true), deal(o, o.rp, false)}) most = d.part > most ? d.part : most;
+  for (const bool pairs : {false, true})
+    for (const Deal& d : {deal(o, o.lp, true, pairs), deal(o, o.rp, true, pairs), deal(o, o.rp, false, pairs)})
+      most = d.part > most ? d.part : most;
   return most;
 }
 

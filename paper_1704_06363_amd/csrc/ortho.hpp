@@ -30,20 +30,11 @@ inline Ortho ortho_of(int K, int rows, int cols) {
   o.l = o.tall ? rows : cols;
   o.rp = (o.r + 31) / 32 * 32;
   o.lp = (o.l + 31) / 32 * 32;
-  const int64_t want = cdiv((int64_t)rows * cols, 256 * 32), most = cdiv(4 * (int64_t)device_cus(), K);
+  const int64_t want = cdiv((int64_t)rows * cols, 256 * 32), most = cdiv(8 * (int64_t)device_cus(), K);
   o.blocks = (int)(want < most ? want : most);
   return o;
 }
-// v = momentum v + g at four entries.
-__device__ __forceinline__ void ortho_momentum(const OrthoStep& s, int64_t at) {
-  if (s.G || !s.v) return;
-  const floatx4 g = *reinterpret_cast<const floatx4*>(s.g + at);
-  floatx4 v = *reinterpret_cast<const floatx4*>(s.v + at);
-#pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = fmaf(s.momentum, v[e], g[e]);
-  *reinterpret_cast<floatx4*>(s.v + at) = v;
-}
-// Four entries of U from `at` on, v as it is after that.
+// Four entries of U from `at` on, v as it is after k_ortho_start.
 __device__ __forceinline__ floatx4 ortho_u(const OrthoStep& s, int64_t at) {
   if (s.G) {
     if (s.dt == HMOE_BF16) {
@@ -60,6 +51,21 @@ __device__ __forceinline__ floatx4 ortho_u(const OrthoStep& s, int64_t at) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) u[e] = fmaf(s.momentum, v[e], g[e]);
   return u;
+}
+// The same with v = momentum v + g first.
+__device__ __forceinline__ floatx4 ortho_first_u(const OrthoStep& s, int64_t at, floatx4 g, floatx4 v) {
+  floatx4 u;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    v[e] = fmaf(s.momentum, v[e], g[e]);
+    u[e] = s.nesterov ? fmaf(s.momentum, v[e], g[e]) : v[e];
+  }
+  *reinterpret_cast<floatx4*>(s.v + at) = v;
+  return u;
+}
+__device__ __forceinline__ floatx4 ortho_first_u(const OrthoStep& s, int64_t at) {
+  if (s.G || !s.v) return ortho_u(s, at);
+  return ortho_first_u(s, at, *reinterpret_cast<const floatx4*>(s.g + at), *reinterpret_cast<const floatx4*>(s.v + at));
 }
 
 __device__ __forceinline__ void pair_of(float v, f16& hi, f16& lo) {
@@ -89,19 +95,7 @@ __device__ __forceinline__ void quad_transpose(float (&v)[4]) {
   }
 }
 
-// One or four consecutive entries of the result where the call wants them: in O, or as the step of w and w_lo.
-__device__ __forceinline__ void ortho_put(const OrthoStep& s, int64_t at, float v) {
-  if (s.G) {
-    if (s.dt == HMOE_BF16) static_cast<bf16*>(s.O)[at] = (bf16)v;
-    else static_cast<float*>(s.O)[at] = v;
-    return;
-  }
-  const float w = fmaf(-s.rate, v, s.keep * s.w[at]);
-  s.w[at] = w;
-  if (!s.w_lo) return;
-  if (s.dt == HMOE_BF16) static_cast<bf16*>(s.w_lo)[at] = (bf16)w;
-  else static_cast<float*>(s.w_lo)[at] = w;
-}
+// Four consecutive entries of the result where the call wants them: in O, or as the step of w and w_lo.
 __device__ __forceinline__ void ortho_put4(const OrthoStep& s, int64_t at, const float (&v)[4]) {
   floatx4 w = {v[0], v[1], v[2], v[3]};
   if (!s.G) {

@@ -84,8 +84,7 @@ __global__ void __launch_bounds__(512) k_ortho_small(Ortho o, OrthoStep s, Small
         const int64_t at = base + (o.tall ? (int64_t)col * o.cols + row : (int64_t)row * o.cols + col);
         floatx4 u = {0.f, 0.f, 0.f, 0.f};
         if (row < o.r && col < o.l) {  // the vector is along cols, a multiple of 8
-          if constexpr (WHOLE) ortho_momentum(s, at);
-          u = ortho_u(s, at);
+          u = WHOLE ? ortho_first_u(s, at) : ortho_u(s, at);
         }
         float v[4] = {u[0], u[1], u[2], u[3]};
         if (!o.tall) quad_transpose(v);
