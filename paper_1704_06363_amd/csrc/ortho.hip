@@ -518,7 +518,7 @@ Deal deal_mid(const Ortho& o, int k, bool sym) {
   const int64_t mt = cdiv(o.r, C::BM);
   d.per = (int)(sym ? mt * (mt + 1) / 2 : mt * cdiv(o.lp, C::BN));
   const int64_t tiles = (int64_t)d.per * o.K, fit = device_cus() / tiles, trips = cdiv(k, 2 * C::CK);
-  d.split = (int)(trips < fit ? trips : fit < 1 ? 1 : fit);
+  d.split = (int)(trips <= 2 ? 1 : trips < fit ? trips : fit < 1 ? 1 : fit);  // a trip takes less than a launch
   d.full = (int)(d.split > 1 ? 0 : tiles);
   d.rest = (int)(d.split > 1 ? tiles : 0);
   d.part = (size_t)d.rest * d.split * C::MI * C::NJ * C::THREADS;

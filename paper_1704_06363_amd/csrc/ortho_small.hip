@@ -295,7 +295,10 @@ Plan plan_of(const Ortho& o) {
   else if (o.r <= 128) p = {128, 1, 0};
   else return p;
   p.chunks = chunks(p.NG);
-  if (p.chunks > (p.RB == 32 ? 64 : 16)) p.RB = 0;
+  // Every workgroup adds up all chunks' Gram matrices, which takes longer than a launch to a product for many chunks of 64
+  // KB each (us for five steps here and on k_ortho_mid: 128 x 1024 98 and 110, 128 x 2048 124 and 112; eight of 128 x
+  // 1024 111 and 126; 32 of 128 x 512 108 and 145, of 128 x 1024 184 and 178; 64 x 4096 70 and 101, 32 of them 180 and 191).
+  if (p.RB == 32 ? p.chunks > 64 : p.RB == 64 ? p.chunks > 16 : p.chunks > 8 || p.chunks * o.K >= device_cus()) p.RB = 0;
   return p;
 }
 
