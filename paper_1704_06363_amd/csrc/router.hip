@@ -398,6 +398,16 @@ __global__ void __launch_bounds__(kRowThreads<P>)
   for (int64_t first = (int64_t)blockIdx.x * G; first < n; first += (int64_t)blocks * G) {
     const int64_t row = first + threadIdx.x / L;
     const bool live = row < n;
+    // all of a row's choices before any is looked at: one by one they took a trip to memory each (32768 rows of 128 experts,
+    // four choices: 23 us)
+    int chosen[HMOE_ROUTER_EXPERTS];
+    float gw[HMOE_ROUTER_EXPERTS];
+#pragma unroll
+    for (int j = 0; j < HMOE_ROUTER_EXPERTS; ++j) {
+      const bool in = j < top && g_weight && live;
+      chosen[j] = in ? expert[row * top + j] : -1;
+      gw[j] = in ? g_weight[row * top + j] : 0.f;
+    }
     float s[P], mx = -INFINITY;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
@@ -416,17 +426,15 @@ __global__ void __launch_bounds__(kRowThreads<P>)
     }
     tot = lanes_sum<L>(tot);
     const bool none = tot == 0.f;
-    if (g_weight && live) {
-      for (int j = 0; j < top; ++j) {
-        const int e = expert[row * top + j];
-        const float gw = g_weight[row * top + j];
 #pragma unroll
-        for (int p = 0; p < P; ++p)
-          if (e == p * L + lane && e < K) {
-            g[p] += gw;
-            on[p] = 1.f;
-          }
-      }
+    for (int j = 0; j < HMOE_ROUTER_EXPERTS; ++j) {
+      if (j >= top) break;
+#pragma unroll
+      for (int p = 0; p < P; ++p)
+        if (chosen[j] == p * L + lane && chosen[j] < K) {
+          g[p] += gw[j];
+          on[p] = 1.f;
+        }
     }
     const float inv = none ? 0.f : 1.f / tot, lse = none ? 0.f : mx + logf(tot);
     float dot = 0.f, wt = 0.f, wg = 0.f;
@@ -664,10 +672,10 @@ int scored_blocks(int64_t n, int K) {
   if (K > 128 || all < device_cus() / 2) return 0;
   return (int)(all < most ? all : most);
 }
-// Pieces of the scores' reduction, of 256 products at least, where rows are few.
+// Pieces of the scores' reduction, of 128 products at least, where rows are few.
 int router_pieces(int64_t n, int K, int d) {
   if (n == 0) return 1;
-  const int64_t tiles = cdiv(n, 64) * cdiv(K, 64), fit = 2 * device_cus() / tiles, most = d / 256;
+  const int64_t tiles = cdiv(n, 64) * cdiv(K, 64), fit = 2 * device_cus() / tiles, most = d / 128;
   const int64_t pieces = fit < most ? fit : most;
   return (int)(pieces < 2 ? 1 : pieces > 16 ? 16 : pieces);
 }
