@@ -867,20 +867,22 @@ COEF = (3.4445, -4.7750, 2.0315)  # of hmoe_orthogonalise's iterations
 
 
 def _same_device(*tensors):
-    """The device that all of them (None aside) are on, a GPU; the library launches on the current one."""
-    dev = None
+    """All of them (None aside) are on one GPU, the current device: the library launches there.  Numbers of devices, as
+    comparing device objects takes a microsecond a call."""
+    at = -1
     for t in tensors:
         if t is None:
             continue
-        if not t.is_cuda:
+        d = t.get_device()
+        if d == at:
+            continue
+        if d < 0:
             raise HmoeError("tensor is not on the GPU")
-        if dev is None:
-            dev = t.device
-        elif t.device != dev:
-            raise HmoeError(f"tensors on {dev} and {t.device}")
-    if dev.index != torch.cuda.current_device():
-        raise HmoeError(f"tensors on {dev}, which is not the current device")
-    return dev
+        if at >= 0:
+            raise HmoeError(f"tensors on devices {at} and {d}")
+        at = d
+    if at != torch._C._cuda_getDevice():
+        raise HmoeError(f"tensors on device {at}, which is not the current one")
 
 
 def make_router(p: dict, top_k: int = 1, renorm: bool = False) -> Router:
