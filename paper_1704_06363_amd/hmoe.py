@@ -869,16 +869,16 @@ COEF = (3.4445, -4.7750, 2.0315)  # of hmoe_orthogonalise's iterations
 def _same_device(*tensors):
     """All of them (None aside) are on one GPU, the current device: the library launches there.  Numbers of devices, as
     comparing device objects takes a microsecond a call."""
-    at = -1
+    at = None
     for t in tensors:
         if t is None:
             continue
-        d = t.get_device()
+        d = t.get_device()  # -1: on the host
         if d == at:
             continue
         if d < 0:
             raise HmoeError("tensor is not on the GPU")
-        if at >= 0:
+        if at is not None:
             raise HmoeError(f"tensors on devices {at} and {d}")
         at = d
     if at != torch._C._cuda_getDevice():
