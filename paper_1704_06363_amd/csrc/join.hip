@@ -12,7 +12,6 @@
 // gradients of the gains in registers over all of its rows.  A workgroup's sums go to the workspace, and
 // k_join_gains adds them in order.
 #include "primitives.hpp"
-#include "slices.hpp"
 #include "train_launch.hpp"
 
 namespace hmoe {

@@ -399,7 +399,7 @@ __global__ void __launch_bounds__(kRowThreads<P>)
     const int64_t row = first + threadIdx.x / L;
     const bool live = row < n;
     // all of a row's choices before any is looked at: one by one they took a trip to memory each (32768 rows of 128 experts,
-    // four choices: 23 us)
+    // four choices: 23 us, 22 so)
     int chosen[HMOE_ROUTER_EXPERTS];
     float gw[HMOE_ROUTER_EXPERTS];
 #pragma unroll
