@@ -63,7 +63,7 @@ int hmoe_router_forward(const hmoe_router_t* p, int64_t n, const void* X, int32_
  *   scores, expert and counts are the forward's; an expert id outside [0, K) is no choice.  g_weight
  *   float[n][top_k] or NULL (zeros).  dX, dR and dbias may each be NULL.  Experts that are off get zeros, and rows
  *   of nothing else too.  ds is held to fp32's accuracy for dR and dbias, to 2^-16 for dX of bf16 data.
- *   balance and z are finite. */
+ *   balance and z are finite.  dX may not be X with dR. */
 int hmoe_router_backward(const hmoe_router_t* p, int64_t n, const void* X, const float* scores, const int32_t* expert,
                          const int32_t* counts, const float* g_weight, float balance, float z, void* dX, float* dR,
                          float* dbias, void* ws, size_t ws_bytes, void* stream);
@@ -87,7 +87,7 @@ typedef struct {
 } hmoe_join_t;
 
 /* x [n x d], y [n][k][d] (NULL if k = 0), gate float[n][k] or NULL (ones); x_out (x') and h [n x d] out, either
- * may be NULL; x_out may be x.  h is the norm of x' before its rounding.  One pass, sums in fp32, no workspace.
+ * may be NULL; x_out may be x, but not y with k > 1.  h is the norm of x' before its rounding.  One pass, sums in fp32, no workspace.
  * Errors (of both): HMOE_EINVAL, HMOE_ESHAPE (d not a multiple of 8, misaligned rows), HMOE_EDTYPE. */
 int hmoe_join_forward(const hmoe_join_t* p, int64_t n, const void* x, const void* y, const float* gate, void* x_out,
                       void* h, void* stream);
@@ -96,7 +96,8 @@ int hmoe_join_forward(const hmoe_join_t* p, int64_t n, const void* x, const void
  * forward (needed with dh), D = dx_out + the gradient through h's norm at x_out:
  *   dx = scale D;  dy_ij = gate gamma_y D through the norm at y_ij;  dgate[i][j] = D . gamma_y N(y_ij);
  *   dgamma_y = sum_ij gate D N(y_ij), dgamma_h = sum_i dh N(x'_i).
- * dx, dy (dtype dt), dgate, dgamma_y, dgamma_h (float) may each be NULL.  dx may be dx_out or dh, and dy may be y.
+ * dx, dy (dtype dt), dgate, dgamma_y, dgamma_h (float) may each be NULL.  dx may be dx_out or dh, and dy may be
+ * y; other results over inputs are not allowed (HMOE_EINVAL where dx is y, or dy another input with k > 1).
  * dgate, dgamma_y and dy need y (k > 0). */
 size_t hmoe_join_workspace(const hmoe_join_t* p, int64_t n); /* of the backward */
 int hmoe_join_backward(const hmoe_join_t* p, int64_t n, const void* x_out, const void* y, const float* gate,
@@ -130,8 +131,9 @@ int hmoe_orthogonalise(const void* G, hmoe_dtype_t dt, int32_t K, int32_t rows, 
 
 /* One step of K weight matrices with such updates, beside hmoe_sgd_step for vectors:
  *   v = momentum v + g;  U = g + momentum v (nesterov) or v;  w = (1 - lr weight_decay) w - lr scale NS(U).
- * w, v float[K][rows][cols] in/out, g float in; v is not used, and may be NULL, when momentum == 0 (U = g).  w_lo out in dtype dt (the updated
- * weights rounded to nearest even) or NULL.  lr, weight_decay, momentum >= 0, scale finite. */
+ * w, v float[K][rows][cols] in/out, g float in; v is not used, and may be NULL, when momentum == 0 (U = g).
+ * w_lo out in dtype dt (the updated weights rounded to nearest even) or NULL.  v, g and w_lo are not each other, and v and
+ * w_lo not w (HMOE_EINVAL).  lr, weight_decay, momentum >= 0, scale finite. */
 size_t hmoe_muon_workspace(int32_t K, int32_t rows, int32_t cols);
 int hmoe_muon_step(float* w, const float* g, float* v, void* w_lo, hmoe_dtype_t dt, int32_t K, int32_t rows,
                    int32_t cols, float lr, float weight_decay, float momentum, int32_t nesterov, float scale,

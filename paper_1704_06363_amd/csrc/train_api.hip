@@ -83,6 +83,7 @@ int hmoe_router_backward(const hmoe_router_t* p, int64_t n, const void* X, const
     if (dR) HMOE_TRY(check_ptr("X", X));
     HMOE_TRY(check_train_ws(router_ws(p, n), ws_bytes, ws));
     if (!dX && !dR && !dbias) return HMOE_OK;
+    if (dX && dR && dX == X) return fail(HMOE_EINVAL, "dX is X, which dR still reads");
     Workspace w(ws, ws_bytes);
     return launch_router_backward(p, n, X, scores, expert, counts, g_weight, balance, z, dX, dR, dbias, w,
                                   (hipStream_t)stream);
@@ -119,6 +120,7 @@ int hmoe_join_forward(const hmoe_join_t* p, int64_t n, const void* x, const void
   if (h) HMOE_TRY(check_ptr("h", h));
   if (!x_out && !h) return fail(HMOE_EINVAL, "x_out and h are both NULL");
   if (h && (h == x_out || h == x || (p->k > 0 && h == y))) return fail(HMOE_EINVAL, "h overlaps another row");
+  if (p->k > 1 && x_out == y) return fail(HMOE_EINVAL, "x_out is y, rows of which are still read");
   return launch_join_forward(p, n, x, y, gate, x_out, h, (hipStream_t)stream);
 }
 
@@ -145,6 +147,9 @@ int hmoe_join_backward(const hmoe_join_t* p, int64_t n, const void* x_out, const
     if (dy) HMOE_TRY(check_ptr("dy", dy));
     if (dx && dx == dy) return fail(HMOE_EINVAL, "dx and dy are the same");
     HMOE_TRY(check_train_ws(join_ws(p, n), ws_bytes, ws));
+    if (dx && dx == y && (dy || dgate || dgamma_y)) return fail(HMOE_EINVAL, "dx is y, which is still read");
+    if (dy && p->k > 1 && ((dh && dy == x_out) || dy == dx_out || dy == dh))
+      return fail(HMOE_EINVAL, "dy is x_out, dx_out or dh, rows of which are still read");
     Workspace w(ws, ws_bytes);
     return launch_join_backward(p, n, x_out, y, gate, dx_out, dh, dx, dy, dgate, dgamma_y, dgamma_h, w,
                                 (hipStream_t)stream);
@@ -221,6 +226,9 @@ int hmoe_muon_step(float* w, const float* g, float* v, void* w_lo, hmoe_dtype_t 
   if (w_lo) HMOE_TRY(check_ptr("w_lo", w_lo));
   if (w_lo == w) return fail(HMOE_EINVAL, "w_lo is w");
   HMOE_TRY(check_train_ws(ortho_ws(K, rows, cols), ws_bytes, ws));
+  // g is read once more after v is written, and w_lo's matrices are written where others' g and v may be read
+  if (momentum > 0.f && (v == g || v == w)) return fail(HMOE_EINVAL, "v is g or w");
+  if (w_lo && (w_lo == g || (momentum > 0.f && w_lo == v))) return fail(HMOE_EINVAL, "w_lo is g or v");
   OrthoStep s = {};
   s.w = w;
   s.g = g;

@@ -75,6 +75,7 @@ class Lora(ctypes.Structure):
 class Router(ctypes.Structure):
     _fields_ = [("K", ctypes.c_int32), ("d", ctypes.c_int32), ("top_k", ctypes.c_int32), ("dt", ctypes.c_int),
                 ("renorm", ctypes.c_int32), ("R", ctypes.c_void_p), ("bias", ctypes.c_void_p)]
+    device = None  # R's, where make_router made it
 
 
 class Join(ctypes.Structure):
@@ -892,6 +893,7 @@ def make_router(p: dict, top_k: int = 1, renorm: bool = False) -> Router:
     prm = Router(K, d, top_k, _dt(R), 1 if renorm else 0, _arg(R, (K, d), R.dtype, "R"),
                  _arg(bias, (K,), torch.float32, "bias"))
     _same_device(R, bias)
+    prm.device = R.get_device()
     return prm
 
 
@@ -899,6 +901,8 @@ def _router(p, X, top_k, renorm):
     prm = p if isinstance(p, Router) else make_router(p, top_k, renorm)
     if _dt(X) != prm.dt:
         raise HmoeError(f"X: dtype {X.dtype}, the router's expected")
+    if prm.device is not None and prm.device != X.get_device():
+        raise HmoeError(f"router on device {prm.device}, X on {X.get_device()}")
     return prm
 
 

@@ -211,3 +211,35 @@ def test_binding_refusals():
         hmoe.muon_step(X.bfloat16(), X, X)
     with pytest.raises(hmoe.HmoeError, match="GPU"):
         hmoe.muon_step(X, X, X)
+
+
+def test_refuses_results_over_what_is_still_read(lib):
+    big = 1 << 40
+    good = (F * 3)(1.0, 2.0, 3.0)
+    # dX is written before dR reads X
+    rc = lib.hmoe_router_backward(ctypes.byref(router()), 10, 32, 16, 16, 16, 16, F(0.1), F(0.1), 32, 64, 16, 16, big, None)
+    refused(rc, -1, "dX is X")
+    # rows of y that another workgroup still reads
+    rc = lib.hmoe_join_forward(join(k=2), 10, 16, 32, 16, 32, 64, None)
+    refused(rc, -1, "x_out is y")
+
+    def grad(k, dx, dy):
+        return lib.hmoe_join_backward(join(k=k), 10, 256, 32, 16, 512, 1024, dx, dy, 16, 16, 16, 16, big, None)
+    for k in (1, 2):
+        refused(grad(k, 32, 128), -1, "dx is y")
+    for dy in (256, 512, 1024):
+        refused(grad(2, 64, dy), -1, "dy is")
+
+    def step(w, g, v, lo, mu=0.9):
+        return lib.hmoe_muon_step(w, g, v, lo, 1, 2, 16, 24, F(0.1), F(0.1), F(mu), 1, F(1.0), 5, good, 16, big, None)
+    refused(step(16, 32, 32, None), -1, "v is")
+    refused(step(16, 32, 16, None), -1, "v is")
+    refused(step(16, 32, 64, 64), -1, "w_lo is")
+    refused(step(16, 32, 64, 32), -1, "w_lo is")
+
+
+def test_refuses_a_router_of_another_device():
+    prm = router(K=3, d=16, top_k=1, dt=hmoe._DT[torch.float32])
+    prm.device = 1
+    with pytest.raises(hmoe.HmoeError, match="router on device 1"):
+        hmoe._router(prm, torch.zeros(4, 16), 1, False)
