@@ -115,12 +115,12 @@ int hmoe_join_backward(const hmoe_join_t* p, int64_t n, const void* x_out, const
  *   X <- a X + (b A + c A^2) X,  A = X X^T  (X^T X on the other side where rows > cols: the same),
  * (a, b, c) = coef, which takes the singular values s of X to a s + b s^3 + c s^5: with (3.4445, -4.775, 2.0315) five
  * steps bring those in [0.01, 1] to [0.7, 1.2], so that X comes near to the orthogonal factor of U.
- * Iterates are kept as two fp16 numbers a value, 22 bits, and products summed in fp32; a bf16 result may take its last
- * step in one fp16 number a value (at most about 1e-3 relative beside its own rounding).  Two steps may be taken at
- * once, with P = a + b A + c A^2, the next A = P A P and the product of two such P.  Entries of X have to stay below 8
- * in magnitude, those of A, b A + c A^2 and P below 16 and those of products of two of them below 256; larger ones
- * become infinities and NaN.  A matrix with infinities or NaN gives NaN and leaves
- * the others as they are.
+ * Iterates are kept as two fp16 numbers a value, 22 bits, and products summed in fp32, of bf16 data, too, whose result
+ * is that of the same numbers in fp32, rounded.  Two steps may be taken at once, with P = a + b A + c A^2, the next A =
+ * P A P and the product of two such P.  K, rows and cols choose the tiles and how sums are divided among them, and so a
+ * result's last bits.  Entries of X have to stay below 8 in magnitude, those of A, b A + c A^2 and P below 16 and those of
+ * products of two of them below 256; larger ones become infinities and NaN.  A matrix with infinities or NaN gives NaN and
+ * leaves the others as they are.
  * cols is a multiple of 8; 1 <= K <= 4096, 1 <= steps <= HMOE_ORTHO_STEPS, coef: three finite floats on the host.
  * hmoe_orthogonalise: G [K][rows][cols] in dtype dt, O the same out; O may be G.
  * Errors (of both): HMOE_EINVAL, HMOE_ESHAPE (cols not a multiple of 8, misaligned pointer), HMOE_EDTYPE,

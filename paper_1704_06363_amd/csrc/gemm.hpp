@@ -981,9 +981,6 @@ struct PipeTile {
             if constexpr (C::F32)
               c = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(floatx4, b[j][ks])[q],
                                                        __builtin_bit_cast(floatx4, a[i][ks])[q], c, 0, 0, 0);
-            else if constexpr (std::is_same<typename C::type, _Float16>::value)
-              c = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, b[j][ks]),
-                                                         __builtin_bit_cast(f16x8, a[i][ks]), c, 0, 0, 0);
             else
               c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[j][ks], a[i][ks], c, 0, 0, 0);
           }

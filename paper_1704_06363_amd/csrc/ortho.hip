@@ -122,10 +122,10 @@ __global__ void __launch_bounds__(256) k_ortho_split(OrthoStep s, Ortho o, int m
 
 // ------------------------------------------------------------------ the products
 
-// Four or eight (N) values from column c (a multiple of N) of a row, as pairs or as one fp16 number each.
+// Four or eight (N) values from column c (a multiple of N) of a row of pairs.
 template <int N>
 using f16xN = _Float16 __attribute__((ext_vector_type(N)));
-template <bool PAIR, int N>
+template <int N>
 __device__ __forceinline__ void put(f16* row, int c, const float* v) {
   f16xN<N> hi, lo;
 #pragma unroll
@@ -135,18 +135,12 @@ __device__ __forceinline__ void put(f16* row, int c, const float* v) {
     hi[e] = h;
     lo[e] = l;
   }
-  if constexpr (PAIR) {
-    *reinterpret_cast<f16xN<N>*>(row + pair_at(c)) = hi;
-    *reinterpret_cast<f16xN<N>*>(row + pair_at(c) + kPairLo) = lo;
-  } else {
-    *reinterpret_cast<f16xN<N>*>(row + c) = hi;
-  }
+  *reinterpret_cast<f16xN<N>*>(row + pair_at(c)) = hi;
+  *reinterpret_cast<f16xN<N>*>(row + pair_at(c) + kPairLo) = lo;
 }
-template <bool PAIR>
 __device__ __forceinline__ void get8(const f16* row, int c, float (&v)[8]) {
-  const f16x8 hi = *reinterpret_cast<const f16x8*>(row + (PAIR ? pair_at(c) : c));
-  f16x8 lo = {};
-  if constexpr (PAIR) lo = *reinterpret_cast<const f16x8*>(row + pair_at(c) + kPairLo);
+  const f16x8 hi = *reinterpret_cast<const f16x8*>(row + pair_at(c));
+  const f16x8 lo = *reinterpret_cast<const f16x8*>(row + pair_at(c) + kPairLo);
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] = (float)hi[e] + (float)lo[e];
 }
@@ -174,10 +168,8 @@ struct Product {
   floatx4* part;  // [tile][piece][accumulator][thread] of those
 };
 
-// Row stride of a matrix with `width` (padded) columns, and the distance of two matrices, in fp16 numbers.  Whatever
-// they hold, a matrix has its place for pairs.
-template <bool PAIR>
-__device__ __forceinline__ int64_t stride(int width) { return PAIR ? 2 * width : width; }
+// Row stride of a matrix with `width` (padded) columns, in fp16 numbers.
+__device__ __forceinline__ int64_t stride(int width) { return 2 * width; }
 
 template <class C, bool SYM>
 struct ProductTile {
@@ -205,7 +197,7 @@ struct ProductTile {
 // Accumulators (i, 2 h) and (i, 2 h + 1) of a tile stored; LAST: where `s` says.  Lanes 16 apart trade halves of the two
 // blocks of 16 columns, after which each holds eight consecutive columns: 16-byte vectors of hi and of lo.  FULL: the
 // tile has no rows or columns that do not exist, and nothing is behind a branch.
-template <class C, bool SYM, bool OUT_PAIR, bool LAST, bool FULL>
+template <class C, bool SYM, bool LAST, bool FULL>
 __device__ __forceinline__ void product_out(const Ortho& o, const Product& p, const OrthoStep& s,
                                             const ProductTile<C, SYM>& t, const Frag<C>& f, int i, int h, floatx4 a0,
                                             floatx4 a1) {
@@ -221,7 +213,7 @@ __device__ __forceinline__ void product_out(const Ortho& o, const Product& p, co
   }
   if (p.E && (FULL || (row < o.r && col < width))) {
     float x[8];
-    get8<C::PAIR>(p.E + t.m * size + row * stride<C::PAIR>(width), col, x);
+    get8(p.E + t.m * size + row * stride(width), col, x);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = fmaf(p.beta, x[e], v[e]);
   }
@@ -233,7 +225,7 @@ __device__ __forceinline__ void product_out(const Ortho& o, const Product& p, co
       if constexpr (!FULL) v[e] = row < o.r && col + e < cols ? v[e] : 0.f;
     }
     f16* out = p.out + t.m * size;
-    if (FULL || (row < (SYM ? o.r : o.rp) && col < width)) put<OUT_PAIR, 8>(out + row * stride<OUT_PAIR>(width), col, v);
+    if (FULL || (row < (SYM ? o.r : o.rp) && col < width)) put<8>(out + row * stride(width), col, v);
     if constexpr (SYM) {
       if (!t.mirror) return;
 #pragma unroll
@@ -241,7 +233,7 @@ __device__ __forceinline__ void product_out(const Ortho& o, const Product& p, co
         float u[4] = {v[z], v[z + 1], v[z + 2], v[z + 3]};
         quad_transpose(u);  // now of column col + z + lane % 4, rows 4 q .. 4 q + 3 of the 16
         const int tr = col + z + (f.lr & 3), tc = row - (f.lr & 3);
-        if (FULL || tr < o.r) put<OUT_PAIR, 4>(out + tr * stride<OUT_PAIR>(width), tc, u);
+        if (FULL || tr < o.r) put<4>(out + tr * stride(width), tc, u);
       }
     }
   } else {
@@ -262,7 +254,7 @@ __device__ __forceinline__ void product_out(const Ortho& o, const Product& p, co
   }
 }
 // All accumulators of a tile, or (ROWS = 1) those of row i0 alone.
-template <class C, bool SYM, bool OUT_PAIR, bool LAST, int ROWS>
+template <class C, bool SYM, bool LAST, int ROWS>
 __device__ __forceinline__ void product_rows(const Ortho& o, const Product& p, const OrthoStep& s,
                                              const ProductTile<C, SYM>& t, int i0, const floatx4 (&acc)[ROWS][C::NJ]) {
   const Frag<C> f;
@@ -271,7 +263,7 @@ __device__ __forceinline__ void product_rows(const Ortho& o, const Product& p, c
     for (int i = 0; i < ROWS; ++i)
 #pragma unroll
       for (int h = 0; h < C::NJ / 2; ++h)
-        product_out<C, SYM, OUT_PAIR, LAST, decltype(full)::value>(o, p, s, t, f, i0 + i, h, acc[i][2 * h], acc[i][2 * h + 1]);
+        product_out<C, SYM, LAST, decltype(full)::value>(o, p, s, t, f, i0 + i, h, acc[i][2 * h], acc[i][2 * h + 1]);
   };
   if (t.r0 + C::BM <= o.r && t.c0 + C::BN <= (SYM ? o.r : o.l)) rows(std::true_type{});
   else rows(std::false_type{});
@@ -285,7 +277,7 @@ __device__ __forceinline__ int xcd_run(int b, int n) {
   return b < even ? b % 8 * (even / 8) + b / 8 : b;
 }
 
-template <class C, bool SYM, bool OUT_PAIR, bool LAST>
+template <class C, bool SYM, bool LAST>
 __global__ void __launch_bounds__(C::THREADS) k_ortho_product(Ortho o, Product p, OrthoStep s) {
   extern __shared__ __attribute__((aligned(16))) char smem_raw[];
   lds<char>* smem = (lds<char>*)smem_raw;
@@ -293,30 +285,30 @@ __global__ void __launch_bounds__(C::THREADS) k_ortho_product(Ortho o, Product p
   const int b = whole ? xcd_run(blockIdx.x, p.full) : p.full + xcd_run(blockIdx.x - p.full, gridDim.x - p.full);
   const int q = b - p.full;
   const ProductTile<C, SYM> t(o, p, q < 0 ? b : p.full + q / p.split);
-  constexpr int kStage = C::PAIR ? C::BK / 2 : C::BK;  // of the reduction
+  constexpr int kStage = C::BK / 2;  // of the reduction
   const int stages = (p.k + kStage - 1) / kStage, piece = q < 0 ? 0 : q % p.split, pieces = q < 0 ? 1 : p.split;
   const int k0 = stages * piece / pieces * kStage, to = stages * (piece + 1) / pieces * kStage;
   const int k_len = (to < p.k ? to : p.k) - k0;
-  const int64_t ldk = stride<C::PAIR>(p.k);
-  const f16* L = p.L + t.m * p.step + t.r0 * ldk + stride<C::PAIR>(k0);
+  const int64_t ldk = stride(p.k);
+  const f16* L = p.L + t.m * p.step + t.r0 * ldk + stride(k0);
   const int rows = o.r - t.r0 < C::BM ? o.r - t.r0 : C::BM;
   floatx4 acc[C::MI][C::NJ];
   if constexpr (SYM) {
     const int cols = o.r - t.c0 < C::BN ? o.r - t.c0 : C::BN;
-    const f16* R = p.R + t.m * p.step + t.c0 * ldk + stride<C::PAIR>(k0);
+    const f16* R = p.R + t.m * p.step + t.c0 * ldk + stride(k0);
     PipeTile<C, true, true> g;
-    g.prime(reinterpret_cast<const bf16*>(L), ldk, rows, reinterpret_cast<const bf16*>(R), ldk, cols, (int)stride<C::PAIR>(k_len), smem);
+    g.prime(reinterpret_cast<const bf16*>(L), ldk, rows, reinterpret_cast<const bf16*>(R), ldk, cols, (int)stride(k_len), smem);
     g.run(smem, acc);
   } else {
     const int cols = o.lp - t.c0 < C::BN ? o.lp - t.c0 : C::BN;
-    const int64_t ld = stride<C::PAIR>(o.lp);
-    const f16* R = p.R + t.m * o.x_size() + k0 * ld + stride<C::PAIR>(t.c0);
+    const int64_t ld = stride(o.lp);
+    const f16* R = p.R + t.m * o.x_size() + k0 * ld + stride(t.c0);
     PipeTile<C, true, false> g;
-    g.prime(reinterpret_cast<const bf16*>(L), ldk, rows, reinterpret_cast<const bf16*>(R), ld, cols, (int)stride<C::PAIR>(k_len), smem);
+    g.prime(reinterpret_cast<const bf16*>(L), ldk, rows, reinterpret_cast<const bf16*>(R), ld, cols, (int)stride(k_len), smem);
     g.run(smem, acc);
   }
   if (q < 0) {
-    product_rows<C, SYM, OUT_PAIR, LAST, C::MI>(o, p, s, t, 0, acc);
+    product_rows<C, SYM, LAST, C::MI>(o, p, s, t, 0, acc);
   } else {
     floatx4* to = p.part + (int64_t)q * C::MI * C::NJ * C::THREADS + threadIdx.x;
 #pragma unroll
@@ -438,7 +430,7 @@ __global__ void __launch_bounds__(256) k_ortho_mid(Ortho o, Product p, OrthoStep
     __syncthreads();  // before the loads of the trip after the next
   }
   if (q < 0) {
-    product_rows<C, SYM, true, LAST, 2>(o, p, s, t, 0, acc);
+    product_rows<C, SYM, LAST, 2>(o, p, s, t, 0, acc);
   } else {
     floatx4* to = p.part + (int64_t)q * 4 * 256 + threadIdx.x;
 #pragma unroll
@@ -449,7 +441,7 @@ __global__ void __launch_bounds__(256) k_ortho_mid(Ortho o, Product p, OrthoStep
 }
 
 // The pieces of the tiles that are split added in order, and their results: blockIdx.y names the accumulators' row.
-template <class C, bool SYM, bool OUT_PAIR, bool LAST>
+template <class C, bool SYM, bool LAST>
 __global__ void __launch_bounds__(C::THREADS) k_ortho_join(Ortho o, Product p, OrthoStep s) {
   const ProductTile<C, SYM> t(o, p, p.full + blockIdx.x);
   const int i = blockIdx.y;
@@ -461,28 +453,20 @@ __global__ void __launch_bounds__(C::THREADS) k_ortho_join(Ortho o, Product p, O
   for (int q = 0; q < p.split; ++q)
 #pragma unroll
     for (int j = 0; j < C::NJ; ++j) acc[0][j] += from[((int64_t)q * C::MI * C::NJ + j) * C::THREADS];
-  product_rows<C, SYM, OUT_PAIR, LAST, 1>(o, p, s, t, i, acc);
+  product_rows<C, SYM, LAST, 1>(o, p, s, t, i, acc);
 }
 
 // Tiles: 256 x 256 of eight waves, or 128 x 128 and 128 x 256 (the swizzle of a K-strided operand spans 256 columns).
-template <bool PAIR, bool LARGE, bool SYM>
+template <bool LARGE, bool SYM>
 struct PickTile;
 template <>
-struct PickTile<true, true, true> { using C = CfgPair<256, 256, 128, 64, false>; };
+struct PickTile<true, true> { using C = CfgPair<256, 256, 128, 64, false>; };
 template <>
-struct PickTile<true, true, false> { using C = CfgPair<256, 256, 128, 64, true>; };
+struct PickTile<true, false> { using C = CfgPair<256, 256, 128, 64, true>; };
 template <>
-struct PickTile<true, false, true> { using C = CfgPair<128, 128, 64, 64, false>; };
+struct PickTile<false, true> { using C = CfgPair<128, 128, 64, 64, false>; };
 template <>
-struct PickTile<true, false, false> { using C = CfgPair<128, 256, 64, 64, true>; };
-template <>
-struct PickTile<false, true, true> { using C = CfgP<f16, 256, 256, 128, 64, false>; };
-template <>
-struct PickTile<false, true, false> { using C = CfgP<f16, 256, 256, 128, 64, true>; };
-template <>
-struct PickTile<false, false, true> { using C = CfgP<f16, 128, 128, 64, 64, false>; };
-template <>
-struct PickTile<false, false, false> { using C = CfgP<f16, 128, 256, 64, 64, true>; };
+struct PickTile<false, false> { using C = CfgPair<128, 256, 64, 64, true>; };
 
 // How the tiles of a product are dealt out.  Whole rounds of the CUs take a tile each; the tiles of the last round, if
 // two or more workgroups are there for each, share their reductions, four stages at least to a piece.
@@ -530,65 +514,60 @@ bool is_mid(const Ortho& o) {
   const int64_t mt = cdiv(o.r, 128);
   return o.r <= 512 && mt * (mt + 1) / 2 * o.K < device_cus() / 4;
 }
-// pairs: k_ortho_mid can be taken -- for symmetric products of larger matrices, too, whose tiles all run at once (1024 x
-// 1024 in pieces of 128 x 128 tiles: 14 us, and 7 to join them).
-Deal deal(const Ortho& o, int k, bool sym, bool pairs) {
-  if (pairs && is_mid(o)) return deal_mid(o, k, sym);
+// k_ortho_mid also takes the symmetric products of larger matrices whose tiles all run at once (1024 x 1024 in pieces of
+// 128 x 128 tiles: 14 us, and 7 to join them).
+Deal deal(const Ortho& o, int k, bool sym) {
+  if (is_mid(o)) return deal_mid(o, k, sym);
   const int64_t m64 = cdiv(o.r, 64);
-  if (pairs && sym && k == o.rp && m64 * (m64 + 1) / 2 * o.K <= device_cus()) return deal_mid(o, k, sym);
-  using L = PickTile<true, true, true>::C;
+  if (sym && k == o.rp && m64 * (m64 + 1) / 2 * o.K <= device_cus()) return deal_mid(o, k, sym);
+  using L = PickTile<true, true>::C;
   const int64_t mt = cdiv(o.r, L::BM), tiles = (sym ? mt * (mt + 1) / 2 : mt * cdiv(o.lp, L::BN)) * o.K;
   // enough work for the large tiles: pieces of sixteen stages on every CU
   const bool large = tiles * (k / 32) / 16 >= device_cus();
   Deal d = large ? deal_on<L>(o, k, sym)
-                 : sym ? deal_on<PickTile<true, false, true>::C>(o, k, sym) : deal_on<PickTile<true, false, false>::C>(o, k, sym);
+                 : sym ? deal_on<PickTile<false, true>::C>(o, k, sym) : deal_on<PickTile<false, false>::C>(o, k, sym);
   d.large = large;
   d.mid = false;
   return d;
 }
 
-template <class C, bool SYM, bool OUT_PAIR, bool LAST>
+template <class C, bool SYM, bool LAST>
 int product_on(const Ortho& o, Product p, const Deal& d, const OrthoStep& s, hipStream_t st) {
   p.per = d.per;
   p.full = d.full;
   p.split = d.split;
-  HMOE_LAUNCH(SYM ? "ortho square" : "ortho apply", (k_ortho_product<C, SYM, OUT_PAIR, LAST>),
+  HMOE_LAUNCH(SYM ? "ortho square" : "ortho apply", (k_ortho_product<C, SYM, LAST>),
               dim3((unsigned)(d.full + d.rest * d.split)), dim3(C::THREADS), C::LDS, st, o, p, s);
   if (d.rest)
-    HMOE_LAUNCH("ortho join", (k_ortho_join<C, SYM, OUT_PAIR, LAST>), dim3(d.rest, C::MI), dim3(C::THREADS), 0, st, o, p, s);
+    HMOE_LAUNCH("ortho join", (k_ortho_join<C, SYM, LAST>), dim3(d.rest, C::MI), dim3(C::THREADS), 0, st, o, p, s);
   return HMOE_OK;
 }
-// Factors and results as pairs, or (fp16 numbers alone) as said.
-template <bool PAIR, bool SYM, bool OUT_PAIR, bool LAST = false>
+template <bool SYM, bool LAST = false>
 int product(const Ortho& o, const Product& p, const OrthoStep& s, hipStream_t st) {
-  const Deal d = deal(o, p.k, SYM, PAIR && OUT_PAIR);
-  if constexpr (PAIR && OUT_PAIR) {
-    if (d.mid) {
-      Product m = p;
-      m.per = d.per;
-      m.full = d.full;
-      m.split = d.split;
-      HMOE_LAUNCH(SYM ? "ortho square" : "ortho apply", (k_ortho_mid<SYM, LAST>), dim3((unsigned)(d.full + d.rest * d.split)),
-                  dim3(CfgMid::THREADS), CfgMid::LDS, st, o, m, s);
-      if (d.rest)
-        HMOE_LAUNCH("ortho join", (k_ortho_join<CfgMid, SYM, true, LAST>), dim3(d.rest, CfgMid::MI), dim3(CfgMid::THREADS), 0,
-                    st, o, m, s);
-      return HMOE_OK;
-    }
+  const Deal d = deal(o, p.k, SYM);
+  if (d.mid) {
+    Product m = p;
+    m.per = d.per;
+    m.full = d.full;
+    m.split = d.split;
+    HMOE_LAUNCH(SYM ? "ortho square" : "ortho apply", (k_ortho_mid<SYM, LAST>), dim3((unsigned)(d.full + d.rest * d.split)),
+                dim3(CfgMid::THREADS), CfgMid::LDS, st, o, m, s);
+    if (d.rest)
+      HMOE_LAUNCH("ortho join", (k_ortho_join<CfgMid, SYM, LAST>), dim3(d.rest, CfgMid::MI), dim3(CfgMid::THREADS), 0, st, o,
+                  m, s);
+    return HMOE_OK;
   }
-  if (d.large) return product_on<typename PickTile<PAIR, true, SYM>::C, SYM, OUT_PAIR, LAST>(o, p, d, s, st);
-  return product_on<typename PickTile<PAIR, false, SYM>::C, SYM, OUT_PAIR, LAST>(o, p, d, s, st);
+  if (d.large) return product_on<typename PickTile<true, SYM>::C, SYM, LAST>(o, p, d, s, st);
+  return product_on<typename PickTile<false, SYM>::C, SYM, LAST>(o, p, d, s, st);
 }
 
 size_t part_size(const Ortho& o) {
   size_t most = 0;
-  for (const bool pairs : {false, true})
-    for (const Deal& d : {deal(o, o.lp, true, pairs), deal(o, o.rp, true, pairs), deal(o, o.rp, false, pairs)})
-      most = d.part > most ? d.part : most;
+  for (const Deal& d : {deal(o, o.lp, true), deal(o, o.rp, true), deal(o, o.rp, false)}) most = d.part > most ? d.part : most;
   return most;
 }
 
-// The steps of one call: X in one of two buffers, the small matrices in four.
+// The steps of one call: X in one of two buffers, the small matrices in three.
 struct Iterations {
   const Ortho& o;
   const OrthoSpace& w;
@@ -601,41 +580,36 @@ struct Iterations {
     const bool of_x = L == w.X[at];
     return Product{L, R, E, out, alpha, beta, diag, of_x ? o.lp : o.rp, of_x ? o.x_size() : o.a_size(), 0, 0, 1, w.part4};
   }
-  template <bool PAIR>
   int gram(f16* A) {
-    return product<PAIR, true, PAIR>(o, make(w.X[at], w.X[at], nullptr, A, kScaleA / (kScaleX * kScaleX), 0.f, 0.f), s, st);
+    return product<true>(o, make(w.X[at], w.X[at], nullptr, A, kScaleA / (kScaleX * kScaleX), 0.f, 0.f), s, st);
   }
   // diag + b A + c A^2
-  template <bool PAIR>
   int poly(const f16* A, float diag, f16* P) {
-    return product<PAIR, true, PAIR>(o, make(A, A, A, P, c / kScaleA, b, diag * kScaleA), s, st);
+    return product<true>(o, make(A, A, A, P, c / kScaleA, b, diag * kScaleA), s, st);
   }
   int times(const f16* L, const f16* R, float scale, f16* out) {
-    return product<true, true, true>(o, make(L, R, nullptr, out, scale, 0.f, 0.f), s, st);
+    return product<true>(o, make(L, R, nullptr, out, scale, 0.f, 0.f), s, st);
   }
-  // X = x X + Q X with Q stored times `scale`; OUT_PAIR: as pairs again
-  template <bool PAIR, bool OUT_PAIR>
+  // X = x X + Q X with Q stored times `scale`
   int apply(const f16* Q, float scale, float x, bool last) {
     const float unit = last ? 1.f / kScaleX : 1.f;
     const Product p = make(Q, w.X[at], x != 0.f ? w.X[at] : nullptr, w.X[1 - at], unit / scale, unit * x, 0.f);
     at = 1 - at;
-    return last ? product<PAIR, false, OUT_PAIR, true>(o, p, s, st) : product<PAIR, false, OUT_PAIR>(o, p, s, st);
+    return last ? product<false, true>(o, p, s, st) : product<false>(o, p, s, st);
   }
-  template <bool PAIR, bool OUT_PAIR>
   int one(bool last) {
-    HMOE_TRY(gram<PAIR>(w.A[0]));
-    HMOE_TRY(poly<PAIR>(w.A[0], 0.f, w.A[1]));
-    return apply<PAIR, OUT_PAIR>(w.A[1], kScaleA, a, last);
+    HMOE_TRY(gram(w.A[0]));
+    HMOE_TRY(poly(w.A[0], 0.f, w.A[1]));
+    return apply(w.A[1], kScaleA, a, last);
   }
-  template <bool OUT_PAIR>
   int two(bool last) {
-    HMOE_TRY(gram<true>(w.A[0]));
-    HMOE_TRY(poly<true>(w.A[0], a, w.A[1]));                          // P
-    HMOE_TRY(times(w.A[1], w.A[0], 1.f / kScaleA, w.A[2]));           // P A
-    HMOE_TRY(times(w.A[2], w.A[1], 1.f / kScaleA, w.A[0]));           // P A P, the next A
-    HMOE_TRY(poly<true>(w.A[0], a, w.A[2]));                          // P'
+    HMOE_TRY(gram(w.A[0]));
+    HMOE_TRY(poly(w.A[0], a, w.A[1]));                                       // P
+    HMOE_TRY(times(w.A[1], w.A[0], 1.f / kScaleA, w.A[2]));                  // P A
+    HMOE_TRY(times(w.A[2], w.A[1], 1.f / kScaleA, w.A[0]));                  // P A P, the next A
+    HMOE_TRY(poly(w.A[0], a, w.A[2]));                                       // P'
     HMOE_TRY(times(w.A[2], w.A[1], kScaleQ / (kScaleA * kScaleA), w.A[0]));  // P' P
-    return apply<true, OUT_PAIR>(w.A[0], kScaleQ, 0.f, last);
+    return apply(w.A[0], kScaleQ, 0.f, last);
   }
 };
 
@@ -662,7 +636,6 @@ int launch_ortho(const OrthoStep& s, int32_t K, int32_t rows, int32_t cols, int3
   if (small_ortho_ws(o) > 0) return launch_small_ortho(s, o, steps, coef, ws, st);
   const OrthoSpace w = ortho_carve(o, part_size(o), ws);
   HMOE_TRY(launch_ortho_start(s, o, w.part, st));
-  const bool low = s.G && s.dt == HMOE_BF16 && !is_mid(o), single_first = low && steps == 1;
   const int64_t parts = cdiv(o.rp, 64) * cdiv(o.lp, 64);
   HMOE_TRY(over_slices(K, parts, 256, [&](int64_t m0, int64_t count) {
     HMOE_LAUNCH("ortho split", k_ortho_split, dim3((unsigned)parts, (unsigned)count), dim3(256), 0, st, s, o, (int)m0,
@@ -672,21 +645,13 @@ int launch_ortho(const OrthoStep& s, int32_t K, int32_t rows, int32_t cols, int3
   Iterations it{o, w, s, st, coef[0], coef[1], coef[2]};
   // Two steps at once where that is less work.  What rounding leaves in A is amplified by a^2 on its way into the
   // second one's, so the first step of all, where the smallest singular values are, is taken alone (rank 3, five
-  // steps: 1.0e-4 with the first two together, 6.9e-5 so, 5.0e-5 with none, fp32 products 4.6e-5).  A
-  // result of bf16 takes its last step in single fp16 numbers, whose noise nothing amplifies any more (rank 3:
-  // 1.4e-4, at most 1e-3 beside the 1.7e-3 of the rounding itself), at a third of the instructions.
+  // steps: 1.0e-4 with the first two together, 6.9e-5 so, 5.0e-5 with none, fp32 products 4.6e-5).
   const bool twos = 2 * o.l >= 3 * o.r;
-  const int pairs_end = low && !single_first ? steps - 1 : steps;
-  int i = 0;
-  while (i < pairs_end) {
-    const bool two = twos && pairs_end - i >= 2 && (i > 0 || low);
-    const int n = two ? 2 : 1;
-    const bool last = i + n == steps, to_single = low && i + n == pairs_end && !last;
-    if (two) HMOE_TRY(to_single ? it.two<false>(last) : it.two<true>(last));
-    else HMOE_TRY((to_single ? it.one<true, false>(last) : it.one<true, true>(last)));
+  for (int i = 0; i < steps;) {
+    const int n = twos && i > 0 && steps - i >= 2 ? 2 : 1;
+    HMOE_TRY(n == 2 ? it.two(i + n == steps) : it.one(i + n == steps));
     i += n;
   }
-  if (i < steps) HMOE_TRY((it.one<false, false>(true)));
   return HMOE_OK;
 }
 
