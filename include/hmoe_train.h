@@ -62,7 +62,7 @@ int hmoe_router_forward(const hmoe_router_t* p, int64_t n, const void* X, int32_
  *   dX = ds R (dtype dt), dR = ds^T X, dbias = sum_i ds_i (float).
  *   scores, expert and counts are the forward's; an expert id outside [0, K) is no choice.  g_weight
  *   float[n][top_k] or NULL (zeros).  dX, dR and dbias may each be NULL.  Experts that are off get zeros, and rows
- *   of nothing else too.  ds is held to fp32's accuracy for dR and dbias, to 2^-16 for dX of bf16 data.
+ *   of nothing else too.  ds is held to fp32's accuracy.
  *   balance and z are finite.  dX may not be X with dR. */
 int hmoe_router_backward(const hmoe_router_t* p, int64_t n, const void* X, const float* scores, const int32_t* expert,
                          const int32_t* counts, const float* g_weight, float balance, float z, void* dX, float* dR,

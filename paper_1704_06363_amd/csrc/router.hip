@@ -6,8 +6,8 @@
 // Bound by HBM: X is read for the scores and for dR, and dX written; the scores (K values a row) lie
 // between.  The products are narrow (K columns, or a reduction over K).  ds is fp32 and keeps its accuracy on
 // the matrix cores: with bf16 data a value is kept as three bf16 numbers that add up to it, a row's in three planes,
-// [values, their remainders, the remainders of those][experts, padded to 16].  The first two against R taken twice
-// give dX to 2^-16, rounded to bf16 once; dR takes all three.
+// [values, their remainders, the remainders of those][experts, padded to 16], and both dX and dR take all three, against R
+// or X taken three times; dX is rounded to bf16 once.
 #include "fewrows.hpp"
 #include "gemm.hpp"
 #include "primitives.hpp"
@@ -482,7 +482,8 @@ __global__ void __launch_bounds__(kRowThreads<P>)
 
 // ------------------------------------------------------------------ the products
 
-// dX = ds R: 64 rows and 256 columns to a workgroup, 64 columns to a wave; fragments straight from memory.
+// dX = ds R: 64 rows and 256 columns to a workgroup, 64 columns to a wave; fragments straight from memory.  bf16, 16
+// experts to a step: the last remainders, then values and remainders against the rows of R taken twice.
 template <typename T>
 __global__ void __launch_bounds__(256) k_router_dx(const T* __restrict__ ds, const T* __restrict__ Rt, int64_t n, int K,
                                                    int d, T* __restrict__ dX) {
@@ -500,16 +501,24 @@ __global__ void __launch_bounds__(256) k_router_dx(const T* __restrict__ ds, con
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int64_t row = m0 + 16 * i + lr < n ? m0 + 16 * i + lr : n - 1;
-    a[i] = ds + row * ld + (sizeof(T) == 2 ? (lg >> 1) * kp + 8 * (lg & 1) : 4 * lg);
+    a[i] = ds + row * ld + (sizeof(T) == 2 ? 8 * (lg & 1) : 4 * lg);
     const int col = c0 + 16 * i + lr < d ? c0 + 16 * i + lr : d - 1;
     b[i] = Rt + (int64_t)col * kp + (sizeof(T) == 2 ? 8 * (lg & 1) : 4 * lg);
   }
-  for (int kb = 0; kb < kp / 16; ++kb) {
-    i32x4 av[4], bv[4];
+  for (int e0 = 0; e0 < kp; e0 += 16) {
+    i32x4 av[4], bv[4], last[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      av[i] = *reinterpret_cast<const i32x4*>(a[i] + kb * 16);
-      bv[i] = *reinterpret_cast<const i32x4*>(b[i] + kb * 16);
+      av[i] = *reinterpret_cast<const i32x4*>(a[i] + e0 + (sizeof(T) == 2 ? (lg >> 1) * kp : 0));
+      bv[i] = *reinterpret_cast<const i32x4*>(b[i] + e0);
+      last[i] = i32x4{0, 0, 0, 0};
+      if (sizeof(T) == 2 && lg < 2) last[i] = *reinterpret_cast<const i32x4*>(a[i] + e0 + 2 * kp);
+    }
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) step_mfma<T>(lg < 2 ? bv[j] : i32x4{0, 0, 0, 0}, last[i], acc[i][j]);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -547,17 +556,17 @@ __global__ void __launch_bounds__(256) k_router_dx(const T* __restrict__ ds, con
   }
 }
 
-// dX = ds R on the engine's tiles, the reduction over the first two planes: for more experts than the narrow form holds.
+// dX = ds R on the engine's tiles, the reduction over the planes: for more experts than the narrow form holds.
 template <class C>
 __global__ void __launch_bounds__(C::THREADS)
     k_router_dx_wide(const bf16* __restrict__ ds, const bf16* __restrict__ Rt, int64_t n, int K, int d, bf16* __restrict__ dX) {
   extern __shared__ __attribute__((aligned(16))) char smem_raw[];
   lds<char>* smem = (lds<char>*)smem_raw;
-  const int ld = ds_width<bf16>(K), k = 2 * padded(K);
+  const int k = ds_width<bf16>(K);
   const TileCoord tc = tile_plain<C>(n, d, k);
   if (!tc.valid) return;
   floatx4 acc[C::MI][C::NJ];
-  gemm_tile<C, true, true>(ds + tc.m0 * ld, ld, tc.m_rows, Rt + (int64_t)tc.n0 * k, k, tc.n_cols, k, smem, acc);
+  gemm_tile<C, true, true>(ds + tc.m0 * k, k, tc.m_rows, Rt + (int64_t)tc.n0 * k, k, tc.n_cols, k, smem, acc);
   store_out<C, bf16>(tc, acc, smem, dX, d, [](int, int, int, float v) { return v; }, RowId{tc.m0}, NoVec{});
 }
 
@@ -720,7 +729,7 @@ RouterSpace router_carve(const hmoe_router_t* p, int64_t n, Workspace& ws) {
   const int pieces = router_pieces(n, p->K, p->d);
   s.planes = pieces > 1 ? ws.take<float>((size_t)pieces * n * p->K) : nullptr;
   s.ds = ws.take<T>((size_t)n * ds_width<T>(p->K));
-  s.Rt = ws.take<T>((size_t)p->d * padded(p->K) * (router_wide<T>(p->K) ? 2 : 1));
+  s.Rt = ws.take<T>((size_t)p->d * padded(p->K) * (router_wide<T>(p->K) ? kParts : 1));
   s.part = ws.take<float>((size_t)cdiv(n, router_piece<T>(n, p->K, p->d)) * (router_wide<T>(p->K) ? ds_width<T>(p->K) : p->K) * p->d);
   return s;
 }
@@ -786,7 +795,7 @@ int router_backward_t(const hmoe_router_t* p, int64_t n, const void* X, const fl
   T* ds = (T*)w.ds;
   constexpr bool BF = sizeof(T) == 2;
   const bool wide = router_wide<T>(K), engine = wide && n > 256;
-  const Transposed<T> t = {(const T*)p->R, (T*)w.Rt, d, dX ? (engine ? 2 : 1) : 0};
+  const Transposed<T> t = {(const T*)p->R, (T*)w.Rt, d, dX ? (engine ? kParts : 1) : 0};
   const int turning = dX ? (int)cdiv(d, 64) * (padded(K) / 16) : 0;
   HMOE_TRY(router_lanes(K, [&](auto l, auto per) {
     constexpr int L = decltype(l)::value, P = decltype(per)::value;
