@@ -77,7 +77,8 @@ int hmoe_router_backward(const hmoe_router_t* p, int64_t n, const void* X, const
  *   x'_i = scale x_i + sum_{j < k} gate[i][j] gamma_y N(y_ij)     (norm_y = 0: y_ij itself instead of N(y_ij))
  *   h_i  = gamma_h N(x'_i)
  * k rows of y belong to a sample: one for a dense layer, those of its experts (0 <= k <= HMOE_JOIN_ROWS).  d is a
- * multiple of 8 up to HMOE_JOIN_WIDTH; gamma_y, gamma_h [d] in dtype dt or NULL (ones); eps > 0. */
+ * multiple of 8 up to HMOE_JOIN_WIDTH; gamma_y, gamma_h [d] in dtype dt or NULL (ones); eps >= 2^-126, the
+ * smallest normal number. */
 typedef struct {
   int32_t d, k;
   hmoe_dtype_t dt;

@@ -1,5 +1,6 @@
 // train_api.hip -- the extern "C" entry points of include/hmoe_train.h: argument validation, workspace
 // checks and dispatch to the launchers.  Host code only.
+#include <float.h>
 #include <math.h>
 
 #include "checks.hpp"
@@ -103,7 +104,9 @@ static int check_join(const hmoe_join_t* p, int64_t n) {
   if (p->d > HMOE_JOIN_WIDTH) return fail(HMOE_EINVAL, "d = %d exceeds %d", p->d, HMOE_JOIN_WIDTH);
   if (p->k < 0 || p->k > HMOE_JOIN_ROWS) return fail(HMOE_EINVAL, "k = %d outside [0, %d]", p->k, HMOE_JOIN_ROWS);
   HMOE_TRY(check_finite("scale", p->scale));
-  if (!(p->eps > 0.f) || !isfinite(p->eps)) return fail(HMOE_EINVAL, "eps = %g is not positive", (double)p->eps);
+  // below them 1 / eps, the square of a row of zeros' factor, is past fp32
+  if (!(p->eps >= FLT_MIN) || !isfinite(p->eps))
+    return fail(HMOE_EINVAL, "eps = %g is not positive and normal", (double)p->eps);
   if (p->gamma_y) HMOE_TRY(check_ptr("gamma_y", p->gamma_y));
   if (p->gamma_h) HMOE_TRY(check_ptr("gamma_h", p->gamma_h));
   return check_n(n);
