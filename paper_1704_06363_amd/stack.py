@@ -1,11 +1,12 @@
 """Layers of adapters whose routers learn, trained: a residual stack in which every sample goes to the experts that a
 layer's router chooses for it, each of them a low-rank adapter beside the layer's shared projection.
 
-  layer      h -> the router's choices and weights (router_forward) -> rows by expert (moe_dispatch) -> projection with
-             the expert's adapter (lora_forward) -> norm, gate by the weights, residual and the norm before the
-             next layer (join_forward)
+  layer      h -> the router's choices and weights (router_forward) -> rows by expert (moe_dispatch; torch copies them
+             first for more than one choice) -> projection with the expert's adapter (lora_forward) -> norm, gate by
+             the weights, residual and the norm before the next layer (join_forward)
   gradients  of the mean of -ln p(tag) (token_logprob over a shared decoder) plus the routers' balance and z losses:
-             token_logprob_backward, lora_backward, join_backward, router_backward, layer by layer
+             token_logprob_backward, lora_backward, join_backward, router_backward, layer by layer; join_forward adds up
+             what comes back to a layer's input
   step       orthogonalised updates (muon_step) of the adapters and the routers' rows, sgd_step for gains and biases
 
     python -m paper_1704_06363_amd.stack [--steps N] [--dtype bf16]
@@ -88,7 +89,8 @@ class Stack:
             r = hmoe.router_backward(router, c["h"], c["router"], b["dgate"], balance, z, renorm=k > 1)
             g.update({f"A{i}": e["dA"], f"B{i}": e["dB"], f"R{i}": r["dR"], f"bias{i}": r["dbias"],
                       f"gamma_y{i}": b["dgamma_y"], f"gamma_h{i}": b["dgamma_h"]})
-            dx, dh = b["dx"], r["dX"] + e["dX"].view(n, k, -1).sum(1)
+            # what comes back from the router and from every choice, in 32 bits and rounded once
+            dx, dh = b["dx"], hmoe.join_forward(r["dX"], e["dX"].view(n, k, -1), norm_y=False, want_h=False)["x"]
         g["gamma"] = hmoe.join_backward(X, gamma_h=p["gamma"], dh=dh, want=("dgamma_h",))["dgamma_h"]
         return t["logp"], [c["router"]["loss"] for c in kept], g
 
