@@ -531,34 +531,42 @@ Deal deal(const Ortho& o, int k, bool sym) {
   return d;
 }
 
+// What a product is, and by the height of its tiles what its launch is called.
+enum Kind { kGram, kSquare, kApply };
+const char* label_of(Kind what, int height) {
+  static const char* const names[3][3] = {{"ortho gram 64", "ortho gram 128", "ortho gram 256"},
+                                          {"ortho square 64", "ortho square 128", "ortho square 256"},
+                                          {"ortho apply 64", "ortho apply 128", "ortho apply 256"}};
+  return names[what][height / 128];
+}
 template <class C, bool SYM, bool LAST>
-int product_on(const Ortho& o, Product p, const Deal& d, const OrthoStep& s, hipStream_t st) {
+int product_on(Kind what, const Ortho& o, Product p, const Deal& d, const OrthoStep& s, hipStream_t st) {
   p.per = d.per;
   p.full = d.full;
   p.split = d.split;
-  HMOE_LAUNCH(SYM ? "ortho square" : "ortho apply", (k_ortho_product<C, SYM, LAST>),
+  HMOE_LAUNCH(label_of(what, C::BM), (k_ortho_product<C, SYM, LAST>),
               dim3((unsigned)(d.full + d.rest * d.split)), dim3(C::THREADS), C::LDS, st, o, p, s);
   if (d.rest)
     HMOE_LAUNCH("ortho join", (k_ortho_join<C, SYM, LAST>), dim3(d.rest, C::MI), dim3(C::THREADS), 0, st, o, p, s);
   return HMOE_OK;
 }
 template <bool SYM, bool LAST = false>
-int product(const Ortho& o, const Product& p, const OrthoStep& s, hipStream_t st) {
+int product(Kind what, const Ortho& o, const Product& p, const OrthoStep& s, hipStream_t st) {
   const Deal d = deal(o, p.k, SYM);
   if (d.mid) {
     Product m = p;
     m.per = d.per;
     m.full = d.full;
     m.split = d.split;
-    HMOE_LAUNCH(SYM ? "ortho square" : "ortho apply", (k_ortho_mid<SYM, LAST>), dim3((unsigned)(d.full + d.rest * d.split)),
+    HMOE_LAUNCH(label_of(what, CfgMid::BM), (k_ortho_mid<SYM, LAST>), dim3((unsigned)(d.full + d.rest * d.split)),
                 dim3(CfgMid::THREADS), CfgMid::LDS, st, o, m, s);
     if (d.rest)
       HMOE_LAUNCH("ortho join", (k_ortho_join<CfgMid, SYM, LAST>), dim3(d.rest, CfgMid::MI), dim3(CfgMid::THREADS), 0, st, o,
                   m, s);
     return HMOE_OK;
   }
-  if (d.large) return product_on<typename PickTile<true, SYM>::C, SYM, LAST>(o, p, d, s, st);
-  return product_on<typename PickTile<false, SYM>::C, SYM, LAST>(o, p, d, s, st);
+  if (d.large) return product_on<typename PickTile<true, SYM>::C, SYM, LAST>(what, o, p, d, s, st);
+  return product_on<typename PickTile<false, SYM>::C, SYM, LAST>(what, o, p, d, s, st);
 }
 
 size_t part_size(const Ortho& o) {
@@ -581,21 +589,21 @@ struct Iterations {
     return Product{L, R, E, out, alpha, beta, diag, of_x ? o.lp : o.rp, of_x ? o.x_size() : o.a_size(), 0, 0, 1, w.part4};
   }
   int gram(f16* A) {
-    return product<true>(o, make(w.X[at], w.X[at], nullptr, A, kScaleA / (kScaleX * kScaleX), 0.f, 0.f), s, st);
+    return product<true>(kGram, o, make(w.X[at], w.X[at], nullptr, A, kScaleA / (kScaleX * kScaleX), 0.f, 0.f), s, st);
   }
   // diag + b A + c A^2
   int poly(const f16* A, float diag, f16* P) {
-    return product<true>(o, make(A, A, A, P, c / kScaleA, b, diag * kScaleA), s, st);
+    return product<true>(kSquare, o, make(A, A, A, P, c / kScaleA, b, diag * kScaleA), s, st);
   }
   int times(const f16* L, const f16* R, float scale, f16* out) {
-    return product<true>(o, make(L, R, nullptr, out, scale, 0.f, 0.f), s, st);
+    return product<true>(kSquare, o, make(L, R, nullptr, out, scale, 0.f, 0.f), s, st);
   }
   // X = x X + Q X with Q stored times `scale`
   int apply(const f16* Q, float scale, float x, bool last) {
     const float unit = last ? 1.f / kScaleX : 1.f;
     const Product p = make(Q, w.X[at], x != 0.f ? w.X[at] : nullptr, w.X[1 - at], unit / scale, unit * x, 0.f);
     at = 1 - at;
-    return last ? product<false, true>(o, p, s, st) : product<false>(o, p, s, st);
+    return last ? product<false, true>(kApply, o, p, s, st) : product<false>(kApply, o, p, s, st);
   }
   int one(bool last) {
     HMOE_TRY(gram(w.A[0]));
