@@ -319,8 +319,9 @@ __global__ void __launch_bounds__(C::THREADS) k_ortho_product(Ortho o, Product p
 }
 
 // The same for few tiles and short reductions, where a product is all latency: 64 x 64 tiles of four waves, and 128 values of
-// K of both operands to a trip to memory, two trips in flight.  (152 x 152 of 152 on the 128 x 128 tiles, three
-// workgroups: 10 us, and 13 where the result adds A; 152 x 1356 of 152 28.)
+// K of both operands to a trip to memory.  The next trip's loads go out before this one's products, but the barrier
+// between waits for them, too, so that a trip takes a latency of memory and its products, one after the other.  (152 x
+// 152 of 152 on the 128 x 128 tiles, three workgroups: 10 us, and 13 where the result adds A; 152 x 1356 of 152 28.)
 // A K-contiguous operand's row is 512 bytes of LDS, chunk c of 16 bytes at c ^ (row & 15).  A K-strided one's 64 columns are 256
 // bytes of a row of X, hi and lo of 32 columns and of the next 32, chunk c at c ^ sw(k) (ks_off's swizzle).
 struct CfgMid {
@@ -509,7 +510,9 @@ Deal deal_mid(const Ortho& o, int k, bool sym) {
   d.part = (size_t)d.rest * d.split * C::MI * C::NJ * C::THREADS;
   return d;
 }
-// Whether a problem's products are few tiles and short reductions.
+// Whether a problem's products are few tiles and short reductions, by the squares of its small matrices: the Gram matrix
+// and the product with X follow them, however long the other side is (five of 512 x 2048: 1280 tiles of X, five rounds of
+// the CUs).
 bool is_mid(const Ortho& o) {
   const int64_t mt = cdiv(o.r, 128);
   return o.r <= 512 && mt * (mt + 1) / 2 * o.K < device_cus() / 4;
